@@ -80,7 +80,10 @@ enum {
   GDN_TREE_MULTI_ROOT = 2,   /* more than one node with parent -1              */
   GDN_TREE_BAD_PARENT = 3,   /* parent outside {-2,-1,0..T-1}, self, or padding */
   GDN_TREE_CYCLE = 4,        /* a real node whose parent chain misses the root */
-  GDN_TREE_BAD_ACCEPTED = 5  /* commit only: accepted outside [-1,T) or padding */
+  GDN_TREE_BAD_ACCEPTED = 5, /* commit only: accepted outside [-1,T) or padding */
+  GDN_KV_BAD_LEN = 6,  /* paged cache: ctx_len or n_new out of range, or no room in the page table */
+  GDN_KV_BAD_PAGE = 7, /* paged cache: a needed page-table entry outside [0, n_pages) */
+  GDN_KV_BAD_POS = 8   /* paged cache: a position without a row in the rotation table */
 };
 
 /* Problem sizes.  B sequences, T node slots per tree (padded tree size),
@@ -243,6 +246,160 @@ int gdn_tree_step(const gdn_dims* dims, const void* prev_meta, const int32_t* pr
                   const void* alpha, const void* beta, const float* conv_w,
                   const float* conv_state, float* conv_state_out, float* S, float* out,
                   hipStream_t stream);
+
+/* ------------------------------------------------------------------------
+ * Softmax-attention layers of the same decode step
+ *
+ * A model with GDN layers has softmax-attention layers between them.  The
+ * four calls below take the same trees (the metadata of gdn_tree_prepare)
+ * through such a layer and through the sampling that ends the step:
+ * gdn_kv_append, gdn_tree_attend, gdn_tree_sample, gdn_tree_accept; then
+ * gdn_tree_commit / gdn_tree_step for the GDN layers and gdn_kv_commit for
+ * the attention layers take the accepted slot.
+ *
+ * Paged cache.  A sequence's token at position p (0 = the first token of the
+ * prompt) lies in page page_table[b][p / page] at place p % page.  Both
+ * caches hold 16-byte packs of x = 16 / element size values:
+ *   keys    [n_pages][Hkv][d / x][page][x]   packs along the head dim
+ *   values  [n_pages][Hkv][page / x][d][x]   packs along the tokens
+ * which are the operands of the matrix instructions as they stand: the keys
+ * of a tile are rows of 16 bytes, the values columns of 16 bytes.
+ *
+ * Cached tokens fill positions 0 .. ctx_len[b] - 1.  Slot i of the current
+ * tree is kept at position ctx_len[b] + i until the commit, and has the
+ * rotation of position ctx_len[b] + depth(i).
+ *
+ * meta is the tree metadata, or NULL for a chain: slot i's parent is i - 1,
+ * slots 0 .. n_new[b] - 1 are real (n_new NULL: all T).  T = 1 without
+ * metadata is plain decoding, a chain of up to GDN_MAX_T tokens a chunk of a
+ * prompt.  n_new is refused together with meta (padding slots carry it).
+ *
+ * A sequence whose tree status is non-zero, or whose ctx_len is negative or
+ * leaves no room for its slots (ctx_len + T, or + n_new, above max_pages *
+ * page), is skipped: outputs zero, caches untouched.
+ * Page-table entries outside [0, n_pages) are never followed. */
+typedef struct {
+  int32_t B, T;      /* sequences, slots per tree (<= GDN_MAX_T)                 */
+  int32_t Hq, Hkv;   /* query heads, key / value heads; Hq % Hkv == 0, query
+                      * head h reads key / value head floor(h Hkv / Hq)          */
+  int32_t d;         /* head dim: 32, 64, 128 or 256                             */
+  int32_t page;      /* tokens per page: 16, 32, 64, 128 or 256                  */
+  int32_t n_pages;   /* pages of each cache                                      */
+  int32_t max_pages; /* entries in a sequence's row of the page table            */
+  int32_t dtype;     /* GDN_F32 or GDN_BF16: q, k, v, caches and outputs         */
+  int32_t rot;       /* leading dims of a head that are rotated: even, 0 .. d    */
+  int32_t n_pos;     /* rows of the rotation table                               */
+  float scale;       /* of the scores; 0 selects 1 / sqrt(d)                     */
+} gdn_attn_dims;
+
+/* Rotates the step's queries and keys and appends keys and values.
+ *   q [B][T][Hq][d], k, v [B][T][Hkv][d]   dtype, the layer's new rows
+ *   rope        fp32 [n_pos][rot / 2][2]   cos and sin of every position; the
+ *               pair (x[e], x[e + rot / 2]) of a head becomes
+ *               (x[e] cos - x[e + rot / 2] sin, x[e + rot / 2] cos + x[e] sin).
+ *               May be NULL for rot 0.
+ *   ctx_len     int32 [B]; page_table int32 [B][max_pages]
+ *   k_cache, v_cache   written at the positions of the real slots
+ *   q_out       dtype [B][T][Hq][d]  rotated queries, zero for padding slots;
+ *               may be q itself (any other overlap is not allowed)
+ *   kv_status   int32 [B] (may be NULL): the tree status if non-zero, else
+ *               GDN_KV_BAD_LEN, GDN_KV_BAD_POS, GDN_KV_BAD_PAGE (pages of the
+ *               real slots) or 0; non-zero sequences are skipped.
+ * Two sequences must not share a page that either of them writes. */
+int gdn_kv_append(const gdn_attn_dims* dims, const void* meta, const int32_t* n_new, const void* q,
+                  const void* k, const void* v, const float* rope, const int32_t* ctx_len,
+                  const int32_t* page_table, void* k_cache, void* v_cache, void* q_out,
+                  int32_t* kv_status, hipStream_t stream);
+
+/* Attention of every slot over the cached tokens, its ancestors and itself:
+ *   o_i = sum_j p_ij v_j,  p_ij = softmax_j(scale q_i . k_j)
+ *   q    dtype [B][T][Hq][d]   rotated queries (gdn_kv_append's q_out)
+ *   out  dtype [B][T][Hq][d]   written; zero for padding slots.  Must not
+ *        overlap q.
+ * Reads the rows that gdn_kv_append wrote.  Softmax statistics and sums are
+ * fp32; with bf16 the weights p enter the second product rounded to bf16.
+ * Keys of a page whose entry is outside [0, n_pages) are left out.  A row of
+ * a slot that is not visible to a query does not reach it, whatever it holds
+ * (infinities and NaN included), nor do cache rows past the last slot.
+ * Work is split over the cached length when there are few rows; the parts
+ * are joined through a workspace that the library keeps per (device, stream)
+ * as for gdn_tree_verify above 128 slots (a call under stream capture that
+ * would have to grow it returns GDN_EUNSUPPORTED: run the same sizes once
+ * uncaptured first). */
+int gdn_tree_attend(const gdn_attn_dims* dims, const void* meta, const int32_t* n_new, const void* q,
+                    const void* k_cache, const void* v_cache, const int32_t* page_table,
+                    const int32_t* ctx_len, void* out, hipStream_t stream);
+
+/* Moves the rows of the accepted path root..accepted to positions
+ * ctx_len[b] .. ctx_len[b] + depth(accepted), in place.
+ *   accepted   int32 [B]   accepted slot, -1 = nothing
+ *   new_len    int32 [B]   written: ctx_len + depth(accepted) + 1, or ctx_len
+ *              of a sequence that commits nothing; must not overlap ctx_len
+ *   kv_status  int32 [B] (may be NULL): the tree status if non-zero, else
+ *              GDN_TREE_BAD_ACCEPTED, GDN_KV_BAD_LEN, GDN_KV_BAD_PAGE (pages
+ *              of the path's rows, before and after) or 0; non-zero sequences
+ *              are left as they are.
+ * Without metadata (a chain) every row is in place already and only new_len
+ * is written; the page table then needs room up to the accepted slot. */
+int gdn_kv_commit(const gdn_attn_dims* dims, const void* meta, const int32_t* accepted,
+                  const int32_t* page_table, const int32_t* ctx_len, void* k_cache, void* v_cache,
+                  int32_t* new_len, int32_t* kv_status, hipStream_t stream);
+
+/* Problem sizes of gdn_tree_sample.  ld: elements from one row of logits to
+ * the next, 0 selects V.  1 <= V <= GDN_MAX_V. */
+typedef struct {
+  int32_t B, T, V;
+  int32_t dtype; /* GDN_F32 or GDN_BF16: logits */
+  int64_t ld;
+} gdn_sample_dims;
+
+#define GDN_MAX_V (1 << 20)
+
+/* Samples one token per slot from its logits with a given random number.
+ *   meta        tree metadata or NULL (all slots real); a padding slot and a
+ *               sequence with a non-zero tree status get token -1, and their
+ *               logits are not read
+ *   logits      dtype [B][T][ld]
+ *   temperature fp32 [B]  NULL = 1; 0 (or less, or NaN): the largest logit,
+ *               the lowest index of equal ones
+ *   top_k       int32 [B] NULL or <= 0: all; else the k largest logits
+ *   top_p       fp32 [B]  NULL or >= 1: all; else, in falling order, a token
+ *               stays while the mass before it is below top_p times the mass
+ *               that top_k left; the first one always stays
+ *   min_p       fp32 [B]  NULL or <= 0: all; else a token stays if its
+ *               probability is at least min_p (at most 1) times the largest
+ *   u           fp32 [B][T] in [0, 1)
+ *   token       int32 [B][T] written: the first index, in vocabulary order,
+ *               at which the running mass of the tokens that stay exceeds u
+ *               times their whole mass; -1 if no logit is above -inf
+ * Equal logits count in order of their index; NaN counts as -inf; +inf
+ * logits share the whole mass.
+ * The mass of a token is round(2^31 * 2^((z - z_max) log2(e) / temperature)),
+ * a whole number, so that no sum depends on its order and equal inputs give
+ * equal tokens however the work is split. */
+int gdn_tree_sample(const gdn_sample_dims* dims, const void* meta, const void* logits,
+                    const float* temperature, const int32_t* top_k, const float* top_p,
+                    const float* min_p, const float* u, int32_t* token, hipStream_t stream);
+
+/* Acceptance along the sampled tokens (Eq. 1-2, on a tree): from
+ * the root, the child whose draft token is the one sampled at the current
+ * node becomes the current node (the lowest slot of equal siblings); where
+ * there is none the walk ends.  Every emitted token is then a sample of the
+ * model given the tokens before it.  Reads only dims->B and dims->T.
+ *   meta       tree metadata, or NULL for a chain of T slots
+ *   draft      int32 [B][T]  token of every slot (the root's is not read as a
+ *              draft: it is the last emitted token)
+ *   token      int32 [B][T]  gdn_tree_sample's
+ *   accepted   int32 [B]     written: last node of the walk, for
+ *              gdn_tree_commit, gdn_tree_step and gdn_kv_commit; -1 for an
+ *              empty tree or one with a non-zero status
+ *   n_emitted  int32 [B]     written: depth(accepted) + 1
+ *   emitted    int32 [B][T]  written: the tokens below the root, then the one
+ *              sampled at the accepted node, then -1
+ * A negative token matches no draft. */
+int gdn_tree_accept(const gdn_dims* dims, const void* meta, const int32_t* draft,
+                    const int32_t* token, int32_t* accepted, int32_t* n_emitted, int32_t* emitted,
+                    hipStream_t stream);
 
 /* Message describing the last non-OK return on the calling thread. */
 const char* gdn_last_error(void);
