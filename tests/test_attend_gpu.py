@@ -221,11 +221,14 @@ def test_graph(A):
         A.attend(d, qo, g["kc"], g["vc"], g["table"], g["ctx"], out, meta=g["meta"])
         A.kv_commit(d, acc, g["table"], g["ctx"], g["kc"], g["vc"], new_len, meta=g["meta"])
 
-    step()
+    s = torch.cuda.Stream()
+    kc0, vc0 = g["kc"].clone(), g["vc"].clone()
+    torch.cuda.synchronize()
+    with torch.cuda.stream(s):
+        step()  # the workspace belongs to the stream: allocated before the capture
     torch.cuda.synchronize()
     graph = torch.cuda.CUDAGraph()
-    kc0, vc0 = g["kc"].clone(), g["vc"].clone()
-    with torch.cuda.graph(graph):
+    with torch.cuda.graph(graph, stream=s):
         step()
     for n in range(4):
         g["ctx"].copy_(c.i32(np.maximum(0, c.ctx - 7 * n)))
