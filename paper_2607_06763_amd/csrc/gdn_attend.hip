@@ -17,6 +17,8 @@
 // to the workspace with their maximum and sum and are joined by a second
 // kernel.  The lengths are on the device: every workgroup finds its run by a
 // scan over them.
+#include <limits.h>
+
 #include "gdn_attn.h"
 
 namespace gdn {
@@ -192,6 +194,12 @@ __device__ __forceinline__ u64 seen_bits(const AttnArgs& a, const MetaPtrs& m, i
   return r ? (lo >> r) | (word(k + 1) << (64 - r)) : lo;
 }
 
+// x where bit n of seen is set, else -inf.
+__device__ __forceinline__ float where_seen(float x, unsigned seen, int n) {
+  const int on = __builtin_amdgcn_sbfe(int(seen), n, 1);  // 0 or -1
+  return __int_as_float((__float_as_int(x) & on) | (0xff800000 & ~on));
+}
+
 // ---------------------------------------------------------------------------
 // State of one wave's 32 rows
 // ---------------------------------------------------------------------------
@@ -245,41 +253,6 @@ struct Rows {
       }
     l += sum[0] + sum[1];
   }
-
-  // Values that are not finite take part by themselves, after a product that
-  // ran without them: the matrix units count, for every row and channel, the
-  // visible keys that hold +inf (or NaN) and -inf (or NaN).  value(q, k): the
-  // pack as the cache holds it, seen: this lane's visible keys of 32.
-  template <typename V>
-  __device__ __forceinline__ void add_bad(unsigned seen, V value) {
-    const int half = (threadIdx.x >> 5) & 1;
-    const float one = 1.0f, none = 0.0f;
-#pragma unroll
-    for (int k = 0; k < D / 32; ++k) {
-      f32x16 up = {}, down = {};
-#pragma unroll
-      for (int q = 0; q < 32 / (2 * X); ++q) {
-        const Frag f = value(q, k);
-        float on[X], hi[X], lo[X];
-#pragma unroll
-        for (int e = 0; e < X; ++e) {
-          const unsigned x = M::bits(f, e);
-          const bool inf = (x & kExp) == kExp, nan = inf && (x & 0x7fffffu);
-          on[e] = (seen >> (q * 2 * X + half * X + e)) & 1 ? one : none;
-          hi[e] = nan || (inf && !(x >> 31)) ? one : none;
-          lo[e] = nan || (inf && (x >> 31)) ? one : none;
-        }
-        up = M::mma(M::pack(hi), M::pack(on), up);
-        down = M::mma(M::pack(lo), M::pack(on), down);
-      }
-#pragma unroll
-      for (int i = 0; i < 16; ++i) {
-        o[k][i] += up[i] > 0.0f ? INFINITY : 0.0f;
-        o[k][i] += down[i] > 0.0f ? -INFINITY : 0.0f;
-      }
-      __builtin_amdgcn_sched_barrier(0);
-    }
-  }
 };
 
 // Position of a lane's row: slot, and whether the slot is real.
@@ -310,6 +283,39 @@ __device__ __forceinline__ void store4(BF16* p, float4 x) {
   *reinterpret_cast<bf16x4*>(p) = bf16x4{(__bf16)x.x, (__bf16)x.y, (__bf16)x.z, (__bf16)x.w};
 }
 
+__device__ __forceinline__ float4 fetch4(const float* p) { return *reinterpret_cast<const float4*>(p); }
+__device__ __forceinline__ float4 fetch4(const BF16* p) { return ld4(p); }
+
+// Where some slots are masked, the product runs without the values that are
+// not finite (0 times infinity is not 0).  This adds them to 4 channels of
+// what a row has written: those of the keys from position `from` up to `to`
+// that the row sees.
+template <typename T, typename O>
+__device__ void add_not_finite(const AttnArgs& a, const MetaPtrs& m, int b, int h, int slot, int ctx, int from, int to,
+                               int d, O* out) {
+  constexpr int X = Pack<T>::kN;
+  const int32_t* row = a.page_table + size_t(b) * a.c.max_pages;
+  const int mask = (1 << a.c.page_shift) - 1;
+  float x[4] = {};
+  for (int p0 = from; p0 < to; p0 += 64) {
+    u64 seen = seen_bits(a, m, b, slot, ctx, p0);
+    if (to - p0 < 64) seen &= (u64(1) << (to - p0)) - 1;
+    for (; seen; seen &= seen - 1) {
+      const int p = p0 + __builtin_ctzll(seen), id = page_of(a.c, row, p);
+      if (id < 0) continue;
+      const T* v = reinterpret_cast<const T*>(a.v_cache) + block_of(a.c, id, h) +
+                   (size_t((p & mask) / X) * a.c.d + d) * X + p % X;
+#pragma unroll
+      for (int e = 0; e < 4; ++e) {
+        const float y = to_f32(v[e * X]);
+        if ((__float_as_uint(y) & kExp) == kExp) x[e] += y;
+      }
+    }
+  }
+  const float4 o = fetch4(out);
+  store4(out, make_float4(o.x + x[0], o.y + x[1], o.z + x[2], o.w + x[3]));
+}
+
 // ---------------------------------------------------------------------------
 // Few rows: a workgroup's four waves share a tile of 32 rows and take 32 keys
 // each of a tile of 128.  Keys and values go from memory to the operand
@@ -321,7 +327,7 @@ constexpr int kStreamKeys = 32 * kWaves;
 
 template <int D>
 constexpr size_t stream_lds() {
-  return sizeof(float) * kWaves * 32 * (D + 4) + sizeof(float2) * kWaves * 32;
+  return sizeof(float) * kWaves * 32 * (D + 4) + sizeof(float2) * kWaves * 32 + 16;
 }
 
 // Registers of a wave: Q, K, V of 32 keys and O take D (2 X 4 / X^2 ..) each;
@@ -340,6 +346,8 @@ __global__ __launch_bounds__(kThreads, (stream_groups<T, D>())) void attend_stre
   extern __shared__ __align__(16) char s_raw[];
   float* s_o = reinterpret_cast<float*>(s_raw);                       // [wave][row][D + 4]
   float2* s_ml = reinterpret_cast<float2*>(s_o + kWaves * 32 * (D + 4));  // [wave][row]
+  int* s_from = reinterpret_cast<int*>(s_ml + kWaves * 32);  // first tile with values left out, two segments in turn
+  int turn = 0;
   const int tid = threadIdx.x, lane = tid % kWave, w = uniform(tid / kWave), n32 = lane & 31, h2 = lane >> 5;
   const int u = blockIdx.x, h = blockIdx.y, rt = blockIdx.z;
   const int M = a.T * (a.Hq / a.c.Hkv);
@@ -356,7 +364,7 @@ __global__ __launch_bounds__(kThreads, (stream_groups<T, D>())) void attend_stre
   const T *kc = reinterpret_cast<const T*>(a.k_cache), *vc = reinterpret_cast<const T*>(a.v_cache);
   const int mask = (1 << a.c.page_shift) - 1, shift = a.c.page_shift;
   const float c = a.scale * kLog2e;
-  for (; g < end; ++b) {
+  for (; g < end; ++b, s_from += turn ? -1 : 1, turn ^= 1) {
     const int tiles = uniform(tiles_of(a, b, kStreamKeys));
     const int t0 = int(g - start), n = int(min((long long)(tiles), end - start)) - t0;
     const bool whole = n == tiles;
@@ -394,6 +402,7 @@ __global__ __launch_bounds__(kThreads, (stream_groups<T, D>())) void attend_stre
     };
     // waves past the end have nothing to load
     const int last = min((t0 + n) * kStreamKeys, len < 0 ? 0 : len);
+    int from = INT_MAX;
     if (p0 < last) pages(p0);
     if constexpr (kAhead) {
       // context: every row sees every key.  The next tile's keys load behind
@@ -447,9 +456,9 @@ __global__ __launch_bounds__(kThreads, (stream_groups<T, D>())) void attend_stre
       const unsigned seen = masked ? unsigned(seen_bits(a, m, b, at.slot, ctx, p0)) & valid : ~0u;
       float s[1][16];
 #pragma unroll
-      for (int i = 0; i < 16; ++i) s[0][i] = (seen >> (i / X * 2 * X + h2 * X + i % X)) & 1 ? acc[i] : -INFINITY;
+      for (int i = 0; i < 16; ++i) s[0][i] = where_seen(acc[i], seen >> (h2 * X), i / X * 2 * X + i % X);
       st.template softmax<1>(s, c);
-      bool bad = false;
+      bool left = false;
 #pragma unroll
       for (int q = 0; q < NS; ++q) {
         const Frag p = Mt::pack(&s[0][q * X]);
@@ -461,7 +470,7 @@ __global__ __launch_bounds__(kThreads, (stream_groups<T, D>())) void attend_stre
 #pragma unroll
             for (int e = 0; e < X; ++e)
               if (!((ok >> e) & 1) || (Mt::bits(f, e) & kExp) == kExp) {
-                bad = bad || ((ok >> e) & 1);
+                left = left || ((ok >> e) & 1);
                 f = Mt::without(f, e);
               }
           }
@@ -469,17 +478,11 @@ __global__ __launch_bounds__(kThreads, (stream_groups<T, D>())) void attend_stre
         }
         __builtin_amdgcn_sched_barrier(0);  // one row of value packs in registers at a time
       }
-      if (__any(bad))
-        st.add_bad(seen, [&](int q, int k) {
-          Frag f = v_pack(q, k);
-#pragma unroll
-          for (int e = 0; e < X; ++e)
-            if (!((valid >> (q * 2 * X + h2 * X + e)) & 1)) f = Mt::without(f, e);
-          return f;
-        });
+      if (from == INT_MAX && __any(left)) from = p0;
     }
 
     // join the waves
+    if (tid == 0) *s_from = INT_MAX;
     const float l = half_sum(st.l);
     if (h2 == 0) s_ml[w * 32 + n32] = make_float2(st.m, l);
     if (r < M) {
@@ -491,6 +494,7 @@ __global__ __launch_bounds__(kThreads, (stream_groups<T, D>())) void attend_stre
               make_float4(st.o[k][4 * i], st.o[k][4 * i + 1], st.o[k][4 * i + 2], st.o[k][4 * i + 3]);
     }
     __syncthreads();
+    if (from != INT_MAX && lane == 0) atomicMin(s_from, from);
     const int rows = min(32, M - rt * 32);
     for (int x = tid; x < rows * (D / 4); x += kThreads) {
       const int rr = x / (D / 4), d = x % (D / 4) * 4;
@@ -521,6 +525,229 @@ __global__ __launch_bounds__(kThreads, (stream_groups<T, D>())) void attend_stre
       }
     }
     __syncthreads();  // before the next sequence's part overwrites the waves' rows
+    if (*s_from != INT_MAX) {
+      from = *s_from;
+      for (int x = tid; x < rows * (D / 4); x += kThreads) {
+        const int rr = x / (D / 4), d = x % (D / 4) * 4;
+        const RowAt to = row_at(a, m, b, h, rt * 32 + rr, M, false);
+        if (!to.real) continue;
+        const int upto = min((t0 + n) * kStreamKeys, len);
+        if (whole)
+          add_not_finite<T>(a, m, b, h, to.slot, ctx, from, upto, d, reinterpret_cast<T*>(a.out) + row_offset<T>(a, b, to) + d);
+        else
+          add_not_finite<T>(a, m, b, h, to.slot, ctx, from, upto, d,
+                            ws.o + ((size_t(slot) * a.c.Hkv + h) * M + rt * 32 + rr) * D + d);
+      }
+      __syncthreads();
+    }
+  }
+}
+
+// ---------------------------------------------------------------------------
+// Many rows (bf16): four waves of 32 rows each share key and value tiles in
+// LDS, double-buffered and loaded past the registers.  The cache's packs are
+// the operand layout, so a tile is copied as it stands and read without bank
+// conflicts (32 lanes read 512 contiguous bytes).
+// ---------------------------------------------------------------------------
+template <int D>
+struct Tile {
+  static constexpr int kKeys = D <= 128 ? 64 : 32;
+  static constexpr int kPacks = kKeys * D / 8;          // of either half
+  static constexpr int kPer = kPacks / kThreads;        // loads of a thread
+  static constexpr size_t kLds = 2 * 2 * kPacks * 16 + 16;
+};
+constexpr int kTileRows = 32 * kWaves;
+
+__device__ __forceinline__ void load_to_lds(const void* src, void* dst) {
+  __builtin_amdgcn_global_load_lds((const __attribute__((address_space(1))) void*)(src),
+                                   (__attribute__((address_space(3))) void*)(dst), 16, 0, 0);
+}
+
+template <int D>
+__global__ __launch_bounds__(kThreads, 2) void attend_tile_kernel(AttnArgs a, int S, int rts, Parts ws) {
+  typedef Tile<D> Tl;
+  typedef Mat<BF16> Mt;
+  typedef Mt::Frag Frag;
+  constexpr int KT = Tl::kKeys, NB = KT / 32;
+  extern __shared__ __align__(16) char s_raw[];
+  uint4* s_kv = reinterpret_cast<uint4*>(s_raw);  // [buffer][K [D / 8][KT], V [KT / 8][D]]
+  int* s_from = reinterpret_cast<int*>(s_kv + 4 * Tl::kPacks);  // first tile with values left out
+  const int tid = threadIdx.x, lane = tid % kWave, w = uniform(tid / kWave), n32 = lane & 31, h2 = lane >> 5;
+  const int M = a.T * (a.Hq / a.c.Hkv);
+  // the row tiles of a run and key head on one XCD, whose L2 they share
+  const int x = blockIdx.x % 8, y = blockIdx.x / 8, rt = y % rts, uh = y / rts * 8 + x;
+  const int u = uh / a.c.Hkv, h = uh % a.c.Hkv;
+  if (u >= S) return;
+  long long total;
+  const long long run = run_length(a, S, KT, &total);
+  long long g = u * run;
+  const long long end = g + run < total ? g + run : total;
+  if (g >= end) return;
+  int b;
+  long long start;
+  find_tile(a, g, KT, &b, &start);
+
+  const MetaPtrs m = meta_ptrs(a.meta, a.B, a.T);
+  const BF16 *kc = reinterpret_cast<const BF16*>(a.k_cache), *vc = reinterpret_cast<const BF16*>(a.v_cache);
+  const int shift = a.c.page_shift, mask = (1 << shift) - 1;
+  const float c = a.scale * kLog2e;
+  for (; g < end; ++b) {
+    const int tiles = uniform(tiles_of(a, b, KT));
+    const int t0 = int(g - start), t1 = int(min((long long)(tiles), end - start));
+    const bool whole = t1 - t0 == tiles;
+    const int slot = 2 * u + (g > u * run ? 1 : 0);
+    start += tiles;
+    g = start;
+
+    const int len = uniform(length_of(a, b)), ctx = uniform(a.ctx_len[b]);
+    const int r = rt * kTileRows + w * 32 + n32;
+    const RowAt at = row_at(a, m, b, h, r, M, len < 0);
+    const int32_t* row = a.page_table + size_t(b) * a.c.max_pages;
+    Rows<BF16, D> st;
+    st.clear();
+    st.load_q(at.real ? reinterpret_cast<const BF16*>(a.q) + row_offset<BF16>(a, b, at) : nullptr, h2);
+
+    // page of the lane's key of a tile, -1: none
+    auto page_at = [&](int t) {
+      const int p = t * KT + lane % KT;
+      return t < t1 && p < len ? page_of(a.c, row, p) : -1;
+    };
+    auto stage = [&](int t, int id, int buf) {
+      const int p0 = t * KT;
+      uint4* sk = s_kv + buf * 2 * Tl::kPacks;
+      const BF16* kl = kc + block_of(a.c, id < 0 ? 0 : id, h) + size_t((p0 + lane % KT) & mask) * 8;
+#pragma unroll
+      for (int n = 0; n < Tl::kPer; ++n) {
+        const int at0 = (n * kWaves + w) * kWave;  // packs at0 + lane
+        load_to_lds(kl + (size_t(at0 / KT + lane / KT) << shift) * 8, sk + at0);
+      }
+#pragma unroll
+      for (int n = 0; n < Tl::kPer; ++n) {
+        const int at0 = (n * kWaves + w) * kWave, q = at0 + lane, grp = q / D;
+        const int vid = __shfl(id, grp * 8);
+        load_to_lds(vc + block_of(a.c, vid < 0 ? 0 : vid, h) + (size_t((p0 + grp * 8) & mask) / 8 * D + q % D) * 8,
+                    sk + Tl::kPacks + at0);
+      }
+    };
+    const int stop = len < 0 ? t0 : t1;  // a skipped sequence has nothing to load
+    int id = page_at(t0), id1 = page_at(t0 + 1);
+    __syncthreads();  // the buffers are free
+    if (tid == 0) *s_from = INT_MAX;
+    if (t0 < stop) stage(t0, id, 0);
+    const u64 all = KT == 64 ? ~u64(0) : 0xffffffffu;
+    int t = t0;
+    u64 valid = 0;
+    uint4 *sk = nullptr, *sv = nullptr;
+    // waits for tile t and starts the next one
+    auto enter = [&]() {
+      asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
+      __syncthreads();
+      sk = s_kv + ((t - t0) & 1) * 2 * Tl::kPacks;
+      sv = sk + Tl::kPacks;
+      if (t + 1 < stop) stage(t + 1, id1, (t + 1 - t0) & 1);
+      id = id1;
+      id1 = page_at(t + 2);
+    };
+    auto scores = [&](float (&s)[NB][16]) {
+#pragma unroll
+      for (int nb = 0; nb < NB; ++nb) {
+        f32x16 acc = {};
+        const uint4* kr = sk + h2 * KT + nb * 32 + Mt::key_of(n32);
+#pragma unroll
+        for (int k = 0; k < D / 16; ++k) acc = Mt::mma(load16<Frag>(kr + 2 * k * KT), st.q[k], acc);
+#pragma unroll
+        for (int i = 0; i < 16; ++i) s[nb][i] = acc[i];
+      }
+    };
+    auto sums = [&](const float (&s)[NB][16]) {
+#pragma unroll
+      for (int nb = 0; nb < NB; ++nb)
+#pragma unroll
+        for (int q = 0; q < 2; ++q) {
+          const Frag p = Mt::pack(&s[nb][q * 8]);
+          const uint4* vr = sv + (nb * 4 + q * 2 + h2) * D + n32;
+#pragma unroll
+          for (int k = 0; k < D / 32; ++k) st.o[k] = Mt::mma(load16<Frag>(vr + k * 32), p, st.o[k]);
+        }
+    };
+    // keys that the tile holds (NB = 1: both halves of the wave hold the same)
+    auto held = [&]() { return __ballot(id >= 0) & all; };
+    // context: every row sees every key
+    for (; t < stop && (t + 1) * KT <= ctx; ++t) {
+      valid = held();
+      if (valid != all) break;
+      enter();
+      float s[NB][16];
+      scores(s);
+      st.template softmax<NB>(s, c);
+      sums(s);
+    }
+    // slots of the tree, the end of the cache and pages that are left out
+    for (; t < stop; ++t) {
+      const int p0 = t * KT;
+      valid = held();
+      enter();
+      // values of absent keys, and those that are not finite, out of the
+      // product: a masked weight is 0, and must stay so whatever it meets
+      bool mine = false;
+      for (int q = tid; q < Tl::kPacks; q += kThreads) {
+        const unsigned ok = unsigned(valid >> (q / D * 8)) & 0xffu;
+        Frag f = load16<Frag>(sv + q);
+        bool change = false;
+#pragma unroll
+        for (int e = 0; e < 8; ++e) {
+          const bool on = (ok >> e) & 1;
+          if (!on || (Mt::bits(f, e) & kExp) == kExp) {
+            mine = mine || on;
+            change = true;
+            f = Mt::without(f, e);
+          }
+        }
+        if (change) *reinterpret_cast<Frag*>(sv + q) = f;
+      }
+      if (mine) atomicMin(s_from, p0);
+      __syncthreads();
+      float s[NB][16];
+      scores(s);
+      const u64 seen = seen_bits(a, m, b, at.slot, ctx, p0) & valid;
+#pragma unroll
+      for (int nb = 0; nb < NB; ++nb)
+#pragma unroll
+        for (int i = 0; i < 16; ++i) s[nb][i] = where_seen(s[nb][i], unsigned(seen >> (nb * 32)) >> (h2 * 8), i / 8 * 16 + i % 8);
+      st.template softmax<NB>(s, c);
+      sums(s);
+    }
+
+    __syncthreads();
+    const int from = *s_from;
+    const float l = half_sum(st.l);
+    if (r < M) {
+      const bool on = at.real && l != 0.0f;
+      const float inv = on ? 1.0f / l : 0.0f;
+      const size_t i = (size_t(slot) * a.c.Hkv + h) * M + r;
+      BF16* out = reinterpret_cast<BF16*>(a.out) + row_offset<BF16>(a, b, at);
+      if (!whole && h2 == 0) ws.ml[i] = make_float2(st.m, l);
+#pragma unroll
+      for (int k = 0; k < D / 32; ++k)
+#pragma unroll
+        for (int e = 0; e < 4; ++e) {
+          const int d = k * 32 + 8 * e + 4 * h2;
+          float4 o = make_float4(st.o[k][4 * e], st.o[k][4 * e + 1], st.o[k][4 * e + 2], st.o[k][4 * e + 3]);
+          if (whole)
+            store4(out + d, on ? make_float4(o.x * inv, o.y * inv, o.z * inv, o.w * inv) : make_float4(0, 0, 0, 0));
+          else
+            *reinterpret_cast<float4*>(ws.o + i * D + d) = o;
+        }
+      if (from != INT_MAX && at.real) {  // on what this lane has written
+        const int upto = min(t1 * KT, len);
+#pragma unroll 1
+        for (int x = 0; x < D / 8; ++x) {
+          const int d = 8 * x + 4 * h2;
+          if (whole) add_not_finite<BF16>(a, m, b, h, at.slot, ctx, from, upto, d, out + d);
+          else add_not_finite<BF16>(a, m, b, h, at.slot, ctx, from, upto, d, ws.o + i * D + d);
+        }
+      }
+    }
   }
 }
 
@@ -580,39 +807,71 @@ int runs_for(long long blocks, long long slots) {
   return int(best);
 }
 
+// Workspace of S runs.
+int parts_for(const AttnArgs& a, int S, hipStream_t stream, Parts* ws) {
+  const size_t rows = size_t(2) * S * a.c.Hkv * a.T * (a.Hq / a.c.Hkv);
+  int rc = GDN_OK;
+  char* p = static_cast<char*>(stream_workspace(rows * (a.c.d * sizeof(float) + sizeof(float2)), stream, &rc));
+  if (!p) return rc;
+  *ws = {reinterpret_cast<float*>(p), reinterpret_cast<float2*>(p + rows * a.c.d * sizeof(float))};
+  return GDN_OK;
+}
+
+template <typename T>
+int launch_join(const AttnArgs& a, int S, int kt, const Parts& ws, hipStream_t stream) {
+  if (S == 1) return GDN_OK;  // no sequence is shared
+  const int M = a.T * (a.Hq / a.c.Hkv), per = kThreads / (a.c.d / 4);
+  attend_join_kernel<T><<<dim3((M + per - 1) / per, a.c.Hkv, a.B), kThreads, 0, stream>>>(a, S, kt, ws);
+  return after_launch();
+}
+
 template <typename T, int D>
 int launch_stream(const AttnArgs& a, hipStream_t stream) {
   const int M = a.T * (a.Hq / a.c.Hkv), rt = (M + 31) / 32;
   const int S = runs_for((long long)(a.c.Hkv) * rt, 256 * stream_groups<T, D>());
-  const size_t rows = size_t(2) * S * a.c.Hkv * M;
-  int rc = GDN_OK;
-  char* p = static_cast<char*>(stream_workspace(rows * (D * sizeof(float) + sizeof(float2)), stream, &rc));
-  if (!p) return rc;
-  const Parts ws = {reinterpret_cast<float*>(p), reinterpret_cast<float2*>(p + rows * D * sizeof(float))};
+  Parts ws;
+  int rc = parts_for(a, S, stream, &ws);
+  if (rc != GDN_OK) return rc;
   constexpr size_t lds = stream_lds<D>();
   rc = ensure_dynamic_lds(reinterpret_cast<const void*>(attend_stream_kernel<T, D>), int(lds), "attend");
   if (rc != GDN_OK) return rc;
   attend_stream_kernel<T, D><<<dim3(S, a.c.Hkv, rt), kThreads, lds, stream>>>(a, S, ws);
-  if ((rc = after_launch()) != GDN_OK || S == 1) return rc;
-  const int per = kThreads / (D / 4);
-  attend_join_kernel<T><<<dim3((M + per - 1) / per, a.c.Hkv, a.B), kThreads, 0, stream>>>(a, S, kStreamKeys, ws);
-  return after_launch();
+  rc = after_launch();
+  return rc != GDN_OK ? rc : launch_join<T>(a, S, kStreamKeys, ws, stream);
 }
 
-template <typename T>
-int launch_type(const AttnArgs& a, hipStream_t stream) {
-  switch (a.c.d) {
-    case 32: return launch_stream<T, 32>(a, stream);
-    case 64: return launch_stream<T, 64>(a, stream);
-    case 128: return launch_stream<T, 128>(a, stream);
-    default: return launch_stream<T, 256>(a, stream);
-  }
+template <int D>
+int launch_tile(const AttnArgs& a, hipStream_t stream) {
+  const int M = a.T * (a.Hq / a.c.Hkv), rt = (M + kTileRows - 1) / kTileRows;
+  const int S = runs_for((long long)(a.c.Hkv) * rt, 512);
+  Parts ws;
+  int rc = parts_for(a, S, stream, &ws);
+  if (rc != GDN_OK) return rc;
+  constexpr size_t lds = Tile<D>::kLds;
+  rc = ensure_dynamic_lds(reinterpret_cast<const void*>(attend_tile_kernel<D>), int(lds), "attend");
+  if (rc != GDN_OK) return rc;
+  const int groups = (S * a.c.Hkv + 7) / 8 * 8;
+  attend_tile_kernel<D><<<groups * rt, kThreads, lds, stream>>>(a, S, rt, ws);
+  rc = after_launch();
+  return rc != GDN_OK ? rc : launch_join<BF16>(a, S, Tile<D>::kKeys, ws, stream);
+}
+
+template <int D>
+int launch_dim(const AttnArgs& a, hipStream_t stream) {
+  if (a.dtype != GDN_BF16) return launch_stream<float, D>(a, stream);
+  if (a.T * (a.Hq / a.c.Hkv) > 32) return launch_tile<D>(a, stream);
+  return launch_stream<BF16, D>(a, stream);
 }
 
 }  // namespace
 
 int launch_attend(const AttnArgs& a, hipStream_t stream) {
-  return a.dtype == GDN_BF16 ? launch_type<BF16>(a, stream) : launch_type<float>(a, stream);
+  switch (a.c.d) {
+    case 32: return launch_dim<32>(a, stream);
+    case 64: return launch_dim<64>(a, stream);
+    case 128: return launch_dim<128>(a, stream);
+    default: return launch_dim<256>(a, stream);
+  }
 }
 
 }  // namespace gdn
