@@ -23,8 +23,8 @@ namespace {
 // top_p alone (or a k above the number of threads) takes the masses of bins of
 // (top - z) c, the logits of the bin that holds the cut, and the masses that
 // stay in vocabulary order; no cut at all takes the last of these only.
-// Rows for which LDS is too small (thousands of equal logits, a low min_p) are
-// left to a second kernel.
+// Rows for which LDS is too small (thousands of equal logits) take the cuts by
+// halving the value.
 // ---------------------------------------------------------------------------
 constexpr int kBins = 1024;
 constexpr float kBinsPerOctave = kBins / 32.0f;  // w is 0 beyond 32 octaves
@@ -37,10 +37,31 @@ struct Cut {
   int i;
 };
 
+// A listed logit: its place in the order as one number (larger is ahead: the
+// value's ordered bits, then the inverted index) and its mass.
 struct alignas(16) Item {
-  float z;
-  int i;
+  u64 key;
   unsigned w, none;
+};
+
+// ordered image of a float: larger value, larger image
+__device__ __forceinline__ unsigned ordered(float z) {
+  const unsigned b = __float_as_uint(z + 0.0f);  // -0 as 0
+  return b >> 31 ? ~b : b | 0x80000000u;
+}
+__device__ __forceinline__ float unordered(unsigned k) { return __uint_as_float(k >> 31 ? k & 0x7fffffffu : ~k); }
+__device__ __forceinline__ u64 key_of(float z, int i) { return u64(ordered(z)) << 32 | unsigned(~i); }
+__device__ __forceinline__ float value_of(u64 key) { return unordered(unsigned(key >> 32)); }
+__device__ __forceinline__ int index_of(u64 key) { return int(~unsigned(key)); }
+
+// What a cut asks of a logit, given the count and the mass of those ahead.
+struct Before {
+  bool by_count;
+  int k;
+  double want;
+  __device__ __forceinline__ bool operator()(u64 cnt, u64 mass) const {
+    return by_count ? cnt < u64(k) : mass == 0 || double(mass) < want;
+  }
 };
 
 template <int NT>
@@ -49,7 +70,7 @@ struct Shared {
   u64 mass[kBins];
   unsigned cnt[kBins];
   Item list[kList];  // listed logits, their indices and masses
-  unsigned short sub[kList];  // places in the list
+  alignas(16) unsigned short sub[kList];  // places in the list
   u64 red[kWaves];
   unsigned redc[kWaves];
   float redf[kWaves];
@@ -102,7 +123,7 @@ __device__ __forceinline__ u64 block_sum(u64 v, Shared<NT>& s) {
 }
 
 // loaded for a row without a whole vector
-__device__ const u32x4 g_low = {0xff800000u, 0xff800000u, 0xff800000u, 0xff800000u};
+__device__ u32x4 g_low = {0xff800000u, 0xff800000u, 0xff800000u, 0xff800000u};
 
 // A row of logits in 16-byte vectors.  A row may start anywhere: vector j
 // holds elements j X - lead .. + X - 1, those outside the row are -inf.  Wave
@@ -146,6 +167,7 @@ struct Row {
   __device__ __forceinline__ int base(int w, int j) const { return (w * per + j) * kWave; }
   __device__ __forceinline__ int at(int w, int j) const { return base(w, j) + int(threadIdx.x) % kWave; }
   __device__ __forceinline__ int first(int v) const { return v * X - lead; }
+  __device__ __forceinline__ int wave_of(int i) const { return (i + lead) / X / kWave / per; }
   // what is in memory of vector v, or of another one
   __device__ __forceinline__ u32x4 load(int v) const { return vec[max(0, min(v, whole - 1))]; }
   // whether the load needs mending: the row's ends, and past them
@@ -168,13 +190,14 @@ struct Row {
 
 // f(z, i) for every logit of the loads j0 .. j1 - 1 of wave w's part, a few at
 // a time.  A NaN fails every comparison of f.
-template <typename T, int NT, typename F>
+template <int kAhead, typename T, int NT, typename F>
 __device__ __forceinline__ void each_of(const Row<T, NT>& row, int w, int j0, int j1, F f) {
-  constexpr int X = Row<T, NT>::X, kAhead = 8;
+  constexpr int X = Row<T, NT>::X;
   for (int j = j0; j < j1; j += kAhead) {
     u32x4 x[kAhead];
 #pragma unroll
     for (int k = 0; k < kAhead; ++k) x[k] = row.load(row.at(w, j + k));
+    __builtin_amdgcn_sched_barrier(0);
 #pragma unroll
     for (int k = 0; k < kAhead; ++k) {
       if (j + k >= j1) break;
@@ -186,8 +209,8 @@ __device__ __forceinline__ void each_of(const Row<T, NT>& row, int w, int j0, in
   }
 }
 
-// The same for the vectors that hold a logit for which test(z) is true: a
-// comparison or two a logit where few vectors do.
+// test(z) for every logit; f(z, i) for all of a vector in which it was true for
+// one: few instructions a logit where few vectors are hit.
 template <typename T, int NT, typename P, typename F>
 __device__ __forceinline__ void each_if(const Row<T, NT>& row, P test, F f) {
   constexpr int X = Row<T, NT>::X, kAhead = 8;
@@ -196,57 +219,51 @@ __device__ __forceinline__ void each_if(const Row<T, NT>& row, P test, F f) {
     u32x4 x[kAhead];
 #pragma unroll
     for (int k = 0; k < kAhead; ++k) x[k] = row.load(row.at(w, j + k));
+    __builtin_amdgcn_sched_barrier(0);
     unsigned hits = 0;
 #pragma unroll
     for (int k = 0; k < kAhead; ++k) {
+      if (j + k >= row.per) break;
       if (row.edge(w, j + k)) x[k] = row.mend(x[k], row.at(w, j + k));
       bool hit = false;
 #pragma unroll
       for (int e = 0; e < X; ++e) hit = hit | test(Row<T, NT>::value(x[k], e));
-      hits |= (hit && j + k < row.per ? 1u : 0u) << k;
+      hits |= (hit ? 1u : 0u) << k;
     }
     for (; hits; hits &= hits - 1) {
       const int v = row.at(w, j + __builtin_ctz(hits));
       const u32x4 y = row.mend(row.load(v), v);
 #pragma unroll
-      for (int e = 0; e < X; ++e) {
-        const float z = Row<T, NT>::value(y, e);
-        if (test(z)) f(z, row.first(v) + e);
-      }
+      for (int e = 0; e < X; ++e) f(Row<T, NT>::value(y, e), row.first(v) + e);
     }
   }
 }
 
-template <typename T, int NT, typename F>
+template <int kAhead, typename T, int NT, typename F>
 __device__ __forceinline__ void each(const Row<T, NT>& row, F f) {
-  each_of(row, __builtin_amdgcn_readfirstlane(threadIdx.x / kWave), 0, row.per, f);
+  each_of<kAhead>(row, __builtin_amdgcn_readfirstlane(threadIdx.x / kWave), 0, row.per, f);
 }
 
-__device__ __forceinline__ bool stays(float z, int i, const Cut& c) { return z > c.z || (z == c.z && i <= c.i); }
-__device__ __forceinline__ bool ahead_of(float y, int j, float z, int i) { return y > z || (y == z && j < i); }
+// without branches: they run in loops over LDS
+__device__ __forceinline__ bool stays(float z, int i, const Cut& c) { return (z > c.z) | ((z == c.z) & (i <= c.i)); }
 
 // The last logit in the order (z falling, index rising) for which
 // before(count of those ahead, mass of those ahead) holds; it holds for the
 // first one and, once it fails, for none after.  Only logits that stay under
 // `cut` count.  By halving the value, then the index: for bins of more
 // logits than the list holds (many equal ones).
-template <typename T, int NT, typename F>
-__device__ __forceinline__ Cut bisect(const Row<T, NT>& row, float top, float c, Cut cut, F before, Shared<NT>& s) {
-  // ordered image of a float: larger value, larger key
-  auto key = [](float z) {
-    const unsigned b = __float_as_uint(z + 0.0f);  // -0 as 0
-    return b >> 31 ? ~b : b | 0x80000000u;
-  };
-  unsigned lo = key(-INFINITY), hi = key(top);  // hi holds at index 0
+template <typename T, int NT>
+__device__ __forceinline__ Cut bisect(const Row<T, NT>& row, float top, float c, Cut cut, Before before, Shared<NT>& s) {
+  unsigned lo = ordered(-INFINITY), hi = ordered(top);  // hi holds at index 0
   int a = 0, b = row.V - 1;                      // then the last index that holds
   while (lo < hi || a < b) {
     const bool values = lo < hi;
     const unsigned k = values ? lo + (hi - lo) / 2 : hi;
     const int i = values ? 0 : a + (b - a + 1) / 2;
     u64 mass = 0, cnt = 0;
-    each(row, [&](float z, int j) {
+    each<4>(row, [&](float z, int j) {
       if (!stays(z, j, cut)) return;
-      const unsigned kz = key(z);
+      const unsigned kz = ordered(z);
       if (kz > k || (kz == k && j < i)) {
         const unsigned w = weight(z, top, c);
         mass += w;
@@ -260,8 +277,7 @@ __device__ __forceinline__ Cut bisect(const Row<T, NT>& row, float top, float c,
     else if (holds) a = i;
     else b = i - 1;
   }
-  const unsigned bits = hi >> 31 ? hi & 0x7fffffffu : ~hi;
-  return {__uint_as_float(bits), a};
+  return {unordered(hi), a};
 }
 
 template <int NT>
@@ -272,11 +288,11 @@ __device__ __forceinline__ void clear_bins(Shared<NT>& s) {
 
 // Prefix over the bins: s.bin = the last bin that holds a mass and for whose
 // first logit `before` holds, s.cnt_before and s.mass_before what lies ahead
-// of it.
-template <int NT, typename F>
-__device__ __forceinline__ void find_bin(F before, Shared<NT>& s) {
+// of it in the bins; mb and cb lie ahead of all bins.
+template <int NT>
+__device__ __forceinline__ void find_bin(Before before, u64 mb, unsigned cb, Shared<NT>& s) {
   constexpr int kPer = kBins / NT;
-  const int tid = threadIdx.x, lane = tid % kWave, w = tid / kWave;
+  const int tid = threadIdx.x, lane = tid % kWave, w = __builtin_amdgcn_readfirstlane(tid / kWave);
   u64 mass = 0;
   unsigned cnt = 0;
 #pragma unroll
@@ -296,13 +312,8 @@ __device__ __forceinline__ void find_bin(F before, Shared<NT>& s) {
   __syncthreads();
   u64 m = im - mass;
   unsigned n = ic - cnt;
-#pragma unroll
-  for (int k = 0; k < NT / kWave; ++k) {
-    const u64 rm = s.red[k];
-    const unsigned rn = s.redc[k];
-    m += k < w ? rm : 0;
-    n += k < w ? rn : 0;
-  }
+#pragma unroll 1
+  for (int k = 0; k < w; ++k) m += s.red[k], n += s.redc[k];
   // each thread's last bin that holds; the largest of them is the answer
   int best = -1;
   u64 bm = 0;
@@ -310,7 +321,7 @@ __device__ __forceinline__ void find_bin(F before, Shared<NT>& s) {
 #pragma unroll
   for (int e = 0; e < kPer; ++e) {
     const u64 q = s.mass[tid * kPer + e];
-    if (q && before(n, m)) best = tid * kPer + e, bm = m, bn = n;
+    if (q && before(u64(n) + cb, m + mb)) best = tid * kPer + e, bm = m, bn = n;
     m += q;
     n += s.cnt[tid * kPer + e];
   }
@@ -320,68 +331,101 @@ __device__ __forceinline__ void find_bin(F before, Shared<NT>& s) {
   __syncthreads();
 }
 
-// The last of the m list places in s.sub (or, identity: of the first m) for
-// which `before` holds, counting those that stay under `old`; cb and mb lie
-// ahead of all.  *kept = the mass up to and with it.
-template <bool kIdentity, int NT, typename F>
-__device__ __forceinline__ Cut rank_cut(int m, u64 mb, unsigned cb, Cut old, F before, u64* kept, Shared<NT>& s) {
-  if (threadIdx.x == 0) s.sum = 0;
-  __syncthreads();
-  u64 mine = 0;
-  Cut cut = {0.0f, 0};
-  for (int a = threadIdx.x; a < m; a += NT) {
-    const Item x = s.list[kIdentity ? a : s.sub[a]];
-    if (!stays(x.z, x.i, old)) continue;
-    u64 mass = mb;
-    unsigned cnt = cb;
-#pragma unroll 4
-    for (int q = 0; q < m; ++q) {
-      const Item y = s.list[kIdentity ? q : s.sub[q]];
-      const bool first = ahead_of(y.z, y.i, x.z, x.i);
-      mass += first ? y.w : 0u;
-      cnt += first ? 1u : 0u;
+// f(item) for the m list places in s.sub (or, of `shares` shares of them, one),
+// eight in flight: one LDS latency a place would be most of the time.  A place
+// past the end has the smallest key and no mass.
+template <int NT, typename F>
+__device__ __forceinline__ void each_of_sub(int m, int share, int shares, const Shared<NT>& s, F f) {
+  for (int q = 8 * share; q < m; q += 8 * shares) {
+    const u32x4 at = *reinterpret_cast<const u32x4*>(&s.sub[q]);
+    Item y[8];
+#pragma unroll
+    for (int k = 0; k < 8; ++k) y[k] = s.list[q + k < m ? (k & 1 ? at[k / 2] >> 16 : at[k / 2] & 0xffffu) : 0u];
+    __builtin_amdgcn_sched_barrier(0);  // or each load is waited for by itself
+#pragma unroll
+    for (int k = 0; k < 8; ++k) {
+      if (q + k >= m) y[k].key = 0, y[k].w = 0;
+      f(y[k]);
     }
-    // masses rise along the order (no listed mass is 0): the largest that
-    // holds is the last one
-    if (before(cnt, mass) && mass + x.w > mine) mine = mass + x.w, cut = {x.z, x.i};
   }
-  if (mine) atomicMax(&s.sum, mine);
-  __syncthreads();
-  const u64 best = s.sum;
-  if (mine == best) s.cut = cut;
-  __syncthreads();
-  *kept = best;
-  cut = s.cut;
-  __syncthreads();
-  return cut;
 }
 
 // The cut for `before` among the n listed logits that stay under `old`; mb and
 // cb lie ahead of all, and all lie between (top - z) scale = 0 and kBins.
-template <int NT, typename F>
-__device__ __forceinline__ Cut cut_of_list(int n, float top, float scale, u64 mb, unsigned cb, Cut old, F before, u64* kept,
+// *kept = the mass up to and with it.
+template <int NT>
+__device__ __forceinline__ Cut cut_of_list(int n, float top, float scale, u64 mb, unsigned cb, Cut old, Before before, u64* kept,
                                            Shared<NT>& s) {
   const int tid = threadIdx.x;
-  if (n <= kFew) return rank_cut<true>(n, mb, cb, old, before, kept, s);
-  auto bin = [&](float z) { return z == top ? 0 : int(fmaxf(0.0f, fminf((top - z) * scale, float(kBins - 1)))); };
+  const u64 least = key_of(old.z, old.i);  // what stays has this key or a larger one
+  auto bin = [&](u64 key) {
+    const float z = value_of(key);
+    return z == top ? 0 : int(fmaxf(0.0f, fminf((top - z) * scale, float(kBins - 1))));
+  };
+  const bool few = n <= kFew;
   clear_bins(s);
+  if (!few) {
+    for (int a = tid; a < n; a += NT) {
+      const Item x = s.list[a];
+      if (x.key >= least) {
+        const int q = bin(x.key);
+        atomicAdd(&s.mass[q], u64(x.w));
+        atomicAdd(&s.cnt[q], 1u);
+      }
+    }
+    __syncthreads();
+    find_bin(before, mb, cb, s);
+    mb += s.mass_before;
+    cb += s.cnt_before;
+    __syncthreads();
+    clear_bins(s);
+  }
+  if (tid == 0) s.m = 0, s.sum = 0;
+  __syncthreads();
   for (int a = tid; a < n; a += NT) {
     const Item x = s.list[a];
-    if (stays(x.z, x.i, old)) {
-      const int q = bin(x.z);
-      atomicAdd(&s.mass[q], u64(x.w));
-      atomicAdd(&s.cnt[q], 1u);
+    if (x.key >= least && (few || bin(x.key) == s.bin)) s.sub[atomicAdd(&s.m, 1)] = a;
+  }
+  __syncthreads();
+  // every member against every other one; several threads a member where there
+  // are fewer of them, their shares added up in the bins
+  const int m = s.m;
+  int width = kWave;
+  while (width < m && width < NT) width *= 2;
+  const int share = width <= NT ? NT / width : 1;
+  u64 mine = 0, best_key = 0;
+  for (int a = tid % width; a < m; a += width) {
+    const Item x = s.list[s.sub[a]];
+    u64 mass = 0;
+    unsigned cnt = 0;
+    each_of_sub(m, tid / width, share, s, [&](const Item& y) {
+      mass += y.key > x.key ? y.w : 0u;
+      cnt += y.key > x.key;
+    });
+    if (share > 1) {  // m <= width < NT: one member a thread
+      atomicAdd(&s.mass[a], mass);
+      atomicAdd(&s.cnt[a], cnt);
+    } else if (before(cnt + cb, mass + mb) && mass + mb + x.w > mine) {
+      // masses rise along the order (no listed mass is 0): the largest that
+      // holds is the last one
+      mine = mass + mb + x.w, best_key = x.key;
     }
   }
-  if (tid == 0) s.m = 0;
   __syncthreads();
-  find_bin([&](u64 cnt, u64 mass) { return before(cnt + cb, mass + mb); }, s);
-  for (int a = tid; a < n; a += NT) {
-    const Item x = s.list[a];
-    if (stays(x.z, x.i, old) && bin(x.z) == s.bin) s.sub[atomicAdd(&s.m, 1)] = a;
+  if (share > 1 && tid < m) {
+    const Item x = s.list[s.sub[tid]];
+    const u64 mass = s.mass[tid] + mb;
+    if (before(u64(s.cnt[tid]) + cb, mass)) mine = mass + x.w, best_key = x.key;
   }
+  if (mine) atomicMax(&s.sum, mine);
   __syncthreads();
-  return rank_cut<false>(s.m, mb + s.mass_before, cb + s.cnt_before, old, before, kept, s);
+  const u64 best = s.sum;
+  if (mine == best) s.cut = {value_of(best_key), index_of(best_key)};
+  __syncthreads();
+  *kept = best;
+  const Cut cut = s.cut;
+  __syncthreads();
+  return cut;
 }
 
 // First place at which a running mass exceeds u times the whole.
@@ -397,27 +441,35 @@ __device__ __forceinline__ void draw_from_list(int n, float u, Cut cut, u64 leas
   const int tid = threadIdx.x, lane = tid % kWave, w = tid / kWave;
   const bool few = n <= kFew;
   const int shift = max(0, 32 - __builtin_clz(unsigned(V)) - (31 - __builtin_clz(unsigned(NT))));  // V >> shift < NT
+  const u64 last = key_of(cut.z, cut.i);
   if (!few) clear_bins(s);
   for (int a = tid; a < n; a += NT) {
     const Item x = s.list[a];
-    const bool on = stays(x.z, x.i, cut) && x.w >= least;
+    const bool on = x.key >= last && x.w >= least;
     if (!on) s.list[a].w = 0;
-    else if (!few) atomicAdd(&s.mass[x.i >> shift], u64(x.w));
+    else if (!few) atomicAdd(&s.mass[index_of(x.key) >> shift], u64(x.w));
   }
   if (tid == 0) s.m = 0;
   __syncthreads();
   if (few) {
     if (tid >= n) return;
     const Item x = s.list[tid];
+    const int i = index_of(x.key);
     u64 run = 0, total = 0;
-#pragma unroll 4
-    for (int q = 0; q < n; ++q) {
-      const Item y = s.list[q];
-      total += y.w;
-      run += y.i < x.i ? y.w : 0u;
+    for (int q = 0; q < n; q += 8) {
+      Item y[8];
+#pragma unroll
+      for (int k = 0; k < 8; ++k) y[k] = s.list[min(q + k, n - 1)];
+      __builtin_amdgcn_sched_barrier(0);
+#pragma unroll
+      for (int k = 0; k < 8; ++k) {
+        const unsigned w = q + k < n ? y[k].w : 0u;
+        total += w;
+        run += index_of(y[k].key) < i ? w : 0u;
+      }
     }
     const u64 goal = goal_of(u, total);
-    if (goal >= run && goal < run + x.w) *token = x.i;
+    if (goal >= run && goal < run + x.w) *token = i;
     return;
   }
   const u64 mine = s.mass[tid], inc = wave_scan64(mine);
@@ -436,19 +488,16 @@ __device__ __forceinline__ void draw_from_list(int n, float u, Cut cut, u64 leas
   const int bucket = s.bin;
   for (int a = tid; a < n; a += NT) {
     const Item x = s.list[a];
-    if (x.w && x.i >> shift == bucket) s.sub[atomicAdd(&s.m, 1)] = a;
+    if (x.w && index_of(x.key) >> shift == bucket) s.sub[atomicAdd(&s.m, 1)] = a;
   }
   __syncthreads();
   const int m = s.m;
   for (int a = tid; a < m; a += NT) {
     const Item x = s.list[s.sub[a]];
+    const int i = index_of(x.key);
     u64 run = s.mass_before;
-#pragma unroll 4
-    for (int q = 0; q < m; ++q) {
-      const Item y = s.list[s.sub[q]];
-      run += y.i < x.i ? y.w : 0u;
-    }
-    if (goal >= run && goal < run + x.w) *token = x.i;
+    each_of_sub(m, 0, 1, s, [&](const Item& y) { run += index_of(y.key) < i ? y.w : 0u; });
+    if (goal >= run && goal < run + x.w) *token = i;
   }
 }
 
@@ -472,7 +521,7 @@ __device__ __forceinline__ void draw_from_row(const Row<T, NT>& row, float u, u6
   const int step = (row.per + kWaves - 1) / kWaves;
   const int j0 = min(w * step, row.per), j1 = min(j0 + step, row.per);
   u64 sub = 0;
-  each_of(row, part, j0, j1, [&](float z, int i) { sub += mass_of(z, i); });
+  each_of<4>(row, part, j0, j1, [&](float z, int i) { sub += mass_of(z, i); });
   sub = wave_sum64(sub);
   if (lane == 0) s.red[w] = sub;
   __syncthreads();
@@ -523,16 +572,40 @@ struct Settings {
   }
 };
 
-struct ByCount {
-  int k;
-  __device__ __forceinline__ bool operator()(u64 cnt, u64) const { return cnt < u64(k); }
-};
-struct ByMass {
-  double want;
-  __device__ __forceinline__ bool operator()(u64 cnt, u64 mass) const { return mass == 0 || double(mass) < want; }
-};
-
-constexpr int kPending = -2;  // token of a row that is left for the second kernel
+// A row that LDS is too small for (seldom any): the cuts by halving, the draw
+// over the row.
+template <typename T, int NT>
+__device__ __forceinline__ void sample_rest(const Row<T, NT>& row, const Settings& o, float top, float u, int32_t* token,
+                                            Shared<NT>& s) {
+  const float c = o.c;
+  if (o.greedy) {
+    int best = row.V;
+    each<4>(row, [&](float z, int i) {
+      if (z == top) best = min(best, i);
+    });
+    if (best < row.V) atomicMin(&s.token, best);
+    __syncthreads();
+    if (threadIdx.x == 0) *token = s.token;
+    return;
+  }
+  Cut cut = {-INFINITY, row.V};
+#pragma unroll 1
+  for (int stage = 0; stage < 2; ++stage) {
+    if (stage == 0 ? !o.use_k : !o.use_p) continue;
+    u64 m = 0;
+    each<4>(row, [&](float z, int i) { m += stays(z, i, cut) ? weight(z, top, c) : 0u; });
+    m = block_sum(m, s);
+    cut = bisect(row, top, c, cut, Before{stage == 0, o.k, double(o.p) * double(m)}, s);
+  }
+  auto mass_of = [&](float z, int i) {
+    if (!stays(z, i, cut)) return u64(0);
+    const u64 w = weight(z, top, c);
+    return w >= o.thr ? w : u64(0);
+  };
+  u64 part = 0;
+  each<4>(row, [&](float z, int i) { part += mass_of(z, i); });
+  draw_from_row(row, u, wave_sum64(part), mass_of, token, s);
+}
 
 template <typename T, int NT>
 __global__ __launch_bounds__(NT, 4) void sample_kernel(SampleArgs a) {
@@ -551,7 +624,7 @@ __global__ __launch_bounds__(NT, 4) void sample_kernel(SampleArgs a) {
   const Settings o(a, b);
   const float u = a.u[r], c = o.c;
   float mine = -INFINITY;  // this thread's maximum
-  each(row, [&](float z, int) { mine = fmaxf(mine, z); });
+  each<8>(row, [&](float z, int) { mine = fmaxf(mine, z); });
   float top = mine;
   for (int d = 1; d < kWave; d <<= 1) top = fmaxf(top, __shfl_xor(top, d));
   if (lane == 0) s.redf[wave] = top;
@@ -563,16 +636,9 @@ __global__ __launch_bounds__(NT, 4) void sample_kernel(SampleArgs a) {
     if (tid == 0) a.token[r] = -1;
     return;
   }
-  // only the logits equal to top have a mass
-  const bool flat = o.greedy || top == INFINITY || c == INFINITY;
 
-  if (!flat && !o.use_k && !o.use_p && !o.use_m) {  // no cut
-    u64 part = 0;
-    each(row, [&](float z, int) { part += weight_near(z, top, c); });
-    draw_from_row(row, u, wave_sum64(part), [&](float z, int) { return u64(weight_near(z, top, c)); }, a.token + r, s);
-    return;
-  }
   // the floor, where there is one
+  const bool flat = o.greedy || top == INFINITY || c == INFINITY;  // only the logits equal to top have a mass
   float floor = -INFINITY;
   if (flat) {
     floor = top;
@@ -584,7 +650,7 @@ __global__ __launch_bounds__(NT, 4) void sample_kernel(SampleArgs a) {
       atomicAdd(&s.mass[q], u64(1));
     }
     __syncthreads();
-    find_bin(ByCount{o.k}, s);  // the bin of the k-th maximum
+    find_bin(Before{true, o.k, 0.0}, 0, 0, s);  // the bin of the k-th maximum
     const int bin = s.bin;
     const u64 n = u64(s.cnt_before) + s.cnt[bin];
     float low = mine > -INFINITY && bin_of(mine, top, c) <= bin ? mine : INFINITY;
@@ -595,16 +661,64 @@ __global__ __launch_bounds__(NT, 4) void sample_kernel(SampleArgs a) {
 #pragma unroll
     for (int w = 0; w < NT / kWave; ++w) low = fminf(low, s.redf[w]);
     if (n >= u64(o.k)) floor = low;  // else fewer than k threads have any logit
-  } else if (!o.use_k && !o.use_p) {
+  } else if (!o.use_k && !o.use_p && o.use_m) {
     const float down = (log2f(fminf(o.least, 1.0f)) - 0.01f) / c;
     floor = fmaxf(-3.4028235e38f, top + down - 1e-6f * (fabsf(top) + fabsf(down)));
   }
-  if (floor == -INFINITY) {
-    // masses by bins, the bin of the cut, what stays in vocabulary order
-    const bool count = o.use_k;
-    u64 total = 0;
-    auto masses = [&]() {
-      each(row, [&](float z, int) {  // without a branch: a mass of 0 changes nothing, NaN has the last bin
+  bool listed = floor > -INFINITY;
+
+  Cut cut = {-INFINITY, a.V};
+  // lists a logit (of that bin) that stays under the cut
+  auto list = [&](float z, int i, int bin) {
+    if ((bin >= 0 && bin_of(z, top, c) != bin) || !stays(z, i, cut)) return;
+    const unsigned w = weight(z, top, c);
+    if (w == 0) return;
+    const int at = atomicAdd(&s.n, 1);
+    if (at < kList) s.list[at] = {key_of(z, i), w, 0};
+  };
+  const unsigned thr = unsigned(o.thr);
+  u64 part = 0;  // mass of this thread's logits that stay
+  bool counted = false;
+  int n = 0;
+  u64 total = 0;
+  if (listed) {
+    if (mine >= floor)  // few threads have anything
+      each_if(row, [&](float z) { return z >= floor; }, [&](float z, int i) {
+        if (z >= floor) list(z, i, -1);
+      });
+    __syncthreads();
+    n = s.n;
+    if (n > kList) {
+      if (flat) {
+        sample_rest(row, o, top, u, a.token + r, s);
+        return;
+      }
+      listed = false;
+    }
+  }
+  if (listed) {
+    if (o.greedy) {
+      int best = a.V;
+      for (int q = tid; q < n; q += NT) best = min(best, index_of(s.list[q].key));
+      if (best < a.V) atomicMin(&s.token, best);
+      __syncthreads();
+      if (tid == 0) a.token[r] = s.token;
+      return;
+    }
+    u64 m = 0;
+    for (int q = tid; q < n; q += NT) m += s.list[q].w;
+    total = block_sum(m, s);
+  }
+#pragma unroll 1
+  for (int stage = 0; stage < 2; ++stage) {  // top_k, then top_p
+    if (stage == 0 ? !o.use_k || (listed && n <= o.k) : !o.use_p) continue;
+    float from = top, scale = c * kBinsPerOctave;
+    u64 mb = 0;
+    unsigned cb = 0;
+    if (!listed) {
+      clear_bins(s);
+      const bool count = stage == 0;
+      each<4>(row, [&](float z, int) {  // without a branch: a mass of 0 changes nothing, NaN has the last bin
         const float y = (z - top) * c;
         const unsigned w = unsigned(__builtin_fmaf(__builtin_amdgcn_exp2f(y), 2147483648.0f, 0.5f));
         const int q = int(fminf(y * -kBinsPerOctave, float(kBins - 1)));
@@ -612,151 +726,73 @@ __global__ __launch_bounds__(NT, 4) void sample_kernel(SampleArgs a) {
         if (count) atomicAdd(&s.cnt[q], w ? 1u : 0u);
       });
       __syncthreads();
-    };
-    clear_bins(s);
-    masses();
-    Cut cut = {-INFINITY, a.V};
-    bool full = false;
-    auto cut_row = [&](auto before, u64* kept) {
-      find_bin(before, s);
-      const int bin = s.bin;
-      // a little more than the bin (bounds that are not numbers, of a c near 0, leave nothing out)
-      const float step = 1.0f / (kBinsPerOctave * c), slack = 0.01f * step + 1e-6f * (fabsf(top) + float(bin + 1) * step);
-      const float low = bin < kBins - 1 ? top - float(bin + 1) * step - slack : -3.4028235e38f;
-      const float high = top - float(bin) * step + slack;
-      const u64 mb = s.mass_before;
-      const unsigned cb = s.cnt_before;
-      each_if(row, [&](float z) { return !(z < low) & !(z > high); }, [&](float z, int i) {
-        if (bin_of(z, top, c) != bin || !stays(z, i, cut)) return;
-        const unsigned w = weight_near(z, top, c);
-        if (w == 0) return;
-        const int at = atomicAdd(&s.n, 1);
-        if (at < kList) s.list[at] = {z, i, w, 0};
-      });
-      __syncthreads();
-      const int m = s.n;
-      __syncthreads();
       if (tid == 0) s.n = 0;
-      if (m > kList) {
-        full = true;
-        return;
+      if (!o.use_k) {
+        u64 m = 0;
+        for (int q = tid; q < kBins; q += NT) m += s.mass[q];
+        total = block_sum(m, s);
       }
-      // bins of the bin
-      const float from = fminf(high, top), scale = from > low ? float(kBins) / (from - low) : 0.0f;
-      cut = cut_of_list(m, from, scale, mb, cb, cut, before, kept, s);
-    };
-    if (o.use_k) {
-      cut_row(ByCount{o.k}, &total);
-    } else {
-      u64 m = 0;
-      for (int q = tid; q < kBins; q += NT) m += s.mass[q];
-      total = block_sum(m, s);
     }
     // bins past the top_k cut hold logits that are gone; none of them can
-    // hold the next cut, because the mass ahead of them is at least total
-    u64 kept;
-    if (o.use_p && !full) {
-      if (o.use_k) {  // the bins of the list took their place
-        clear_bins(s);
-        masses();
+    // hold the top_p cut, because the mass ahead of them is at least total
+    const Before before = {stage == 0, o.k, double(o.p) * double(total)};
+    if (!listed) {
+      find_bin(before, 0, 0, s);
+      const int bin = s.bin;
+      mb = s.mass_before;
+      cb = s.cnt_before;
+      // a little more than the bin (bounds that are not numbers, of a c near 0, leave nothing out)
+      const float step = 1.0f / scale, slack = 0.01f * step + 1e-6f * (fabsf(top) + float(bin + 1) * step);
+      const float low = bin < kBins - 1 ? top - float(bin + 1) * step - slack : -3.4028235e38f;
+      const float high = top - float(bin) * step + slack;
+      if (stage == 0 && o.use_p) {
+        each_if(row, [&](float z) { return !(z < low) & !(z > high); }, [&](float z, int i) { list(z, i, bin); });
+      } else {  // nothing more is cut: the masses of the bins ahead, in the same pass
+        counted = true;
+        each_if(row,
+                [&](float z) {
+                  const float y = (z - top) * c;
+                  const unsigned w = unsigned(__builtin_fmaf(__builtin_amdgcn_exp2f(y), 2147483648.0f, 0.5f));
+                  const int q = int(fminf(y * -kBinsPerOctave, float(kBins - 1)));
+                  part += (q < bin) & (w >= thr) ? w : 0u;
+                  return q == bin;
+                },
+                [&](float z, int i) { list(z, i, bin); });
       }
-      cut_row(ByMass{double(o.p) * double(total)}, &kept);
+      __syncthreads();
+      n = s.n;
+      if (n > kList) {
+        sample_rest(row, o, top, u, a.token + r, s);
+        return;
+      }
+      from = fminf(high, top);  // bins of the bin
+      scale = from > low ? float(kBins) / (from - low) : 0.0f;
     }
-    if (full) {
-      if (tid == 0) a.token[r] = kPending;
-      return;
-    }
-    const unsigned thr = unsigned(o.thr);
-    auto mass_of = [&](float z, int i) {
-      const unsigned w = weight_near(z, top, c);
-      return u64((z > cut.z) | ((z == cut.z) & (i <= cut.i)) && w >= thr ? w : 0u);
-    };
-    u64 part = 0;
-    each(row, [&](float z, int i) { part += mass_of(z, i); });
-    draw_from_row(row, u, wave_sum64(part), mass_of, a.token + r, s);
+    cut = cut_of_list(n, from, scale, mb, cb, cut, before, &total, s);
+  }
+  if (listed) {
+    draw_from_list(n, u, cut, o.thr, a.V, a.token + r, s);
     return;
   }
-
-  // list what is above it: few threads have anything
-  if (mine >= floor)
-    each_if(row, [&](float z) { return z >= floor; }, [&](float z, int i) {
-      const unsigned w = weight(z, top, c);
-      if (w == 0) return;
-      const int at = atomicAdd(&s.n, 1);
-      if (at < kList) s.list[at] = {z, i, w, 0};
-    });
-  __syncthreads();
-  const int n = s.n;
-  if (n > kList) {
-    if (tid == 0) a.token[r] = kPending;
-    return;
-  }
-  if (o.greedy) {
-    int best = a.V;
-    for (int q = tid; q < n; q += NT) best = min(best, s.list[q].i);
-    if (best < a.V) atomicMin(&s.token, best);
-    __syncthreads();
-    if (tid == 0) a.token[r] = s.token;
-    return;
-  }
-  u64 total = 0, kept;
-  const float scale = c * kBinsPerOctave;
-  Cut cut = {-INFINITY, a.V};
-  if (o.use_k && n > o.k) {
-    cut = cut_of_list(n, top, scale, 0, 0, cut, ByCount{o.k}, &total, s);
-  } else {
-    u64 m = 0;
-    for (int q = tid; q < n; q += NT) m += s.list[q].w;
-    total = block_sum(m, s);
-  }
-  if (o.use_p) cut = cut_of_list(n, top, scale, 0, 0, cut, ByMass{double(o.p) * double(total)}, &kept, s);
-  draw_from_list(n, u, cut, o.thr, a.V, a.token + r, s);
-}
-
-// The rows that LDS is too small for: the cuts by halving, the draw over the
-// row.  Seldom any.
-template <typename T, int NT>
-__global__ __launch_bounds__(NT, 4) void sample_rest_kernel(SampleArgs a) {
-  __shared__ Shared<NT> s;
-  const int r = blockIdx.x, b = r / a.T, tid = threadIdx.x;
-  if (a.token[r] != kPending) return;
-  __syncthreads();  // every thread has read the token
-  const Row<T, NT> row(reinterpret_cast<const T*>(a.logits) + (long long)(r) * a.ld, a.V);
-  const Settings o(a, b);
-  const float c = o.c;
-  float top = -INFINITY;
-  each(row, [&](float z, int) { top = fmaxf(top, z); });
-  for (int d = 1; d < kWave; d <<= 1) top = fmaxf(top, __shfl_xor(top, d));
-  if (tid % kWave == 0) s.redf[tid / kWave] = top;
-  if (tid == 0) s.token = a.V;
-  __syncthreads();
-  for (int w = 0; w < NT / kWave; ++w) top = fmaxf(top, s.redf[w]);
-  if (o.greedy) {
-    int best = a.V;
-    each(row, [&](float z, int i) {
-      if (z == top) best = min(best, i);
-    });
-    if (best < a.V) atomicMin(&s.token, best);
-    __syncthreads();
-    if (tid == 0) a.token[r] = s.token;
-    return;
-  }
-  Cut cut = {-INFINITY, a.V};
   auto mass_of = [&](float z, int i) {
-    if (!stays(z, i, cut)) return u64(0);
-    const u64 w = weight(z, top, c);
-    return w >= o.thr ? w : u64(0);
+    const unsigned w = weight_near(z, top, c);
+    return u64(stays(z, i, cut) & (w >= thr) ? w : 0u);
   };
-  auto mass = [&]() {
-    u64 m = 0;
-    each(row, [&](float z, int i) { m += stays(z, i, cut) ? weight(z, top, c) : 0u; });
-    return block_sum(m, s);
-  };
-  if (o.use_k) cut = bisect(row, top, c, cut, ByCount{o.k}, s);
-  if (o.use_p) cut = bisect(row, top, c, cut, ByMass{double(o.p) * double(mass())}, s);
-  u64 part = 0;
-  each(row, [&](float z, int i) { part += mass_of(z, i); });
-  draw_from_row(row, a.u[r], wave_sum64(part), mass_of, a.token + r, s);
+  if (!counted) {
+    each<4>(row, [&](float z, int i) { part += mass_of(z, i); });
+    part = wave_sum64(part);
+  } else {  // and what stays of the listed bin
+    part = wave_sum64(part);
+    clear_bins(s);
+    const u64 last = key_of(cut.z, cut.i);
+    for (int q = tid; q < n; q += NT) {
+      const Item x = s.list[q];
+      if (x.key >= last && x.w >= thr) atomicAdd(&s.mass[row.wave_of(index_of(x.key))], u64(x.w));
+    }
+    __syncthreads();
+    part += s.mass[wave];
+  }
+  draw_from_row(row, u, part, mass_of, a.token + r, s);
 }
 
 // ---------------------------------------------------------------------------
@@ -822,22 +858,18 @@ int after_launch(const char* who) {
 
 }  // namespace
 
-template <typename T, int NT>
-static int launch_rows(const SampleArgs& a, hipStream_t stream) {
-  sample_kernel<T, NT><<<a.B * a.T, NT, 0, stream>>>(a);
-  const int rc = after_launch("sample");
-  if (rc != GDN_OK || a.V <= Shared<NT>::kList) return rc;  // no row needs more than the list
-  sample_rest_kernel<T, 1024><<<a.B * a.T, 1024, 0, stream>>>(a);
-  return after_launch("sample");
-}
-
-// Threads for a row: up to 8 vectors each.
+// Threads for a row.  Between the passes over a row every wave takes part in
+// the same bookkeeping, so with many rows fewer waves a row are faster (4096
+// rows of 8000, top_k: 82 us with 256 threads, 142 and 282 with 512 and 1024),
+// with few rows more (one row of 131072, top_p: 117, 70, 59 us).  A short row
+// leaves many threads nothing to load.
 template <typename T>
 static int launch_type(const SampleArgs& a, hipStream_t stream) {
-  const int vectors = a.V / Pack<T>::kN;
-  if (vectors <= 8 * 256) return launch_rows<T, 256>(a, stream);
-  if (vectors <= 8 * 512) return launch_rows<T, 512>(a, stream);
-  return launch_rows<T, 1024>(a, stream);
+  const long long rows = (long long)(a.B) * a.T, vectors = a.V / Pack<T>::kN;
+  if (rows >= 2048 || vectors <= 2048) sample_kernel<T, 256><<<rows, 256, 0, stream>>>(a);
+  else if (rows > 256 || vectors <= 4096) sample_kernel<T, 512><<<rows, 512, 0, stream>>>(a);
+  else sample_kernel<T, 1024><<<rows, 1024, 0, stream>>>(a);
+  return after_launch("sample");
 }
 
 int launch_sample(const SampleArgs& a, hipStream_t stream) {
