@@ -120,18 +120,34 @@ __device__ __forceinline__ long long uniform(long long v) {
   return (long long)(unsigned(uniform(int(v)))) | (long long)(uniform(int(v >> 32))) << 32;
 }
 
-__device__ __forceinline__ long long wave_sum_ll(long long v) {
-  for (int s = 1; s < kWave; s <<= 1) v += __shfl_xor(v, s);
-  return uniform(v);
+// Inclusive prefix over the lanes, in DPP steps (the shuffles of a wider type
+// through LDS took a microsecond of the smallest calls).
+__device__ __forceinline__ unsigned wave_scan(unsigned v) {
+#define GDN_STEP(ctrl, rows) v += unsigned(__builtin_amdgcn_update_dpp(0, int(v), ctrl, rows, 0xF, false))
+  GDN_STEP(0x111, 0xF);  // row_shr by 1, 2, 4, 8
+  GDN_STEP(0x112, 0xF);
+  GDN_STEP(0x114, 0xF);
+  GDN_STEP(0x118, 0xF);
+  GDN_STEP(0x142, 0xA);  // row 0's last lane to row 1, row 2's to row 3
+  GDN_STEP(0x143, 0xC);  // lane 31 to rows 2 and 3
+#undef GDN_STEP
+  return v;
 }
 
-// Tiles of a run: all tiles over S, at least one.
-__device__ __forceinline__ long long run_length(const AttnArgs& a, int S, int kt, long long* total) {
-  long long n = 0;
-  for (int b = threadIdx.x % kWave; b < (a.B + kWave - 1) / kWave * kWave; b += kWave) n += tiles_of(a, b, kt);
-  n = wave_sum_ll(n);
-  *total = n;
-  return (n + S - 1) / S;
+// Tiles of 64 sequences stay below 2^32 (a page table's row spans at most 2^30
+// positions, a tile at least 32).
+struct Run {
+  long long total, length;  // tiles of all sequences, of a run
+};
+
+__device__ __forceinline__ Run run_length(const AttnArgs& a, int S, int kt) {
+  const int lane = threadIdx.x % kWave;
+  Run r = {0, 0};
+  for (int b0 = 0; b0 < a.B; b0 += kWave)
+    r.total += unsigned(__builtin_amdgcn_readlane(int(wave_scan(tiles_of(a, b0 + lane, kt))), kWave - 1));
+  r.length = uniform((r.total + S - 1) / S);
+  r.total = uniform(r.total);
+  return r;
 }
 
 // Sequence that holds global tile g, and the tile at which it begins.
@@ -140,19 +156,15 @@ __device__ __forceinline__ void find_tile(const AttnArgs& a, long long g, int kt
   long long run = 0;
   for (int b0 = 0; b0 < a.B; b0 += kWave) {
     const int n = tiles_of(a, b0 + lane, kt);
-    long long inc = n;
-    for (int d = 1; d < kWave; d <<= 1) {
-      const long long up = __shfl_up(inc, d);
-      if (lane >= d) inc += up;
-    }
+    const unsigned inc = wave_scan(n);
     const u64 past = __ballot(run + inc > g);
     if (past) {
       const int at = __builtin_ctzll(past);
       *b = b0 + at;
-      *start = uniform(run + __shfl(inc, at) - __shfl(n, at));
+      *start = uniform(run + unsigned(__builtin_amdgcn_readlane(int(inc), at)) - __builtin_amdgcn_readlane(n, at));
       return;
     }
-    run = uniform(run + __shfl(inc, kWave - 1));
+    run = uniform(run + unsigned(__builtin_amdgcn_readlane(int(inc), kWave - 1)));
   }
   *b = a.B;
   *start = run;
@@ -160,9 +172,13 @@ __device__ __forceinline__ void find_tile(const AttnArgs& a, long long g, int kt
 
 // First global tile of sequence b.
 __device__ __forceinline__ long long first_tile(const AttnArgs& a, int b, int kt) {
+  const int lane = threadIdx.x % kWave;
   long long n = 0;
-  for (int i = threadIdx.x % kWave; i < b; i += kWave) n += tiles_of(a, i, kt);
-  return wave_sum_ll(n);
+  for (int b0 = 0; b0 < b; b0 += kWave) {
+    const int i = b0 + lane;
+    n += unsigned(__builtin_amdgcn_readlane(int(wave_scan(i < b ? tiles_of(a, i, kt) : 0)), kWave - 1));
+  }
+  return uniform(n);
 }
 
 // Workspace of the parts: slot 2 u + 1 of run u for a part that begins inside
@@ -351,8 +367,8 @@ __global__ __launch_bounds__(kThreads, (stream_groups<T, D>())) void attend_stre
   const int tid = threadIdx.x, lane = tid % kWave, w = uniform(tid / kWave), n32 = lane & 31, h2 = lane >> 5;
   const int u = blockIdx.x, h = blockIdx.y, rt = blockIdx.z;
   const int M = a.T * (a.Hq / a.c.Hkv);
-  long long total;
-  const long long run = run_length(a, S, kStreamKeys, &total);
+  const Run all_runs = run_length(a, S, kStreamKeys);
+  const long long run = all_runs.length, total = all_runs.total;
   long long g = u * run;
   const long long end = g + run < total ? g + run : total;
   if (g >= end) return;
@@ -578,8 +594,8 @@ __global__ __launch_bounds__(kThreads, 2) void attend_tile_kernel(AttnArgs a, in
   const int x = blockIdx.x % 8, y = blockIdx.x / 8, rt = y % rts, uh = y / rts * 8 + x;
   const int u = uh / a.c.Hkv, h = uh % a.c.Hkv;
   if (u >= S) return;
-  long long total;
-  const long long run = run_length(a, S, KT, &total);
+  const Run all_runs = run_length(a, S, KT);
+  const long long run = all_runs.length, total = all_runs.total;
   long long g = u * run;
   const long long end = g + run < total ? g + run : total;
   if (g >= end) return;
@@ -757,8 +773,7 @@ __global__ __launch_bounds__(kThreads, 2) void attend_tile_kernel(AttnArgs a, in
 template <typename T>
 __global__ __launch_bounds__(kThreads) void attend_join_kernel(AttnArgs a, int S, int kt, Parts ws) {
   const int b = blockIdx.z, h = blockIdx.y, D = a.c.d, M = a.T * (a.Hq / a.c.Hkv);
-  long long total;
-  const long long run = run_length(a, S, kt, &total);
+  const long long run = run_length(a, S, kt).length;
   const long long t0 = first_tile(a, b, kt), t1 = t0 + tiles_of(a, b, kt) - 1;
   const int u0 = int(t0 / run), u1 = int(t1 / run);
   if (u0 == u1) return;
@@ -767,18 +782,33 @@ __global__ __launch_bounds__(kThreads) void attend_join_kernel(AttnArgs a, int S
   const MetaPtrs m = meta_ptrs(a.meta, a.B, a.T);
   const RowAt at = row_at(a, m, b, h, r, M, false);
   auto part = [&](int u) { return (size_t(2 * u + (u == u0 && t0 > u0 * run ? 1 : 0)) * a.c.Hkv + h) * M + r; };
-  float mx = -INFINITY;
-  for (int u = u0; u <= u1; ++u) mx = fmaxf(mx, ws.ml[part(u)].x);
-  float sum = 0.0f;
+  float mx = -INFINITY, sum = 0.0f;
   float4 o = make_float4(0, 0, 0, 0);
-  for (int u = u0; u <= u1; ++u) {
-    const size_t i = part(u);
-    const float2 ml = ws.ml[i];
-    if (ml.x == -INFINITY && ml.y == 0.0f) continue;
-    const float f = ml.x == -INFINITY ? 0.0f : __builtin_amdgcn_exp2f(ml.x - mx);
-    const float4 y = *reinterpret_cast<const float4*>(ws.o + i * D + d);
-    sum += f * ml.y;
-    o.x += f * y.x, o.y += f * y.y, o.z += f * y.z, o.w += f * y.w;
+  constexpr int kAhead = 8;  // parts in flight
+  for (int u = u0; u <= u1; u += kAhead) {
+    float2 ml[kAhead];
+    float4 y[kAhead];
+#pragma unroll
+    for (int k = 0; k < kAhead; ++k) {
+      const size_t i = part(min(u + k, u1));
+      ml[k] = ws.ml[i];
+      y[k] = *reinterpret_cast<const float4*>(ws.o + i * D + d);
+    }
+    float top = mx;
+#pragma unroll
+    for (int k = 0; k < kAhead; ++k) top = fmaxf(top, ml[k].x);
+    const float fix = mx == -INFINITY ? 0.0f : __builtin_amdgcn_exp2f(mx - top);
+    if (mx > -INFINITY) sum *= fix, o.x *= fix, o.y *= fix, o.z *= fix, o.w *= fix;
+    mx = top;
+#pragma unroll
+    for (int k = 0; k < kAhead; ++k) {
+      // a part without a visible key has nothing (one whose scores are not
+      // numbers has a sum that is none)
+      if (u + k > u1 || (ml[k].x == -INFINITY && ml[k].y == 0.0f)) continue;
+      const float f = ml[k].x == -INFINITY ? 0.0f : __builtin_amdgcn_exp2f(ml[k].x - mx);
+      sum += f * ml[k].y;
+      o.x += f * y[k].x, o.y += f * y[k].y, o.z += f * y[k].z, o.w += f * y[k].w;
+    }
   }
   const bool on = at.real && sum != 0.0f;
   const float inv = on ? 1.0f / sum : 0.0f;

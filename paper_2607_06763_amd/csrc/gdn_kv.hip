@@ -7,117 +7,176 @@ namespace gdn {
 namespace {
 
 constexpr int kThreads = 256;
-constexpr int kTok = 8;  // tokens per workgroup: one bf16 value pack
+constexpr int kTok = 8;    // tokens per workgroup: one bf16 value pack
+constexpr int kUnits = 4;  // units of a thread in flight
+
+// (x, y) of a pack of pairs to (x cos - y sin, y cos + x sin)
+template <typename T>
+__device__ __forceinline__ void turn(u32x4& x, u32x4& y, const float2* cs) {
+  constexpr int X = Pack<T>::kN;
+  u32x4 xo = {}, yo = {};
+#pragma unroll
+  for (int e = 0; e < X; ++e) {
+    const float2 r = cs[e];
+    if constexpr (X == 8) {
+      const float p = __uint_as_float(e & 1 ? x[e / 2] & 0xffff0000u : x[e / 2] << 16);
+      const float n = __uint_as_float(e & 1 ? y[e / 2] & 0xffff0000u : y[e / 2] << 16);
+      const unsigned a = __builtin_bit_cast(uint16_t, (__bf16)(p * r.x - n * r.y));
+      const unsigned b = __builtin_bit_cast(uint16_t, (__bf16)(n * r.x + p * r.y));
+      xo[e / 2] |= a << (e & 1 ? 16 : 0);
+      yo[e / 2] |= b << (e & 1 ? 16 : 0);
+    } else {
+      const float p = __uint_as_float(x[e]), n = __uint_as_float(y[e]);
+      xo[e] = __float_as_uint(p * r.x - n * r.y);
+      yo[e] = __float_as_uint(n * r.x + p * r.y);
+    }
+  }
+  x = xo;
+  y = yo;
+}
 
 // ---------------------------------------------------------------------------
 // Append.
 //
-// A workgroup holds the slots of one group of 8 positions (one value pack in
-// bf16, two in fp32) of a sequence, so that a value pack whose 8 tokens are
-// all new is written whole, and one of `parts` shares of their (head, pack)
-// units.  Bound by bytes.
+// Workgroups of queries hold a share of 8 slots' (head, pack) units; those of
+// keys and values hold a group of 8 positions (one value pack in bf16, two in
+// fp32), so that a value pack whose 8 tokens are all new is written whole.
+// Bound by bytes, and by the chain in front of them (length and depths, then
+// pages and angles): the queries, most of the bytes, are on their way before
+// it.  32 x 128 slots, 24 + 4 heads of 256, cold caches: 44 us for 120 MB (64
+// with every load behind the checks, 50 with ordinary loads; non-temporal
+// stores took 42, but the rows are read again by the attention).
 // ---------------------------------------------------------------------------
 template <typename T>
-__global__ __launch_bounds__(kThreads) void append_kernel(AttnArgs a, int parts) {
+__global__ __launch_bounds__(kThreads) void append_kernel(AttnArgs a, int qparts, int kparts) {
   constexpr int X = Pack<T>::kN;
   __shared__ float2 s_cs[kTok][128];  // cos and sin of the group's tokens
   __shared__ int s_page[kTok];        // page of the token, -1: absent
-  __shared__ int s_red[3];
-  const int b = blockIdx.z, tid = threadIdx.x, part = blockIdx.y;
-  const int ctx = a.ctx_len[b], span = span_of(a, b);
+  __shared__ int s_bad;
+  const int b = blockIdx.z, tid = threadIdx.x, h2 = a.rot / 2, d = a.c.d;
+  const bool isq = int(blockIdx.y) < qparts;
+  const int part = isq ? blockIdx.y : blockIdx.y - qparts, parts = isq ? qparts : kparts;
+  const int H = isq ? a.Hq : a.c.Hkv;
+  const size_t tok0 = size_t(b) * a.T;
+  const T* src = reinterpret_cast<const T*>(isq ? a.q : a.k);
+  // units of a head where the half of the rotated part is whole packs: pairs of
+  // packs (c, c + half), which one thread owns (q may be q_out), then the packs
+  // that are not rotated
+  const int half = h2 / X, np = d / X - half;
+  const bool packs = h2 % X == 0;
+  const int units = kTok * H * np;
+  u32x4 x0[kUnits], x1[kUnits];
+  // unit u as token, head and pack: queries along the packs, keys along the
+  // tokens (8 lanes write 128 bytes)
+  auto unit = [&](int u, int& t, int& h, int& c) {
+    if (isq) {
+      const int r = u / np;
+      c = u - r * np;
+      t = r / H;
+      h = r - t * H;
+    } else {
+      t = u % kTok;
+      h = u / kTok / np;
+      c = u / kTok - h * np;
+    }
+    c = c < half ? c : c + half;
+  };
+  auto fetch = [&](int first, int u0) {
+#pragma unroll
+    for (int n = 0; n < kUnits; ++n) {
+      const int u = u0 + n * kThreads;
+      int t, h, c;
+      unit(u, t, h, c);
+      const int i = first + t;
+      if (u >= units || i < 0 || i >= a.T) continue;
+      const T* p = src + ((tok0 + i) * H + h) * d + c * X;
+      x0[n] = __builtin_nontemporal_load(reinterpret_cast<const u32x4*>(p));  // read once
+      if (c < half) x1[n] = __builtin_nontemporal_load(reinterpret_cast<const u32x4*>(p + h2));
+    }
+  };
+  int u0 = part * kUnits * kThreads + tid;
+  if (packs && isq) fetch(blockIdx.x * kTok, u0);
+
   const MetaPtrs m = meta_ptrs(a.meta, a.B, a.T);
+  const int32_t* dep = m.depth + size_t(b) * a.T;
+  int own[GDN_MAX_T / kThreads];  // depths of slots tid, tid + kThreads
+#pragma unroll
+  for (int n = 0; n < GDN_MAX_T / kThreads; ++n) {
+    const int i = tid + n * kThreads;
+    own[n] = i < a.T ? (a.meta ? dep[i] : i) : -1;
+  }
+  const int ctx = a.ctx_len[b], span = span_of(a, b);
   int status = a.meta ? m.status[b] : 0;
   if (!status) status = len_status(a, ctx, span);
   const int32_t* row = a.page_table + size_t(b) * a.c.max_pages;
-
-  // deepest real slot and bad pages of the whole sequence: every workgroup
-  // takes the same decision
-  if (tid < 3) s_red[tid] = tid == 0 ? -1 : 0;
+  // the group's first slot; positions from a multiple of 8 on for the caches
+  // (may be < 0)
+  const int i0 = isq || status ? int(blockIdx.x) * kTok : ((ctx >> 3) + int(blockIdx.x)) * kTok - ctx;
+  if (i0 >= a.T || (!isq && status)) return;
+  if (tid < kTok) s_page[tid] = -1;
+  if (tid == 0) s_bad = 0;
   __syncthreads();
-  for (int i = tid; i < (status ? 0 : a.T); i += kThreads) {
-    const int dep = a.meta ? m.depth[size_t(b) * a.T + i] : (i < span ? i : -1);
-    if (dep >= 0) {
-      atomicMax(&s_red[0], dep);
-      if (page_of(a.c, row, ctx + i) < 0) s_red[1] = 1;
+  // every workgroup checks the whole sequence and takes the same decision
+  int bad = 0;
+#pragma unroll
+  for (int n = 0; n < GDN_MAX_T / kThreads; ++n) {
+    const int i = tid + n * kThreads;
+    if (!status && own[n] >= 0 && (a.meta || i < span)) {
+      const int pg = page_of(a.c, row, ctx + i);
+      if (a.rot && (long long)(ctx) + own[n] >= a.n_pos) bad |= 1;
+      if (pg < 0) bad |= 2;
+      if (i >= i0 && i < i0 + kTok) s_page[i - i0] = pg;
     }
   }
-  __syncthreads();
-  if (!status && s_red[0] >= 0) {
-    if (a.rot && (long long)(ctx) + s_red[0] >= a.n_pos) status = GDN_KV_BAD_POS;
-    else if (s_red[1]) status = GDN_KV_BAD_PAGE;
-  }
-  if (a.status && blockIdx.x == 0 && part == 0 && tid == 0) a.status[b] = status;
-
-  // slots of this group: positions g * 8 .. g * 8 + 7; a skipped sequence's
-  // groups start at slot 0 (its queries are cleared all the same)
-  const int base = status ? 0 : ctx;
-  const int i0 = ((base >> 3) + int(blockIdx.x)) * kTok - base;  // slot of the group's first position, may be < 0
-  if (i0 >= a.T) return;
-  if (tid < kTok) {
-    const int i = i0 + tid;
-    int pg = -1;
-    if (!status && i >= 0 && i < a.T) {
-      const bool real = a.meta ? m.depth[size_t(b) * a.T + i] >= 0 : i < span;
-      if (real) pg = page_of(a.c, row, ctx + i);
-    }
-    s_page[tid] = pg;
-  }
-  const int h2 = a.rot / 2;
   for (int u = tid; u < (status ? 0 : kTok * h2); u += kThreads) {
     const int t = u / h2, e = u % h2, i = i0 + t;
     if (i < 0 || i >= a.T) continue;
-    const int dep = a.meta ? m.depth[size_t(b) * a.T + i] : (i < span ? i : -1);
-    if (dep >= 0) s_cs[t][e] = reinterpret_cast<const float2*>(a.rope)[size_t(ctx + dep) * h2 + e];
+    const int at = a.meta ? dep[i] : (i < span ? i : -1);
+    if (at >= 0 && (long long)(ctx) + at < a.n_pos) s_cs[t][e] = reinterpret_cast<const float2*>(a.rope)[size_t(ctx + at) * h2 + e];
   }
+  if (bad) atomicOr(&s_bad, bad);
   __syncthreads();
+  bad = s_bad;
+  if (!status && bad) status = bad & 1 ? GDN_KV_BAD_POS : GDN_KV_BAD_PAGE;
+  if (isq && a.status && blockIdx.x == 0 && part == 0 && tid == 0) a.status[b] = status;
+  if (bad) {  // nothing is real
+    if (!isq) return;
+    __syncthreads();
+    if (tid < kTok) s_page[tid] = -1;
+    __syncthreads();
+  }
 
-  const int d = a.c.d, H = a.Hq + a.c.Hkv;
-  const size_t tok0 = size_t(b) * a.T;
-  // queries and keys.  Pairs of packs (c, c + h2 / X) where the half of the
-  // rotated part is whole packs; a thread owns both, so q may be q_out.
-  if (h2 % X == 0) {
-    const int hp = h2 / X, np = d / X - hp;  // paired packs, units of a head
-    for (int u = part * kThreads + tid; u < kTok * H * np; u += parts * kThreads) {
-      const int c = u % np, r = u / np, h = r % H, t = r / H, i = i0 + t;
-      if (i < 0 || i >= a.T) continue;
-      const int pg = s_page[t];
-      const bool isq = h < a.Hq;
-      if (!isq && pg < 0) continue;
-      const int kh = h - a.Hq;
-      const T* src = isq ? reinterpret_cast<const T*>(a.q) + ((tok0 + i) * a.Hq + h) * d
-                         : reinterpret_cast<const T*>(a.k) + ((tok0 + i) * a.c.Hkv + kh) * d;
-      T *dst, *kc = reinterpret_cast<T*>(a.k_cache);
-      size_t step;  // elements from one pack to the next
-      if (isq) {
-        dst = reinterpret_cast<T*>(a.out) + ((tok0 + i) * a.Hq + h) * d;
-        step = X;
-      } else {
-        const int pos = ctx + i;
-        dst = kc + block_of(a.c, pg, kh) + size_t(pos & ((1 << a.c.page_shift) - 1)) * X;
-        step = size_t(X) << a.c.page_shift;
-      }
-      const bool pair = c < hp;
-      const int c0 = pair ? c : c + hp;
-      __align__(16) T x0[X], x1[X];
-      if (pg < 0) {
-        const uint4 zero = make_uint4(0, 0, 0, 0);
-        *reinterpret_cast<uint4*>(dst + c0 * step) = zero;
-        if (pair) *reinterpret_cast<uint4*>(dst + (c0 + hp) * step) = zero;
-        continue;
-      }
-      copy16(x0, src + c0 * X);
-      if (pair) {
-        copy16(x1, src + (c0 + hp) * X);
+  const int mask = (1 << a.c.page_shift) - 1;
+  T *qo = reinterpret_cast<T*>(a.out), *kc = reinterpret_cast<T*>(a.k_cache), *vc = reinterpret_cast<T*>(a.v_cache);
+  const int p8 = (ctx + i0) & mask;  // keys, values: place of the group's first position in its page, which all 8 share
+  if (packs) {
+    for (; u0 - tid < units; u0 += parts * kUnits * kThreads) {
+      if (!isq || u0 >= parts * kUnits * kThreads) fetch(i0, u0);
 #pragma unroll
-        for (int e = 0; e < X; ++e) {
-          const float2 cs = s_cs[t][c0 * X + e];
-          const float p = to_f32(x0[e]), n = to_f32(x1[e]);
-          st(&x0[e], p * cs.x - n * cs.y);
-          st(&x1[e], n * cs.x + p * cs.y);
+      for (int n = 0; n < kUnits; ++n) {
+        const int u = u0 + n * kThreads;
+        int t, h, c;
+        unit(u, t, h, c);
+        const int i = i0 + t;
+        if (u >= units || i < 0 || i >= a.T) continue;
+        const int pg = s_page[t];
+        const bool pair = c < half;
+        T* dst;
+        size_t step = h2;  // from a pack to its partner
+        if (isq) {
+          dst = qo + ((tok0 + i) * H + h) * d + c * X;
+          if (pg < 0) x0[n] = x1[n] = u32x4{0, 0, 0, 0};
+        } else {
+          if (pg < 0) continue;
+          dst = kc + block_of(a.c, pg, h) + ((size_t(c) << a.c.page_shift) + p8 + t) * X;
+          step <<= a.c.page_shift;
         }
-        copy16(dst + (c0 + hp) * step, x1);
+        if (pair) {
+          if (pg >= 0) turn<T>(x0[n], x1[n], &s_cs[t][c * X]);
+          *reinterpret_cast<u32x4*>(dst + step) = x1[n];
+        }
+        *reinterpret_cast<u32x4*>(dst) = x0[n];
       }
-      copy16(dst + c0 * step, x0);
     }
   } else {
     // a half that ends inside a pack: one thread per head, pair by pair
@@ -125,50 +184,67 @@ __global__ __launch_bounds__(kThreads) void append_kernel(AttnArgs a, int parts)
       const int h = u % H, t = u / H, i = i0 + t;
       if (i < 0 || i >= a.T) continue;
       const int pg = s_page[t];
-      const bool isq = h < a.Hq;
       if (!isq && pg < 0) continue;
-      const int kh = h - a.Hq;
-      const T* src = isq ? reinterpret_cast<const T*>(a.q) + ((tok0 + i) * a.Hq + h) * d
-                         : reinterpret_cast<const T*>(a.k) + ((tok0 + i) * a.c.Hkv + kh) * d;
-      T* q = reinterpret_cast<T*>(a.out) + ((tok0 + i) * a.Hq + h) * d;
-      T* kc = reinterpret_cast<T*>(a.k_cache);
-      const int off = (ctx + i) & ((1 << a.c.page_shift) - 1);
+      const T* p = src + ((tok0 + i) * H + h) * d;
       for (int e = 0; e < d; ++e) {
         if (e >= h2 && e < 2 * h2) continue;
         const bool pair = e < h2;
-        const float p = to_f32(src[e]), n = pair ? to_f32(src[e + h2]) : 0.0f;
+        const float x = to_f32(p[e]), y = pair ? to_f32(p[e + h2]) : 0.0f;
         const float2 cs = pair && pg >= 0 ? s_cs[t][e] : make_float2(1.0f, 0.0f);
-        const float y0 = p * cs.x - n * cs.y, y1 = n * cs.x + p * cs.y;
-        for (int k = 0; k < (pair ? 2 : 1); ++k) {
-          const int at = e + k * h2;
-          T* dst = isq ? q + at : kc + block_of(a.c, pg, kh) + ((size_t(at / X) << a.c.page_shift) + off) * X + at % X;
-          st(dst, pg < 0 ? 0.0f : (k ? y1 : y0));
+        const float z[2] = {x * cs.x - y * cs.y, y * cs.x + x * cs.y};
+        for (int n = 0; n < (pair ? 2 : 1); ++n) {
+          const int at = e + n * h2;
+          T* dst = isq ? qo + ((tok0 + i) * H + h) * d + at
+                       : kc + block_of(a.c, pg, h) + ((size_t(at / X) << a.c.page_shift) + p8 + t) * X + at % X;
+          st(dst, pg < 0 ? 0.0f : z[n]);
         }
       }
     }
   }
-  // values: a thread holds one channel's tokens of a value pack
-  if (status) return;
-  const int per = kTok / X;
-  T* vc = reinterpret_cast<T*>(a.v_cache);
+  // Values: a unit is a pack of channels of X tokens, turned into a pack of
+  // tokens of X channels.
+  if (isq) return;
   const T* v = reinterpret_cast<const T*>(a.v);
-  for (int u = part * kThreads + tid; u < per * a.c.Hkv * d; u += parts * kThreads) {
-    const int e = u % d, r = u / d, h = r % a.c.Hkv, t0 = r / a.c.Hkv * X;
-    __align__(16) T x[X];
+  const int chunks = a.c.Hkv * (d / X);
+  for (int u = part * kThreads + tid; u < (kTok / X) * chunks; u += parts * kThreads) {
+    const int t0 = u / chunks * X, r = u % chunks, h = r / (d / X), e = r % (d / X) * X;
+    u32x4 x[X];
     bool whole = true;
 #pragma unroll
-    for (int k = 0; k < X; ++k) {
-      const int i = i0 + t0 + k;
-      whole = whole && s_page[t0 + k] >= 0;
-      if (s_page[t0 + k] >= 0) x[k] = v[((tok0 + i) * a.c.Hkv + h) * d + e];
+    for (int n = 0; n < X; ++n) {
+      whole = whole && s_page[t0 + n] >= 0;
+      if (s_page[t0 + n] >= 0)
+        x[n] = __builtin_nontemporal_load(reinterpret_cast<const u32x4*>(v + ((tok0 + i0 + t0 + n) * a.c.Hkv + h) * d + e));
     }
-    const int off = (ctx + i0 + t0) & ((1 << a.c.page_shift) - 1);
-    if (whole) {  // 8 positions of one group share their page
-      copy16(vc + block_of(a.c, s_page[t0], h) + (size_t(off / X) * d + e) * X, x);
+    const size_t at = (size_t((p8 + t0) / X) * d + e) * X;  // in the page's block
+    if (whole) {
+      T* dst = vc + block_of(a.c, s_page[t0], h) + at;
+#pragma unroll
+      for (int m = 0; m < X; ++m) {
+        u32x4 y;
+        if constexpr (X == 8) {
+#pragma unroll
+          for (int n = 0; n < 4; ++n) {  // tokens 2 n and 2 n + 1 of channel m
+            const unsigned lo = x[2 * n][m / 2], hi = x[2 * n + 1][m / 2];
+            y[n] = m & 1 ? (lo >> 16) | (hi & 0xffff0000u) : (lo & 0xffffu) | (hi << 16);
+          }
+        } else {
+#pragma unroll
+          for (int n = 0; n < 4; ++n) y[n] = x[n % X][m % 4];
+        }
+        *reinterpret_cast<u32x4*>(dst + m * X) = y;
+      }
     } else {
 #pragma unroll
-      for (int k = 0; k < X; ++k)
-        if (s_page[t0 + k] >= 0) vc[block_of(a.c, s_page[t0 + k], h) + (size_t(off / X) * d + e) * X + k] = x[k];
+      for (int n = 0; n < X; ++n) {
+        if (s_page[t0 + n] < 0) continue;
+        T* dst = vc + block_of(a.c, s_page[t0 + n], h) + at + n;
+#pragma unroll
+        for (int m = 0; m < X; ++m) {
+          if constexpr (X == 8) dst[m * X].bits = uint16_t(x[n][m / 2] >> (m & 1 ? 16 : 0));
+          else dst[m * X] = __uint_as_float(x[n][m % 4]);
+        }
+      }
     }
   }
 }
@@ -279,17 +355,14 @@ int after_launch(const char* who) {
 
 int launch_kv_append(const AttnArgs& a, hipStream_t stream) {
   const int groups = (a.T + kTok - 1) / kTok + 1;  // a group more where ctx is not a multiple of 8
-  // enough workgroups for the chip, each with a unit per thread at least
-  const int x = a.dtype == GDN_BF16 ? 8 : 4;
-  const long long units = (long long)(kTok) * (a.Hq + a.c.Hkv) * (a.c.d / x) / 2 + 1;
-  long long parts = (2048 + (long long)(groups) * a.B - 1) / ((long long)(groups) * a.B);
-  parts = parts < units / kThreads + 1 ? parts : units / kThreads + 1;
-  if (a.T == 1) parts = 1 + ((a.Hq + a.c.Hkv) * (a.c.d / x) / 2) / (4 * kThreads);
-  const dim3 grid(groups, unsigned(parts), a.B);
+  const int x = a.dtype == GDN_BF16 ? 8 : 4, np = a.c.d / x - a.rot / 2 / x;
+  const int qparts = (kTok * a.Hq * np + kUnits * kThreads - 1) / (kUnits * kThreads);
+  const int kparts = (kTok * a.c.Hkv * np + kUnits * kThreads - 1) / (kUnits * kThreads);
+  const dim3 grid(groups, qparts + kparts, a.B);
   if (a.dtype == GDN_BF16)
-    append_kernel<BF16><<<grid, kThreads, 0, stream>>>(a, int(parts));
+    append_kernel<BF16><<<grid, kThreads, 0, stream>>>(a, qparts, kparts);
   else
-    append_kernel<float><<<grid, kThreads, 0, stream>>>(a, int(parts));
+    append_kernel<float><<<grid, kThreads, 0, stream>>>(a, qparts, kparts);
   return after_launch("kv_append");
 }
 

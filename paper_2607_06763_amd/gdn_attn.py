@@ -25,6 +25,25 @@ class AttnDims(ctypes.Structure):
     _fields_ = [(n, ctypes.c_int32) for n in ("B", "T", "Hq", "Hkv", "d", "page", "n_pages", "max_pages", "dtype",
                                               "rot", "n_pos")] + [("scale", ctypes.c_float)]
 
+    def __setattr__(self, name, value):
+        super().__setattr__(name, value)
+        self.__dict__.pop("_shapes", None)
+
+    def shapes(self):
+        """dtype and the shapes of q, k, the caches, a page table, lengths, the rotation table and the metadata; made
+        once for these sizes (reading the fields takes longer than the call)."""
+        import torch
+        s = self.__dict__.get("_shapes")
+        if s is None:
+            B, T, d, page = self.B, self.T, self.d, self.page
+            bf16 = self.dtype == GDN_BF16
+            x = 8 if bf16 else 4
+            s = (torch.bfloat16 if bf16 else torch.float32, (B, T, self.Hq, d), (B, T, self.Hkv, d),
+                 (self.n_pages, self.Hkv, d // x, page, x), (self.n_pages, self.Hkv, page // x, d, x),
+                 (B, self.max_pages), (B,), (self.n_pos, self.rot // 2, 2) if self.rot else None, (meta_bytes(B, T),))
+            self.__dict__["_shapes"] = s
+        return s
+
     def __repr__(self):
         return "AttnDims(" + ", ".join(f"{n}={getattr(self, n)}" for n, _ in self._fields_) + ")"
 
@@ -38,15 +57,9 @@ def make_attn_dims(B, T, Hq, Hkv, d, page, n_pages, max_pages, dtype="bf16", rot
     return AttnDims(B, T, Hq, Hkv, d, page, n_pages, max_pages, dt, d if rot is None else rot, n_pos, float(scale))
 
 
-def _dtype(d: AttnDims):
-    import torch
-    return torch.bfloat16 if d.dtype == GDN_BF16 else torch.float32
-
-
 def cache_shapes(d: AttnDims):
     """Shapes of the key and the value cache."""
-    x = 8 if d.dtype == GDN_BF16 else 4
-    return ((d.n_pages, d.Hkv, d.d // x, d.page, x), (d.n_pages, d.Hkv, d.page // x, d.d, x))
+    return d.shapes()[3:5]
 
 
 def gather_rows(d: AttnDims, k_cache, v_cache, page_table, n: int):
@@ -60,39 +73,31 @@ def gather_rows(d: AttnDims, k_cache, v_cache, page_table, n: int):
     return k, v_cache[pg, :, off // x, :, off % x]
 
 
-def _tree(d, meta, n_new):
-    import torch
-    return ((meta, (meta_bytes(d.B, d.T),), torch.uint8, "meta", None), (n_new, (d.B,), torch.int32, "n_new", None))
-
-
 def kv_append(d: AttnDims, q, k, v, rope, ctx_len, page_table, k_cache, v_cache, q_out, kv_status=None, meta=None,
               n_new=None, stream=None) -> None:
     """gdn_kv_append: rotates q into q_out (which may be q) and k, and appends
     k and v to the paged caches; rope fp32 [n_pos][rot / 2][2] (None for rot 0)."""
     import torch
-    i32, dt = torch.int32, _dtype(d)
-    B, T = d.B, d.T
-    qs, ks = (B, T, d.Hq, d.d), (B, T, d.Hkv, d.d)
-    kc, vc = cache_shapes(d)
-    rs = (rope, (d.n_pos, d.rot // 2, 2), torch.float32, "rope")
+    i32 = torch.int32
+    dt, qs, ks, kc, vc, ts, ls, rs, ms = d.shapes()
     _check(lib().gdn_kv_append(ctypes.byref(d), *_ptrs((
-        *_tree(d, meta, n_new), (q, qs, dt, "q"), (k, ks, dt, "k"), (v, ks, dt, "v"),
-        rs if d.rot else (*rs, None), (ctx_len, (B,), i32, "ctx_len"),
-        (page_table, (B, d.max_pages), i32, "page_table"), (k_cache, kc, dt, "k_cache"), (v_cache, vc, dt, "v_cache"),
-        (q_out, qs, dt, "q_out"), (kv_status, (B,), i32, "kv_status", None))), _stream(stream)))
+        (meta, ms, torch.uint8, "meta", None), (n_new, ls, i32, "n_new", None), (q, qs, dt, "q"), (k, ks, dt, "k"),
+        (v, ks, dt, "v"), (rope, rs, torch.float32, "rope") if rs else (None, rs, None, "rope", None),
+        (ctx_len, ls, i32, "ctx_len"), (page_table, ts, i32, "page_table"), (k_cache, kc, dt, "k_cache"),
+        (v_cache, vc, dt, "v_cache"), (q_out, qs, dt, "q_out"), (kv_status, ls, i32, "kv_status", None))),
+        _stream(stream)))
 
 
 def attend(d: AttnDims, q, k_cache, v_cache, page_table, ctx_len, out, meta=None, n_new=None, stream=None) -> None:
     """gdn_tree_attend: attention of every slot over the cached tokens, its
     ancestors and itself; q as rotated by kv_append."""
     import torch
-    i32, dt = torch.int32, _dtype(d)
-    qs = (d.B, d.T, d.Hq, d.d)
-    kc, vc = cache_shapes(d)
+    i32 = torch.int32
+    dt, qs, _, kc, vc, ts, ls, _, ms = d.shapes()
     _check(lib().gdn_tree_attend(ctypes.byref(d), *_ptrs((
-        *_tree(d, meta, n_new), (q, qs, dt, "q"), (k_cache, kc, dt, "k_cache"), (v_cache, vc, dt, "v_cache"),
-        (page_table, (d.B, d.max_pages), i32, "page_table"), (ctx_len, (d.B,), i32, "ctx_len"),
-        (out, qs, dt, "out"))), _stream(stream)))
+        (meta, ms, torch.uint8, "meta", None), (n_new, ls, i32, "n_new", None), (q, qs, dt, "q"),
+        (k_cache, kc, dt, "k_cache"), (v_cache, vc, dt, "v_cache"), (page_table, ts, i32, "page_table"),
+        (ctx_len, ls, i32, "ctx_len"), (out, qs, dt, "out"))), _stream(stream)))
 
 
 def kv_commit(d: AttnDims, accepted, page_table, ctx_len, k_cache, v_cache, new_len, kv_status=None, meta=None,
@@ -100,13 +105,12 @@ def kv_commit(d: AttnDims, accepted, page_table, ctx_len, k_cache, v_cache, new_
     """gdn_kv_commit: moves the accepted path's rows to the front of the new
     rows of both caches, in place; new_len = ctx_len + depth + 1."""
     import torch
-    i32, dt = torch.int32, _dtype(d)
-    kc, vc = cache_shapes(d)
+    i32 = torch.int32
+    dt, _, _, kc, vc, ts, ls, _, ms = d.shapes()
     _check(lib().gdn_kv_commit(ctypes.byref(d), *_ptrs((
-        (meta, (meta_bytes(d.B, d.T),), torch.uint8, "meta", None), (accepted, (d.B,), i32, "accepted"),
-        (page_table, (d.B, d.max_pages), i32, "page_table"), (ctx_len, (d.B,), i32, "ctx_len"),
-        (k_cache, kc, dt, "k_cache"), (v_cache, vc, dt, "v_cache"), (new_len, (d.B,), i32, "new_len"),
-        (kv_status, (d.B,), i32, "kv_status", None))), _stream(stream)))
+        (meta, ms, torch.uint8, "meta", None), (accepted, ls, i32, "accepted"), (page_table, ts, i32, "page_table"),
+        (ctx_len, ls, i32, "ctx_len"), (k_cache, kc, dt, "k_cache"), (v_cache, vc, dt, "v_cache"),
+        (new_len, ls, i32, "new_len"), (kv_status, ls, i32, "kv_status", None))), _stream(stream)))
 
 
 def sample(logits, u, token, temperature=None, top_k=None, top_p=None, min_p=None, meta=None, stream=None) -> None:

@@ -146,6 +146,9 @@ def _ptrs(args):
             if not p & 15:
                 out.append(p)
                 continue
+        elif t is None and len(a) > 4:
+            out.append(None)
+            continue
         out.append(_reject(*a[:4], len(a) > 4))
     return out
 
