@@ -568,7 +568,7 @@ __global__ __launch_bounds__(kThreads, (stream_groups<T, D>())) void attend_stre
 template <int D>
 struct Tile {
   static constexpr int kKeys = D <= 128 ? 64 : 32;
-  static constexpr int kPacks = kKeys * D / 8;          // of either half
+  static constexpr int kPacks = kKeys * D / 8;          // of keys, and of values
   static constexpr int kPer = kPacks / kThreads;        // loads of a thread
   static constexpr size_t kLds = 2 * 2 * kPacks * 16 + 16;
 };
@@ -623,11 +623,11 @@ __global__ __launch_bounds__(kThreads, 2) void attend_tile_kernel(AttnArgs a, in
     st.clear();
     st.load_q(at.real ? reinterpret_cast<const BF16*>(a.q) + row_offset<BF16>(a, b, at) : nullptr, h2);
 
-    // page of the lane's key of a tile, -1: none
-    auto page_at = [&](int t) {
-      const int p = t * KT + lane % KT;
-      return t < t1 && p < len ? page_of(a.c, row, p) : -1;
-    };
+    // page-table entry of the lane's key of a tile.  Nothing looks at it before
+    // the next tile: a wait for it would be one for the tile's loads too.
+    const int last_entry = (len - 1) >> shift;
+    auto entry_at = [&](int t) { return row[min((t * KT + lane % KT) >> shift, last_entry)]; };
+    auto page_in = [&](int t, int entry) { return t * KT + lane % KT < len && unsigned(entry) < unsigned(a.c.n_pages) ? entry : -1; };
     auto stage = [&](int t, int id, int buf) {
       const int p0 = t * KT;
       uint4* sk = s_kv + buf * 2 * Tl::kPacks;
@@ -646,10 +646,14 @@ __global__ __launch_bounds__(kThreads, 2) void attend_tile_kernel(AttnArgs a, in
       }
     };
     const int stop = len < 0 ? t0 : t1;  // a skipped sequence has nothing to load
-    int id = page_at(t0), id1 = page_at(t0 + 1);
-    __syncthreads();  // the buffers are free
+    int id = -1, next = 0;  // page of the tile, entry of the next one's
+    __syncthreads();        // the buffers are free
     if (tid == 0) *s_from = INT_MAX;
-    if (t0 < stop) stage(t0, id, 0);
+    if (t0 < stop) {
+      id = page_in(t0, entry_at(t0));
+      next = entry_at(t0 + 1);
+      stage(t0, id, 0);
+    }
     const u64 all = KT == 64 ? ~u64(0) : 0xffffffffu;
     int t = t0;
     u64 valid = 0;
@@ -660,38 +664,67 @@ __global__ __launch_bounds__(kThreads, 2) void attend_tile_kernel(AttnArgs a, in
       __syncthreads();
       sk = s_kv + ((t - t0) & 1) * 2 * Tl::kPacks;
       sv = sk + Tl::kPacks;
-      if (t + 1 < stop) stage(t + 1, id1, (t + 1 - t0) & 1);
-      id = id1;
-      id1 = page_at(t + 2);
+      id = page_in(t + 1, next);
+      next = entry_at(t + 2);
+      if (t + 1 < stop) stage(t + 1, id, (t + 1 - t0) & 1);
     };
-    auto scores = [&](float (&s)[NB][16]) {
+    // Operands come from LDS four at a time, a group ahead of the products
+    // (left to itself the compiler waits for every operand).
+    constexpr int kGroup = 4, kGroups = Tl::kPacks / 64 / kGroup;  // 64 packs an operand
+    auto k_group = [&](Frag (&f)[kGroup], int n) {
 #pragma unroll
-      for (int nb = 0; nb < NB; ++nb) {
-        f32x16 acc = {};
-        const uint4* kr = sk + h2 * KT + nb * 32 + Mt::key_of(n32);
-#pragma unroll
-        for (int k = 0; k < D / 16; ++k) acc = Mt::mma(load16<Frag>(kr + 2 * k * KT), st.q[k], acc);
-#pragma unroll
-        for (int i = 0; i < 16; ++i) s[nb][i] = acc[i];
+      for (int k = 0; k < kGroup; ++k) {
+        const int j = n * kGroup + k, nb = j / (D / 16), c = j % (D / 16);
+        f[k] = load16<Frag>(sk + (2 * c + h2) * KT + nb * 32 + Mt::key_of(n32));
       }
     };
-    auto sums = [&](const float (&s)[NB][16]) {
+    auto v_group = [&](Frag (&f)[kGroup], int n) {
+#pragma unroll
+      for (int k = 0; k < kGroup; ++k) {
+        const int j = n * kGroup + k, q = j / (D / 32), c = j % (D / 32);
+        f[k] = load16<Frag>(sv + (2 * q + h2) * D + c * 32 + n32);
+      }
+    };
+    auto scores = [&](float (&s)[NB][16]) {
+      f32x16 acc[NB] = {};
+      Frag f[2][kGroup];
+      k_group(f[0], 0);
+#pragma unroll
+      for (int n = 0; n < kGroups; ++n) {
+        if (n + 1 < kGroups) k_group(f[(n + 1) & 1], n + 1);
+        __builtin_amdgcn_sched_barrier(0);
+#pragma unroll
+        for (int k = 0; k < kGroup; ++k) {
+          const int j = n * kGroup + k;
+          acc[j / (D / 16)] = Mt::mma(f[n & 1][k], st.q[j % (D / 16)], acc[j / (D / 16)]);
+        }
+        __builtin_amdgcn_sched_barrier(0);
+      }
 #pragma unroll
       for (int nb = 0; nb < NB; ++nb)
 #pragma unroll
-        for (int q = 0; q < 2; ++q) {
-          const Frag p = Mt::pack(&s[nb][q * 8]);
-          const uint4* vr = sv + (nb * 4 + q * 2 + h2) * D + n32;
+        for (int i = 0; i < 16; ++i) s[nb][i] = acc[nb][i];
+    };
+    auto sums = [&](const float (&s)[NB][16]) {
+      Frag f[2][kGroup];
+      v_group(f[0], 0);
 #pragma unroll
-          for (int k = 0; k < D / 32; ++k) st.o[k] = Mt::mma(load16<Frag>(vr + k * 32), p, st.o[k]);
+      for (int n = 0; n < kGroups; ++n) {
+        if (n + 1 < kGroups) v_group(f[(n + 1) & 1], n + 1);
+        __builtin_amdgcn_sched_barrier(0);
+#pragma unroll
+        for (int k = 0; k < kGroup; ++k) {
+          const int j = n * kGroup + k, q = j / (D / 32);
+          st.o[j % (D / 32)] = Mt::mma(f[n & 1][k], Mt::pack(&s[q / 2][q % 2 * 8]), st.o[j % (D / 32)]);
         }
+        __builtin_amdgcn_sched_barrier(0);
+      }
     };
     // keys that the tile holds (NB = 1: both halves of the wave hold the same)
     auto held = [&]() { return __ballot(id >= 0) & all; };
     // context: every row sees every key
-    for (; t < stop && (t + 1) * KT <= ctx; ++t) {
-      valid = held();
-      if (valid != all) break;
+    valid = held();
+    for (; t < stop && (t + 1) * KT <= ctx && valid == all; ++t, valid = held()) {
       enter();
       float s[NB][16];
       scores(s);
@@ -699,9 +732,8 @@ __global__ __launch_bounds__(kThreads, 2) void attend_tile_kernel(AttnArgs a, in
       sums(s);
     }
     // slots of the tree, the end of the cache and pages that are left out
-    for (; t < stop; ++t) {
+    for (; t < stop; ++t, valid = held()) {
       const int p0 = t * KT;
-      valid = held();
       enter();
       // values of absent keys, and those that are not finite, out of the
       // product: a masked weight is 0, and must stay so whatever it meets
