@@ -241,9 +241,10 @@ struct Rows {
     for (int k = 0; k < D / (2 * X); ++k) q[k] = row ? load16<Frag>(row + (2 * k + h) * X) : Frag{};
   }
 
-  // Scores of N tiles of 32 keys to weights; c = scale log2(e).
+  // The running maximum for N tiles of 32 scores (c = scale log2(e)); returns
+  // what a weight's exponent is counted from.
   template <int N>
-  __device__ __forceinline__ void softmax(float (&s)[N][16], float c) {
+  __device__ __forceinline__ float follow(const float (&s)[N][16], float c) {
     float mx = s[0][0];
 #pragma unroll
     for (int n = 0; n < N; ++n)
@@ -258,7 +259,13 @@ struct Rows {
       l *= fix;
       m = to;
     }
-    const float ref = m == -INFINITY ? 0.0f : m;  // nothing seen yet
+    return m == -INFINITY ? 0.0f : m;  // nothing seen yet
+  }
+
+  // Scores to weights.
+  template <int N>
+  __device__ __forceinline__ void softmax(float (&s)[N][16], float c) {
+    const float ref = follow<N>(s, c);
     float sum[2] = {0.0f, 0.0f};
 #pragma unroll
     for (int n = 0; n < N; ++n)
@@ -564,10 +571,16 @@ __global__ __launch_bounds__(kThreads, (stream_groups<T, D>())) void attend_stre
 // LDS, double-buffered and loaded past the registers.  The cache's packs are
 // the operand layout, so a tile is copied as it stands and read without bank
 // conflicts (32 lanes read 512 contiguous bytes).
+//
+// A wave issues in order, so the scores of the next tile are computed between
+// the exponentials of this one, a product and the work of 256 / d scores in
+// turn: the matrix units run while the others do.  Operands come from LDS a
+// group ahead of their products (left to itself the compiler waits for each).
+// Up to d = 128 two workgroups a CU; at 256 one, with the registers of both.
 // ---------------------------------------------------------------------------
 template <int D>
 struct Tile {
-  static constexpr int kKeys = D <= 128 ? 64 : 32;
+  static constexpr int kKeys = 64, kPerCu = D <= 128 ? 2 : 1;  // workgroups a CU
   static constexpr int kPacks = kKeys * D / 8;          // of keys, and of values
   static constexpr int kPer = kPacks / kThreads;        // loads of a thread
   static constexpr size_t kLds = 2 * 2 * kPacks * 16 + 16;
@@ -580,13 +593,13 @@ __device__ __forceinline__ void load_to_lds(const void* src, void* dst) {
 }
 
 template <int D>
-__global__ __launch_bounds__(kThreads, 2) void attend_tile_kernel(AttnArgs a, int S, int rts, Parts ws) {
+__global__ __launch_bounds__(kThreads, Tile<D>::kPerCu) void attend_tile_kernel(AttnArgs a, int S, int rts, Parts ws) {
   typedef Tile<D> Tl;
   typedef Mat<BF16> Mt;
   typedef Mt::Frag Frag;
   constexpr int KT = Tl::kKeys, NB = KT / 32;
   extern __shared__ __align__(16) char s_raw[];
-  uint4* s_kv = reinterpret_cast<uint4*>(s_raw);  // [buffer][K [D / 8][KT], V [KT / 8][D]]
+  uint4* s_kv = reinterpret_cast<uint4*>(s_raw);  // two of K [D / 8][KT], two of V [KT / 8][D]
   int* s_from = reinterpret_cast<int*>(s_kv + 4 * Tl::kPacks);  // first tile with values left out
   const int tid = threadIdx.x, lane = tid % kWave, w = uniform(tid / kWave), n32 = lane & 31, h2 = lane >> 5;
   const int M = a.T * (a.Hq / a.c.Hkv);
@@ -626,51 +639,28 @@ __global__ __launch_bounds__(kThreads, 2) void attend_tile_kernel(AttnArgs a, in
     // page-table entry of the lane's key of a tile.  Nothing looks at it before
     // the next tile: a wait for it would be one for the tile's loads too.
     const int last_entry = (len - 1) >> shift;
-    auto entry_at = [&](int t) { return row[min((t * KT + lane % KT) >> shift, last_entry)]; };
-    auto page_in = [&](int t, int entry) { return t * KT + lane % KT < len && unsigned(entry) < unsigned(a.c.n_pages) ? entry : -1; };
-    auto stage = [&](int t, int id, int buf) {
-      const int p0 = t * KT;
-      uint4* sk = s_kv + buf * 2 * Tl::kPacks;
-      const BF16* kl = kc + block_of(a.c, id < 0 ? 0 : id, h) + size_t((p0 + lane % KT) & mask) * 8;
+    auto entry_at = [&](int t) { return row[min((t * KT + lane) >> shift, last_entry)]; };
+    auto page_in = [&](int t, int entry) { return t * KT + lane < len && unsigned(entry) < unsigned(a.c.n_pages) ? entry : -1; };
+    auto stage_k = [&](int t, int id, int buf) {
+      const BF16* kl = kc + block_of(a.c, id < 0 ? 0 : id, h) + size_t((t * KT + lane) & mask) * 8;
 #pragma unroll
       for (int n = 0; n < Tl::kPer; ++n) {
-        const int at0 = (n * kWaves + w) * kWave;  // packs at0 + lane
-        load_to_lds(kl + (size_t(at0 / KT + lane / KT) << shift) * 8, sk + at0);
+        const int at0 = (n * kWaves + w) * kWave;  // packs at0 + lane: one key a lane
+        load_to_lds(kl + (size_t(at0 / KT) << shift) * 8, s_kv + buf * Tl::kPacks + at0);
       }
+    };
+    auto stage_v = [&](int t, int id, int buf) {
 #pragma unroll
       for (int n = 0; n < Tl::kPer; ++n) {
         const int at0 = (n * kWaves + w) * kWave, q = at0 + lane, grp = q / D;
         const int vid = __shfl(id, grp * 8);
-        load_to_lds(vc + block_of(a.c, vid < 0 ? 0 : vid, h) + (size_t((p0 + grp * 8) & mask) / 8 * D + q % D) * 8,
-                    sk + Tl::kPacks + at0);
+        load_to_lds(vc + block_of(a.c, vid < 0 ? 0 : vid, h) + (size_t((t * KT + grp * 8) & mask) / 8 * D + q % D) * 8,
+                    s_kv + (2 + buf) * Tl::kPacks + at0);
       }
     };
-    const int stop = len < 0 ? t0 : t1;  // a skipped sequence has nothing to load
-    int id = -1, next = 0;  // page of the tile, entry of the next one's
-    __syncthreads();        // the buffers are free
-    if (tid == 0) *s_from = INT_MAX;
-    if (t0 < stop) {
-      id = page_in(t0, entry_at(t0));
-      next = entry_at(t0 + 1);
-      stage(t0, id, 0);
-    }
-    const u64 all = KT == 64 ? ~u64(0) : 0xffffffffu;
-    int t = t0;
-    u64 valid = 0;
-    uint4 *sk = nullptr, *sv = nullptr;
-    // waits for tile t and starts the next one
-    auto enter = [&]() {
-      asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
-      __syncthreads();
-      sk = s_kv + ((t - t0) & 1) * 2 * Tl::kPacks;
-      sv = sk + Tl::kPacks;
-      id = page_in(t + 1, next);
-      next = entry_at(t + 2);
-      if (t + 1 < stop) stage(t + 1, id, (t + 1 - t0) & 1);
-    };
-    // Operands come from LDS four at a time, a group ahead of the products
-    // (left to itself the compiler waits for every operand).
-    constexpr int kGroup = 4, kGroups = Tl::kPacks / 64 / kGroup;  // 64 packs an operand
+    // operands in groups: 64 packs each, the keys of a tile, then its values
+    constexpr int kGroup = 4, kOps = Tl::kPacks / 64, kGroups = kOps / kGroup;
+    const uint4 *sk, *sv;
     auto k_group = [&](Frag (&f)[kGroup], int n) {
 #pragma unroll
       for (int k = 0; k < kGroup; ++k) {
@@ -685,18 +675,110 @@ __global__ __launch_bounds__(kThreads, 2) void attend_tile_kernel(AttnArgs a, in
         f[k] = load16<Frag>(sv + (2 * q + h2) * D + c * 32 + n32);
       }
     };
-    auto scores = [&](float (&s)[NB][16]) {
+    auto score = [&](f32x16 (&acc)[NB], Frag f, int j) { acc[j / (D / 16)] = Mt::mma(f, st.q[j % (D / 16)], acc[j / (D / 16)]); };
+
+    const int stop = len < 0 ? t0 : t1;  // a skipped sequence has nothing to load
+    int id = -1, id1 = -1, next = 0;     // pages of this tile and the next, entry of the one after
+    Frag f[2][kGroup];
+    float s[NB][16];
+    __syncthreads();  // the buffers are free
+    if (tid == 0) *s_from = INT_MAX;
+    if (t0 < stop) {
+      id = page_in(t0, entry_at(t0));
+      id1 = page_in(t0 + 1, entry_at(t0 + 1));
+      next = entry_at(t0 + 2);
+      stage_k(t0, id, 0);
+      asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
+      __syncthreads();
+      stage_v(t0, id, 0);
+      if (t0 + 1 < stop) stage_k(t0 + 1, id1, 1);
+      sk = s_kv;
       f32x16 acc[NB] = {};
-      Frag f[2][kGroup];
-      k_group(f[0], 0);
 #pragma unroll
       for (int n = 0; n < kGroups; ++n) {
-        if (n + 1 < kGroups) k_group(f[(n + 1) & 1], n + 1);
+        k_group(f[0], n);
+#pragma unroll
+        for (int k = 0; k < kGroup; ++k) score(acc, f[0][k], n * kGroup + k);
+      }
+#pragma unroll
+      for (int nb = 0; nb < NB; ++nb)
+#pragma unroll
+        for (int i = 0; i < 16; ++i) s[nb][i] = acc[nb][i];
+    }
+    for (int t = t0; t < stop; ++t) {
+      const int p0 = t * KT, r = (t - t0) & 1;
+      // the keys of the next tile and the values of this one are there, the
+      // buffers of their predecessors are free
+      const u64 valid = __ballot(id >= 0);
+      asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
+      __syncthreads();
+      id = id1;
+      id1 = page_in(t + 2, next);
+      next = entry_at(t + 3);
+      if (t + 2 < stop) stage_k(t + 2, id1, r);
+      if (t + 1 < stop) stage_v(t + 1, id, r ^ 1);
+      sk = s_kv + (r ^ 1) * Tl::kPacks;
+      sv = s_kv + (2 + r) * Tl::kPacks;
+      if (p0 + KT > ctx || valid != ~u64(0)) {
+        // slots of the tree, the end of the cache, pages that are left out:
+        // values of absent keys, and those that are not finite, leave the
+        // product (a masked weight is 0, and must stay so whatever it meets)
+        bool mine = false;
+        for (int q = tid; q < Tl::kPacks; q += kThreads) {
+          const unsigned ok = unsigned(valid >> (q / D * 8)) & 0xffu;
+          Frag y = load16<Frag>(sv + q);
+          bool change = false;
+#pragma unroll
+          for (int e = 0; e < 8; ++e) {
+            const bool on = (ok >> e) & 1;
+            if (!on || (Mt::bits(y, e) & kExp) == kExp) {
+              mine = mine || on;
+              change = true;
+              y = Mt::without(y, e);
+            }
+          }
+          if (change) *reinterpret_cast<Frag*>(const_cast<uint4*>(sv + q)) = y;
+        }
+        if (mine) atomicMin(s_from, p0);
+        __syncthreads();
+        const u64 seen = seen_bits(a, m, b, at.slot, ctx, p0) & valid;
+#pragma unroll
+        for (int nb = 0; nb < NB; ++nb)
+#pragma unroll
+          for (int i = 0; i < 16; ++i) s[nb][i] = where_seen(s[nb][i], unsigned(seen >> (nb * 32)) >> (h2 * 8), i / 8 * 16 + i % 8);
+      }
+      k_group(f[0], 0);
+      const float ref = st.template follow<NB>(s, c);
+      f32x16 acc[NB] = {};  // scores of the next tile (of nothing, after the last)
+      Frag p[NB * 2];
+      float sum[2] = {0.0f, 0.0f};
+#pragma unroll
+      for (int j = 0; j < kOps; ++j) {
+        if (j % kGroup == 0) {
+          if (j / kGroup + 1 < kGroups) k_group(f[(j / kGroup + 1) & 1], j / kGroup + 1);
+          else v_group(f[kGroups & 1], 0);
+        }
+        score(acc, f[j / kGroup & 1][j % kGroup], j);
+        constexpr int kEach = NB * 16 / kOps;
+#pragma unroll
+        for (int e = 0; e < kEach; ++e) {
+          const int x = j * kEach + e;
+          float& y = s[x / 16][x % 16];
+          y = __builtin_amdgcn_exp2f(__builtin_fmaf(y, c, -ref));
+          sum[x & 1] += y;
+          if (x % 8 == 7) p[x / 8] = Mt::pack(&s[x / 16][x % 16 - 7]);
+        }
+        __builtin_amdgcn_sched_barrier(0);
+      }
+      st.l += sum[0] + sum[1];
+#pragma unroll
+      for (int n = 0; n < kGroups; ++n) {
+        if (n + 1 < kGroups) v_group(f[(kGroups + n + 1) & 1], n + 1);
         __builtin_amdgcn_sched_barrier(0);
 #pragma unroll
         for (int k = 0; k < kGroup; ++k) {
           const int j = n * kGroup + k;
-          acc[j / (D / 16)] = Mt::mma(f[n & 1][k], st.q[j % (D / 16)], acc[j / (D / 16)]);
+          st.o[j % (D / 32)] = Mt::mma(f[(kGroups + n) & 1][k], p[j / (D / 32)], st.o[j % (D / 32)]);
         }
         __builtin_amdgcn_sched_barrier(0);
       }
@@ -704,66 +786,6 @@ __global__ __launch_bounds__(kThreads, 2) void attend_tile_kernel(AttnArgs a, in
       for (int nb = 0; nb < NB; ++nb)
 #pragma unroll
         for (int i = 0; i < 16; ++i) s[nb][i] = acc[nb][i];
-    };
-    auto sums = [&](const float (&s)[NB][16]) {
-      Frag f[2][kGroup];
-      v_group(f[0], 0);
-#pragma unroll
-      for (int n = 0; n < kGroups; ++n) {
-        if (n + 1 < kGroups) v_group(f[(n + 1) & 1], n + 1);
-        __builtin_amdgcn_sched_barrier(0);
-#pragma unroll
-        for (int k = 0; k < kGroup; ++k) {
-          const int j = n * kGroup + k, q = j / (D / 32);
-          st.o[j % (D / 32)] = Mt::mma(f[n & 1][k], Mt::pack(&s[q / 2][q % 2 * 8]), st.o[j % (D / 32)]);
-        }
-        __builtin_amdgcn_sched_barrier(0);
-      }
-    };
-    // keys that the tile holds (NB = 1: both halves of the wave hold the same)
-    auto held = [&]() { return __ballot(id >= 0) & all; };
-    // context: every row sees every key
-    valid = held();
-    for (; t < stop && (t + 1) * KT <= ctx && valid == all; ++t, valid = held()) {
-      enter();
-      float s[NB][16];
-      scores(s);
-      st.template softmax<NB>(s, c);
-      sums(s);
-    }
-    // slots of the tree, the end of the cache and pages that are left out
-    for (; t < stop; ++t, valid = held()) {
-      const int p0 = t * KT;
-      enter();
-      // values of absent keys, and those that are not finite, out of the
-      // product: a masked weight is 0, and must stay so whatever it meets
-      bool mine = false;
-      for (int q = tid; q < Tl::kPacks; q += kThreads) {
-        const unsigned ok = unsigned(valid >> (q / D * 8)) & 0xffu;
-        Frag f = load16<Frag>(sv + q);
-        bool change = false;
-#pragma unroll
-        for (int e = 0; e < 8; ++e) {
-          const bool on = (ok >> e) & 1;
-          if (!on || (Mt::bits(f, e) & kExp) == kExp) {
-            mine = mine || on;
-            change = true;
-            f = Mt::without(f, e);
-          }
-        }
-        if (change) *reinterpret_cast<Frag*>(sv + q) = f;
-      }
-      if (mine) atomicMin(s_from, p0);
-      __syncthreads();
-      float s[NB][16];
-      scores(s);
-      const u64 seen = seen_bits(a, m, b, at.slot, ctx, p0) & valid;
-#pragma unroll
-      for (int nb = 0; nb < NB; ++nb)
-#pragma unroll
-        for (int i = 0; i < 16; ++i) s[nb][i] = where_seen(s[nb][i], unsigned(seen >> (nb * 32)) >> (h2 * 8), i / 8 * 16 + i % 8);
-      st.template softmax<NB>(s, c);
-      sums(s);
     }
 
     __syncthreads();
@@ -905,7 +927,7 @@ int launch_stream(const AttnArgs& a, hipStream_t stream) {
 template <int D>
 int launch_tile(const AttnArgs& a, hipStream_t stream) {
   const int M = a.T * (a.Hq / a.c.Hkv), rt = (M + kTileRows - 1) / kTileRows;
-  const int S = runs_for((long long)(a.c.Hkv) * rt, 512);
+  const int S = runs_for((long long)(a.c.Hkv) * rt, 256 * Tile<D>::kPerCu);
   Parts ws;
   int rc = parts_for(a, S, stream, &ws);
   if (rc != GDN_OK) return rc;
