@@ -619,6 +619,8 @@ __global__ __launch_bounds__(kThreads, Tile<D>::kPerCu) void attend_tile_kernel(
   const MetaPtrs m = meta_ptrs(a.meta, a.B, a.T);
   const BF16 *kc = reinterpret_cast<const BF16*>(a.k_cache), *vc = reinterpret_cast<const BF16*>(a.v_cache);
   const int shift = a.c.page_shift, mask = (1 << shift) - 1;
+  const size_t page_size = block_of(a.c, 1, 0);
+  const BF16 *kh = kc + block_of(a.c, 0, h), *vh = vc + block_of(a.c, 0, h);
   const float c = a.scale * kLog2e;
   for (; g < end; ++b) {
     const int tiles = uniform(tiles_of(a, b, KT));
@@ -642,7 +644,7 @@ __global__ __launch_bounds__(kThreads, Tile<D>::kPerCu) void attend_tile_kernel(
     auto entry_at = [&](int t) { return row[min((t * KT + lane) >> shift, last_entry)]; };
     auto page_in = [&](int t, int entry) { return t * KT + lane < len && unsigned(entry) < unsigned(a.c.n_pages) ? entry : -1; };
     auto stage_k = [&](int t, int id, int buf) {
-      const BF16* kl = kc + block_of(a.c, id < 0 ? 0 : id, h) + size_t((t * KT + lane) & mask) * 8;
+      const BF16* kl = kh + size_t(id < 0 ? 0 : id) * page_size + size_t((t * KT + lane) & mask) * 8;
 #pragma unroll
       for (int n = 0; n < Tl::kPer; ++n) {
         const int at0 = (n * kWaves + w) * kWave;  // packs at0 + lane: one key a lane
@@ -652,10 +654,10 @@ __global__ __launch_bounds__(kThreads, Tile<D>::kPerCu) void attend_tile_kernel(
     auto stage_v = [&](int t, int id, int buf) {
 #pragma unroll
       for (int n = 0; n < Tl::kPer; ++n) {
-        const int at0 = (n * kWaves + w) * kWave, q = at0 + lane, grp = q / D;
-        const int vid = __shfl(id, grp * 8);
-        load_to_lds(vc + block_of(a.c, vid < 0 ? 0 : vid, h) + (size_t((t * KT + grp * 8) & mask) / 8 * D + q % D) * 8,
-                    s_kv + (2 + buf) * Tl::kPacks + at0);
+        const int at0 = (n * kWaves + w) * kWave, grp = at0 / D;  // packs at0 + lane: of one page
+        const int vid = __builtin_amdgcn_readlane(id, grp * 8);
+        const BF16* vl = vh + size_t(vid < 0 ? 0 : vid) * page_size + size_t((t * KT + grp * 8) & mask) * D + at0 % D * 8;
+        load_to_lds(vl + lane * 8, s_kv + (2 + buf) * Tl::kPacks + at0);
       }
     };
     // operands in groups: 64 packs each, the keys of a tile, then its values
