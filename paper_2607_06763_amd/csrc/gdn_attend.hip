@@ -749,6 +749,7 @@ __global__ __launch_bounds__(kThreads, Tile<D>::kPerCu) void attend_tile_kernel(
 #pragma unroll
           for (int i = 0; i < 16; ++i) s[nb][i] = where_seen(s[nb][i], unsigned(seen >> (nb * 32)) >> (h2 * 8), i / 8 * 16 + i % 8);
       }
+      __builtin_amdgcn_s_setprio(1);  // before the waves in their products alone
       k_group(f[0], 0);
       const float ref = st.template follow<NB>(s, c);
       f32x16 acc[NB] = {};  // scores of the next tile (of nothing, after the last)
@@ -772,6 +773,7 @@ __global__ __launch_bounds__(kThreads, Tile<D>::kPerCu) void attend_tile_kernel(
         }
         __builtin_amdgcn_sched_barrier(0);
       }
+      __builtin_amdgcn_s_setprio(0);
       st.l += sum[0] + sum[1];
 #pragma unroll
       for (int n = 0; n < kGroups; ++n) {
