@@ -281,7 +281,8 @@ int gdn_tree_step(const gdn_dims* dims, const void* prev_meta, const int32_t* pr
 typedef struct {
   int32_t B, T;      /* sequences, slots per tree (<= GDN_MAX_T)                 */
   int32_t Hq, Hkv;   /* query heads, key / value heads; Hq % Hkv == 0, query
-                      * head h reads key / value head floor(h Hkv / Hq)          */
+                      * head h reads key / value head floor(h Hkv / Hq);
+                      * T Hq / Hkv <= GDN_MAX_KV_ROWS                            */
   int32_t d;         /* head dim: 32, 64, 128 or 256                             */
   int32_t page;      /* tokens per page: 16, 32, 64, 128 or 256                  */
   int32_t n_pages;   /* pages of each cache                                      */
@@ -292,6 +293,8 @@ typedef struct {
   float scale;       /* of the scores; 0 selects 1 / sqrt(d)                     */
 } gdn_attn_dims;
 
+#define GDN_MAX_KV_ROWS (1 << 20) /* query rows of a key / value head */
+
 /* Rotates the step's queries and keys and appends keys and values.
  *   q [B][T][Hq][d], k, v [B][T][Hkv][d]   dtype, the layer's new rows
  *   rope        fp32 [n_pos][rot / 2][2]   cos and sin of every position; the
@@ -301,7 +304,8 @@ typedef struct {
  *   ctx_len     int32 [B]; page_table int32 [B][max_pages]
  *   k_cache, v_cache   written at the positions of the real slots
  *   q_out       dtype [B][T][Hq][d]  rotated queries, zero for padding slots;
- *               may be q itself (any other overlap is not allowed)
+ *               may be q itself (any other overlap, with k and v too, is
+ *               not allowed)
  *   kv_status   int32 [B] (may be NULL): the tree status if non-zero, else
  *               GDN_KV_BAD_LEN, GDN_KV_BAD_POS, GDN_KV_BAD_PAGE (pages of the
  *               real slots) or 0; non-zero sequences are skipped.
@@ -335,6 +339,7 @@ int gdn_tree_attend(const gdn_attn_dims* dims, const void* meta, const int32_t* 
  *   accepted   int32 [B]   accepted slot, -1 = nothing
  *   new_len    int32 [B]   written: ctx_len + depth(accepted) + 1, or ctx_len
  *              of a sequence that commits nothing; must not overlap ctx_len
+ *              or accepted
  *   kv_status  int32 [B] (may be NULL): the tree status if non-zero, else
  *              GDN_TREE_BAD_ACCEPTED, GDN_KV_BAD_LEN, GDN_KV_BAD_PAGE (pages
  *              of the path's rows, before and after) or 0; non-zero sequences
@@ -395,7 +400,8 @@ int gdn_tree_sample(const gdn_sample_dims* dims, const void* meta, const void* l
  *              empty tree or one with a non-zero status
  *   n_emitted  int32 [B]     written: depth(accepted) + 1
  *   emitted    int32 [B][T]  written: the tokens below the root, then the one
- *              sampled at the accepted node, then -1
+ *              sampled at the accepted node, then -1; must not overlap draft
+ *              or token
  * A negative token matches no draft. */
 int gdn_tree_accept(const gdn_dims* dims, const void* meta, const int32_t* draft,
                     const int32_t* token, int32_t* accepted, int32_t* n_emitted, int32_t* emitted,

@@ -897,6 +897,8 @@ int runs_for(long long blocks, long long slots) {
 
 // Workspace of S runs.
 int parts_for(const AttnArgs& a, int S, hipStream_t stream, Parts* ws) {
+  *ws = {nullptr, nullptr};
+  if (S == 1) return GDN_OK;  // every sequence is whole
   const size_t rows = size_t(2) * S * a.c.Hkv * a.T * (a.Hq / a.c.Hkv);
   int rc = GDN_OK;
   char* p = static_cast<char*>(stream_workspace(rows * (a.c.d * sizeof(float) + sizeof(float2)), stream, &rc));

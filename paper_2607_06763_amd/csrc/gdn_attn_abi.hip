@@ -27,8 +27,10 @@ static int check_attn(const gdn_attn_dims* d, const void* meta, const int32_t* n
     return set_error(GDN_EUNSUPPORTED, "%s: page=%d (supported 16, 32, 64, 128, 256)", who, d->page);
   if (d->T > GDN_MAX_T) return set_error(GDN_EUNSUPPORTED, "%s: T=%d > %d", who, d->T, GDN_MAX_T);
   // a grid's y and z; positions and row offsets inside a sequence are 32-bit
-  if (d->B > 65535 || d->Hq > 65535 / 4 || (long long)(d->max_pages) * d->page > 0x40000000LL)
-    return set_error(GDN_EUNSUPPORTED, "%s: B=%d Hq=%d max_pages=%d", who, d->B, d->Hq, d->max_pages);
+  if (d->B > 65535 || d->Hq > 65535 / 4 || (long long)(d->T) * (d->Hq / d->Hkv) > GDN_MAX_KV_ROWS ||
+      (long long)(d->max_pages) * d->page > 0x40000000LL)
+    return set_error(GDN_EUNSUPPORTED, "%s: B=%d T=%d Hq=%d Hkv=%d max_pages=%d", who, d->B, d->T, d->Hq, d->Hkv,
+                     d->max_pages);
   return GDN_OK;
 }
 
@@ -76,6 +78,9 @@ int gdn_kv_append(const gdn_attn_dims* dims, const void* meta, const int32_t* n_
   const size_t qb = size_t(dims->B) * dims->T * dims->Hq * dims->d * (dims->dtype == GDN_BF16 ? 2 : 4);
   if (q != q_out && overlap(q, qb, q_out, qb))
     return set_error(GDN_EINVAL, "kv_append: q and q_out overlap in part");
+  const size_t kb = qb / dims->Hq * dims->Hkv;
+  if (overlap(k, kb, q_out, qb) || overlap(v, kb, q_out, qb))
+    return set_error(GDN_EINVAL, "kv_append: q_out overlaps k or v");
   AttnArgs a = make_args(dims, meta, n_new, ctx_len, page_table);
   a.q = q;
   a.k = k;
@@ -115,7 +120,8 @@ int gdn_kv_commit(const gdn_attn_dims* dims, const void* meta, const int32_t* ac
   if (!accepted || !ctx_len || !page_table || !k_cache || !v_cache || !new_len)
     return set_error(GDN_EINVAL, "kv_commit: NULL tensor pointer");
   const size_t lb = size_t(dims->B) * 4;
-  if (overlap(ctx_len, lb, new_len, lb)) return set_error(GDN_EINVAL, "kv_commit: ctx_len and new_len overlap");
+  if (overlap(ctx_len, lb, new_len, lb) || overlap(accepted, lb, new_len, lb))
+    return set_error(GDN_EINVAL, "kv_commit: new_len overlaps ctx_len or accepted");
   AttnArgs a = make_args(dims, meta, nullptr, ctx_len, page_table);
   a.accepted = accepted;
   a.k_cache = k_cache;
@@ -166,6 +172,9 @@ int gdn_tree_accept(const gdn_dims* dims, const void* meta, const int32_t* draft
   if (dims->B == 0 || dims->T == 0) return GDN_OK;
   if (!draft || !token || !accepted || !n_emitted || !emitted)
     return set_error(GDN_EINVAL, "accept: NULL tensor pointer");
+  const size_t nb = size_t(dims->B) * dims->T * 4;
+  if (overlap(draft, nb, emitted, nb) || overlap(token, nb, emitted, nb))
+    return set_error(GDN_EINVAL, "accept: emitted overlaps draft or token");
   return launch_accept(dims->B, dims->T, meta, draft, token, accepted, n_emitted, emitted, stream);
 }
 
