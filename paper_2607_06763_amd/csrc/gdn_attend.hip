@@ -19,6 +19,8 @@
 // scan over them.
 #include <limits.h>
 
+#include <algorithm>
+
 #include "gdn_attn.h"
 
 namespace gdn {
@@ -101,17 +103,19 @@ __device__ __forceinline__ float half_sum(float x) {
 // ---------------------------------------------------------------------------
 // Schedule
 // ---------------------------------------------------------------------------
-// Positions of sequence b; -1 if it is skipped.
-__device__ __forceinline__ int length_of(const AttnArgs& a, int b) {
-  const int ctx = a.ctx_len[b], span = span_of(a, b);
-  if (a.meta && meta_ptrs(a.meta, a.B, a.T).status[b] != 0) return -1;
-  return len_status(a, ctx, span) ? -1 : ctx + span;
-}
+// A sequence: its cached positions, those with the step's (-1 if it is
+// skipped), and its tiles.  One without keys still has a tile: someone clears
+// its outputs.
+struct Seq {
+  int ctx, len, tiles;
+};
 
-// A sequence without keys still has a tile: someone clears its outputs.
-__device__ __forceinline__ int tiles_of(const AttnArgs& a, int b, int kt) {
-  const int n = b < a.B ? length_of(a, b) : 0;
-  return b < a.B ? (n > kt ? (n + kt - 1) / kt : 1) : 0;
+__device__ __forceinline__ Seq seq_of(const AttnArgs& a, int b, int kt) {
+  if (b >= a.B) return {0, 0, 0};
+  const int ctx = a.ctx_len[b], span = span_of(a, b);
+  const bool bad = a.meta && meta_ptrs(a.meta, a.B, a.T).status[b] != 0;
+  const int len = bad || len_status(a, ctx, span) ? -1 : ctx + span;
+  return {ctx, len, len > kt ? (len + kt - 1) / kt : 1};
 }
 
 // A value that every lane holds, in scalar registers.
@@ -134,55 +138,77 @@ __device__ __forceinline__ unsigned wave_scan(unsigned v) {
   return v;
 }
 
-// Tiles of 64 sequences stay below 2^32 (a page table's row spans at most 2^30
-// positions, a tile at least 32).
-struct Run {
-  long long total, length;  // tiles of all sequences, of a run
+// The tiles of all sequences in a row, cut into S equal runs.  Lane l keeps
+// sequence l of the first 64, so that these are loaded once.  Tiles of 64
+// sequences stay below 2^32 (a page table's row spans at most 2^30 positions, a
+// tile at least 32).
+struct Schedule {
+  Seq own;
+  unsigned upto;        // tiles of sequences 0 .. lane
+  long long total, run;  // tiles of all sequences, of a run
 };
 
-__device__ __forceinline__ Run run_length(const AttnArgs& a, int S, int kt) {
+__device__ __forceinline__ Schedule schedule(const AttnArgs& a, int S, int kt) {
   const int lane = threadIdx.x % kWave;
-  Run r = {0, 0};
-  for (int b0 = 0; b0 < a.B; b0 += kWave)
-    r.total += unsigned(__builtin_amdgcn_readlane(int(wave_scan(tiles_of(a, b0 + lane, kt))), kWave - 1));
-  r.length = uniform((r.total + S - 1) / S);
+  Schedule r;
+  r.own = seq_of(a, lane, kt);
+  r.upto = wave_scan(r.own.tiles);
+  r.total = unsigned(__builtin_amdgcn_readlane(int(r.upto), kWave - 1));
+  for (int b0 = kWave; b0 < a.B; b0 += kWave)
+    r.total += unsigned(__builtin_amdgcn_readlane(int(wave_scan(seq_of(a, b0 + lane, kt).tiles)), kWave - 1));
   r.total = uniform(r.total);
+  const long long most = r.total + S - 1;
+  r.run = uniform(most >> 32 ? most / S : (long long)(unsigned(most) / unsigned(S)));
   return r;
 }
 
+__device__ __forceinline__ Seq seq_at(const AttnArgs& a, const Schedule& w, int b, int kt) {
+  if (b < kWave)
+    return {__builtin_amdgcn_readlane(w.own.ctx, b), __builtin_amdgcn_readlane(w.own.len, b),
+            __builtin_amdgcn_readlane(w.own.tiles, b)};
+  const Seq x = seq_of(a, b, kt);
+  return {uniform(x.ctx), uniform(x.len), uniform(x.tiles)};
+}
+
 // Sequence that holds global tile g, and the tile at which it begins.
-__device__ __forceinline__ void find_tile(const AttnArgs& a, long long g, int kt, int* b, long long* start) {
+__device__ __forceinline__ void find_tile(const AttnArgs& a, const Schedule& w, long long g, int kt, int* b, long long* start) {
   const int lane = threadIdx.x % kWave;
-  long long run = 0;
-  for (int b0 = 0; b0 < a.B; b0 += kWave) {
-    const int n = tiles_of(a, b0 + lane, kt);
-    const unsigned inc = wave_scan(n);
-    const u64 past = __ballot(run + inc > g);
+  long long before = 0;
+  int n = w.own.tiles;
+  unsigned inc = w.upto;
+  for (int b0 = 0;;) {
+    const u64 past = __ballot(before + inc > g);
     if (past) {
       const int at = __builtin_ctzll(past);
       *b = b0 + at;
-      *start = uniform(run + unsigned(__builtin_amdgcn_readlane(int(inc), at)) - __builtin_amdgcn_readlane(n, at));
+      *start = uniform(before + unsigned(__builtin_amdgcn_readlane(int(inc), at)) - __builtin_amdgcn_readlane(n, at));
       return;
     }
-    run = uniform(run + unsigned(__builtin_amdgcn_readlane(int(inc), kWave - 1)));
+    before = uniform(before + unsigned(__builtin_amdgcn_readlane(int(inc), kWave - 1)));
+    b0 += kWave;
+    if (b0 >= a.B) break;
+    n = seq_of(a, b0 + lane, kt).tiles;
+    inc = wave_scan(n);
   }
   *b = a.B;
-  *start = run;
+  *start = before;
 }
 
 // First global tile of sequence b.
-__device__ __forceinline__ long long first_tile(const AttnArgs& a, int b, int kt) {
+__device__ __forceinline__ long long first_tile(const AttnArgs& a, const Schedule& w, int b, int kt) {
   const int lane = threadIdx.x % kWave;
   long long n = 0;
+  if (b < kWave) return b ? unsigned(__builtin_amdgcn_readlane(int(w.upto), b - 1)) : 0;
   for (int b0 = 0; b0 < b; b0 += kWave) {
     const int i = b0 + lane;
-    n += unsigned(__builtin_amdgcn_readlane(int(wave_scan(i < b ? tiles_of(a, i, kt) : 0)), kWave - 1));
+    n += unsigned(__builtin_amdgcn_readlane(int(wave_scan(i < b ? seq_of(a, i, kt).tiles : 0)), kWave - 1));
   }
   return uniform(n);
 }
 
 // Workspace of the parts: slot 2 u + 1 of run u for a part that begins inside
-// the run, 2 u for one that begins with it.
+// the run, 2 u for one that begins with it.  A row that sees nothing there,
+// and one of a padding slot, has maximum -inf and sum 0.
 struct Parts {
   float* o;    // [2 S][Hkv][M][d]
   float2* ml;  // [2 S][Hkv][M]
@@ -284,11 +310,13 @@ struct RowAt {
   bool real;
 };
 
-__device__ __forceinline__ RowAt row_at(const AttnArgs& a, const MetaPtrs& m, int b, int h, int r, int M, bool skip) {
+__device__ __forceinline__ RowAt row_of(const AttnArgs& a, int h, int r) {
   const int G = a.Hq / a.c.Hkv;
-  RowAt w;
-  w.slot = r < M ? r / G : 0;
-  w.head = h * G + (r < M ? r % G : 0);
+  return {r / G, h * G + r % G, true};
+}
+
+__device__ __forceinline__ RowAt row_at(const AttnArgs& a, const MetaPtrs& m, int b, int h, int r, int M, bool skip) {
+  RowAt w = row_of(a, h, r < M ? r : 0);
   w.real = r < M && !skip;
   if (w.real) w.real = a.meta ? m.depth[size_t(b) * a.T + w.slot] >= 0 : w.slot < span_of(a, b);
   return w;
@@ -374,28 +402,28 @@ __global__ __launch_bounds__(kThreads, (stream_groups<T, D>())) void attend_stre
   const int tid = threadIdx.x, lane = tid % kWave, w = uniform(tid / kWave), n32 = lane & 31, h2 = lane >> 5;
   const int u = blockIdx.x, h = blockIdx.y, rt = blockIdx.z;
   const int M = a.T * (a.Hq / a.c.Hkv);
-  const Run all_runs = run_length(a, S, kStreamKeys);
-  const long long run = all_runs.length, total = all_runs.total;
+  const Schedule plan = schedule(a, S, kStreamKeys);
+  const long long run = plan.run, total = plan.total;
   long long g = u * run;
   const long long end = g + run < total ? g + run : total;
   if (g >= end) return;
   int b;
   long long start;
-  find_tile(a, g, kStreamKeys, &b, &start);
+  find_tile(a, plan, g, kStreamKeys, &b, &start);
 
   const MetaPtrs m = meta_ptrs(a.meta, a.B, a.T);
   const T *kc = reinterpret_cast<const T*>(a.k_cache), *vc = reinterpret_cast<const T*>(a.v_cache);
   const int mask = (1 << a.c.page_shift) - 1, shift = a.c.page_shift;
   const float c = a.scale * kLog2e;
   for (; g < end; ++b, s_from += turn ? -1 : 1, turn ^= 1) {
-    const int tiles = uniform(tiles_of(a, b, kStreamKeys));
+    const Seq seq = seq_at(a, plan, b, kStreamKeys);
+    const int tiles = seq.tiles, len = seq.len, ctx = seq.ctx;
     const int t0 = int(g - start), n = int(min((long long)(tiles), end - start)) - t0;
     const bool whole = n == tiles;
     const int slot = 2 * u + (g > u * run ? 1 : 0);
     start += tiles;
     g = start;
 
-    const int len = uniform(length_of(a, b)), ctx = uniform(a.ctx_len[b]);
     const int r = rt * 32 + n32;
     const RowAt at = row_at(a, m, b, h, r, M, len < 0);
     const int32_t* row = a.page_table + size_t(b) * a.c.max_pages;
@@ -507,7 +535,7 @@ __global__ __launch_bounds__(kThreads, (stream_groups<T, D>())) void attend_stre
     // join the waves
     if (tid == 0) *s_from = INT_MAX;
     const float l = half_sum(st.l);
-    if (h2 == 0) s_ml[w * 32 + n32] = make_float2(st.m, l);
+    if (h2 == 0) s_ml[w * 32 + n32] = at.real ? make_float2(st.m, l) : make_float2(-INFINITY, 0.0f);
     if (r < M) {
 #pragma unroll
       for (int k = 0; k < D / 32; ++k)
@@ -536,10 +564,9 @@ __global__ __launch_bounds__(kThreads, (stream_groups<T, D>())) void attend_stre
         o.x += f * y.x, o.y += f * y.y, o.z += f * y.z, o.w += f * y.w;
       }
       if (whole) {
-        const RowAt to = row_at(a, m, b, h, rt * 32 + rr, M, len < 0);
-        const float inv = to.real && sum != 0.0f ? 1.0f / sum : 0.0f;
-        const bool on = to.real && sum != 0.0f;
-        store4(reinterpret_cast<T*>(a.out) + row_offset<T>(a, b, to) + d,
+        const bool on = sum != 0.0f;
+        const float inv = on ? 1.0f / sum : 0.0f;
+        store4(reinterpret_cast<T*>(a.out) + row_offset<T>(a, b, row_of(a, h, rt * 32 + rr)) + d,
                on ? make_float4(o.x * inv, o.y * inv, o.z * inv, o.w * inv) : make_float4(0, 0, 0, 0));
       } else {
         const size_t i = (size_t(slot) * a.c.Hkv + h) * M + rt * 32 + rr;
@@ -607,14 +634,14 @@ __global__ __launch_bounds__(kThreads, Tile<D>::kPerCu) void attend_tile_kernel(
   const int x = blockIdx.x % 8, y = blockIdx.x / 8, rt = y % rts, uh = y / rts * 8 + x;
   const int u = uh / a.c.Hkv, h = uh % a.c.Hkv;
   if (u >= S) return;
-  const Run all_runs = run_length(a, S, KT);
-  const long long run = all_runs.length, total = all_runs.total;
+  const Schedule plan = schedule(a, S, KT);
+  const long long run = plan.run, total = plan.total;
   long long g = u * run;
   const long long end = g + run < total ? g + run : total;
   if (g >= end) return;
   int b;
   long long start;
-  find_tile(a, g, KT, &b, &start);
+  find_tile(a, plan, g, KT, &b, &start);
 
   const MetaPtrs m = meta_ptrs(a.meta, a.B, a.T);
   const BF16 *kc = reinterpret_cast<const BF16*>(a.k_cache), *vc = reinterpret_cast<const BF16*>(a.v_cache);
@@ -623,14 +650,14 @@ __global__ __launch_bounds__(kThreads, Tile<D>::kPerCu) void attend_tile_kernel(
   const BF16 *kh = kc + block_of(a.c, 0, h), *vh = vc + block_of(a.c, 0, h);
   const float c = a.scale * kLog2e;
   for (; g < end; ++b) {
-    const int tiles = uniform(tiles_of(a, b, KT));
+    const Seq seq = seq_at(a, plan, b, KT);
+    const int tiles = seq.tiles, len = seq.len, ctx = seq.ctx;
     const int t0 = int(g - start), t1 = int(min((long long)(tiles), end - start));
     const bool whole = t1 - t0 == tiles;
     const int slot = 2 * u + (g > u * run ? 1 : 0);
     start += tiles;
     g = start;
 
-    const int len = uniform(length_of(a, b)), ctx = uniform(a.ctx_len[b]);
     const int r = rt * kTileRows + w * 32 + n32;
     const RowAt at = row_at(a, m, b, h, r, M, len < 0);
     const int32_t* row = a.page_table + size_t(b) * a.c.max_pages;
@@ -800,7 +827,7 @@ __global__ __launch_bounds__(kThreads, Tile<D>::kPerCu) void attend_tile_kernel(
       const float inv = on ? 1.0f / l : 0.0f;
       const size_t i = (size_t(slot) * a.c.Hkv + h) * M + r;
       BF16* out = reinterpret_cast<BF16*>(a.out) + row_offset<BF16>(a, b, at);
-      if (!whole && h2 == 0) ws.ml[i] = make_float2(st.m, l);
+      if (!whole && h2 == 0) ws.ml[i] = at.real ? make_float2(st.m, l) : make_float2(-INFINITY, 0.0f);
 #pragma unroll
       for (int k = 0; k < D / 32; ++k)
 #pragma unroll
@@ -826,52 +853,82 @@ __global__ __launch_bounds__(kThreads, Tile<D>::kPerCu) void attend_tile_kernel(
 }
 
 // ---------------------------------------------------------------------------
-// Joins the parts of the sequences that several runs share.
+// Joins the parts of the sequences that several runs share.  Four channels of
+// a row a thread; with few rows and many parts `lanes` threads share these
+// (taken by one thread in turn they cost 0.15 us each: 20 us where two
+// sequences share 512 runs, 5 us this way).  What it costs otherwise is a trip
+// for the lengths, one for the parts and one for the outputs.
 // ---------------------------------------------------------------------------
 template <typename T>
-__global__ __launch_bounds__(kThreads) void attend_join_kernel(AttnArgs a, int S, int kt, Parts ws) {
+__global__ __launch_bounds__(kThreads) void attend_join_kernel(AttnArgs a, int S, int kt, int lanes, Parts ws) {
+  __shared__ float4 s_o[kThreads];
+  __shared__ float2 s_ml[kThreads];
   const int b = blockIdx.z, h = blockIdx.y, D = a.c.d, M = a.T * (a.Hq / a.c.Hkv);
-  const long long run = run_length(a, S, kt).length;
-  const long long t0 = first_tile(a, b, kt), t1 = t0 + tiles_of(a, b, kt) - 1;
-  const int u0 = int(t0 / run), u1 = int(t1 / run);
+  const Schedule plan = schedule(a, S, kt);
+  const long long run = plan.run, t0 = first_tile(a, plan, b, kt), t1 = t0 + seq_at(a, plan, b, kt).tiles - 1;
+  const int u0 = plan.total >> 31 ? int(t0 / run) : int(t0) / int(run);
+  const int u1 = plan.total >> 31 ? int(t1 / run) : int(t1) / int(run);
   if (u0 == u1) return;
-  const int per = kThreads / (D / 4), r = blockIdx.x * per + threadIdx.x / (D / 4), d = threadIdx.x % (D / 4) * 4;
-  if (r >= M) return;
-  const MetaPtrs m = meta_ptrs(a.meta, a.B, a.T);
-  const RowAt at = row_at(a, m, b, h, r, M, false);
-  auto part = [&](int u) { return (size_t(2 * u + (u == u0 && t0 > u0 * run ? 1 : 0)) * a.c.Hkv + h) * M + r; };
-  float mx = -INFINITY, sum = 0.0f;
-  float4 o = make_float4(0, 0, 0, 0);
-  constexpr int kAhead = 8;  // parts in flight
-  for (int u = u0; u <= u1; u += kAhead) {
-    float2 ml[kAhead];
-    float4 y[kAhead];
+  const int q = D / 4, per = kThreads / q / lanes;
+  const int d = threadIdx.x % q * 4, at = threadIdx.x / q % lanes, rr = threadIdx.x / q / lanes;
+  const int first = 2 * u0 + (t0 > u0 * run ? 1 : 0);
+  for (int r0 = blockIdx.x * per; r0 < M; r0 += gridDim.x * per) {
+    const int r = min(r0 + rr, M - 1);
+    float mx = -INFINITY, sum = 0.0f;
+    float4 o = make_float4(0, 0, 0, 0);
+    constexpr int kAhead = 8;  // parts in flight
+    for (int v = u0; v <= u1; v += kAhead * lanes) {
+      float2 ml[kAhead];
+      float4 y[kAhead];
 #pragma unroll
-    for (int k = 0; k < kAhead; ++k) {
-      const size_t i = part(min(u + k, u1));
-      ml[k] = ws.ml[i];
-      y[k] = *reinterpret_cast<const float4*>(ws.o + i * D + d);
+      for (int k = 0; k < kAhead; ++k) {
+        if (v + k * lanes > u1) continue;
+        const int u = min(v + k * lanes + at, u1);
+        const size_t i = (size_t(u == u0 ? first : 2 * u) * a.c.Hkv + h) * M + r;
+        ml[k] = ws.ml[i];
+        y[k] = *reinterpret_cast<const float4*>(ws.o + i * D + d);
+      }
+      float top = mx;
+#pragma unroll
+      for (int k = 0; k < kAhead; ++k)
+        if (v + k * lanes <= u1) top = fmaxf(top, ml[k].x);
+      const float fix = mx == -INFINITY ? 0.0f : __builtin_amdgcn_exp2f(mx - top);
+      if (mx > -INFINITY) sum *= fix, o.x *= fix, o.y *= fix, o.z *= fix, o.w *= fix;
+      mx = top;
+#pragma unroll
+      for (int k = 0; k < kAhead; ++k) {
+        // a part without a visible key has nothing (one whose scores are not
+        // numbers has a sum that is none)
+        if (v + k * lanes + at > u1 || (ml[k].x == -INFINITY && ml[k].y == 0.0f)) continue;
+        const float f = ml[k].x == -INFINITY ? 0.0f : __builtin_amdgcn_exp2f(ml[k].x - mx);
+        sum += f * ml[k].y;
+        o.x += f * y[k].x, o.y += f * y[k].y, o.z += f * y[k].z, o.w += f * y[k].w;
+      }
     }
-    float top = mx;
-#pragma unroll
-    for (int k = 0; k < kAhead; ++k) top = fmaxf(top, ml[k].x);
-    const float fix = mx == -INFINITY ? 0.0f : __builtin_amdgcn_exp2f(mx - top);
-    if (mx > -INFINITY) sum *= fix, o.x *= fix, o.y *= fix, o.z *= fix, o.w *= fix;
-    mx = top;
-#pragma unroll
-    for (int k = 0; k < kAhead; ++k) {
-      // a part without a visible key has nothing (one whose scores are not
-      // numbers has a sum that is none)
-      if (u + k > u1 || (ml[k].x == -INFINITY && ml[k].y == 0.0f)) continue;
-      const float f = ml[k].x == -INFINITY ? 0.0f : __builtin_amdgcn_exp2f(ml[k].x - mx);
-      sum += f * ml[k].y;
-      o.x += f * y[k].x, o.y += f * y[k].y, o.z += f * y[k].z, o.w += f * y[k].w;
+    if (lanes > 1) {
+      __syncthreads();  // the row before is read
+      s_o[threadIdx.x] = o;
+      s_ml[threadIdx.x] = make_float2(mx, sum);
+      __syncthreads();
+      if (at) continue;
+      for (int k = 1; k < lanes; ++k) mx = fmaxf(mx, s_ml[threadIdx.x + k * q].x);
+      sum = 0.0f;
+      o = make_float4(0, 0, 0, 0);
+      for (int k = 0; k < lanes; ++k) {
+        const float2 ml = s_ml[threadIdx.x + k * q];
+        const float4 y = s_o[threadIdx.x + k * q];
+        if (ml.x == -INFINITY && ml.y == 0.0f) continue;
+        const float f = ml.x == -INFINITY ? 0.0f : __builtin_amdgcn_exp2f(ml.x - mx);
+        sum += f * ml.y;
+        o.x += f * y.x, o.y += f * y.y, o.z += f * y.z, o.w += f * y.w;
+      }
     }
+    if (r0 + rr >= M) continue;
+    const bool on = sum != 0.0f;
+    const float inv = on ? 1.0f / sum : 0.0f;
+    store4(reinterpret_cast<T*>(a.out) + row_offset<T>(a, b, row_of(a, h, r)) + d,
+           on ? make_float4(o.x * inv, o.y * inv, o.z * inv, o.w * inv) : make_float4(0, 0, 0, 0));
   }
-  const bool on = at.real && sum != 0.0f;
-  const float inv = on ? 1.0f / sum : 0.0f;
-  store4(reinterpret_cast<T*>(a.out) + row_offset<T>(a, b, at) + d,
-         on ? make_float4(o.x * inv, o.y * inv, o.z * inv, o.w * inv) : make_float4(0, 0, 0, 0));
 }
 
 int after_launch() {
@@ -910,8 +967,16 @@ int parts_for(const AttnArgs& a, int S, hipStream_t stream, Parts* ws) {
 template <typename T>
 int launch_join(const AttnArgs& a, int S, int kt, const Parts& ws, hipStream_t stream) {
   if (S == 1) return GDN_OK;  // no sequence is shared
-  const int M = a.T * (a.Hq / a.c.Hkv), per = kThreads / (a.c.d / 4);
-  attend_join_kernel<T><<<dim3((M + per - 1) / per, a.c.Hkv, a.B), kThreads, 0, stream>>>(a, S, kt, ws);
+  const int M = a.T * (a.Hq / a.c.Hkv), q = a.c.d / 4;
+  // threads for the parts of a sequence (S / B on average): more than one while
+  // each has over four and the rows alone give under two workgroups a CU
+  int lanes = 1;
+  while (lanes < kThreads / q && 4LL * lanes * a.B < S && (long long)(M) * q * lanes * a.c.Hkv * a.B < 512 * kThreads)
+    lanes *= 2;
+  const int per = kThreads / q / lanes, blocks = (M + per - 1) / per;
+  // a round of workgroups, if there are rows for more
+  const int most = std::max(1, 2048 / (a.c.Hkv * a.B));
+  attend_join_kernel<T><<<dim3(std::min(blocks, most), a.c.Hkv, a.B), kThreads, 0, stream>>>(a, S, kt, lanes, ws);
   return after_launch();
 }
 

@@ -81,11 +81,6 @@ __device__ __forceinline__ int len_status(const AttnArgs& a, int ctx, int span) 
   return (span < 0 || span > a.T || ctx < 0 || (long long)(ctx) + span > room) ? GDN_KV_BAD_LEN : 0;
 }
 
-// 16-byte move.
-__device__ __forceinline__ void copy16(void* dst, const void* src) {
-  *reinterpret_cast<uint4*>(dst) = *reinterpret_cast<const uint4*>(src);
-}
-
 // fp32 -> bf16, round to nearest even (NaN stays NaN)
 __device__ __forceinline__ void st(float* p, float x) { *p = x; }
 __device__ __forceinline__ void st(BF16* p, float x) { *reinterpret_cast<__bf16*>(p) = (__bf16)x; }
