@@ -435,19 +435,24 @@ __global__ __launch_bounds__(kThreads, (stream_groups<T, D>())) void attend_stre
     int p0 = (t0 * kWaves + w) * 32;
     const int key = Mt::key_of(n32);
     const T *vp0, *vp1;  // values of the first and the last 16 keys
-    const T* kp;         // the lane's key
+    const T* kp;         // the lane's first pack of its key
     unsigned valid;
-    auto pages = [&](int p) {
-      const int id0 = uniform(p < len ? page_of(a.c, row, p) : -1);
-      const int id1 = uniform(p + 16 < len ? page_of(a.c, row, p + 16) : -1);
+    auto entry = [&](int p) { return row[p < len ? p >> shift : 0]; };
+    auto set_pages = [&](int p, int e0, int e1) {  // of their page-table entries
+      const bool on0 = p < len && unsigned(e0) < unsigned(a.c.n_pages);
+      const bool on1 = p + 16 < len && unsigned(e1) < unsigned(a.c.n_pages);
       const unsigned all = len - p >= 32 ? ~0u : (1u << (len - p)) - 1;  // p < len
-      valid = (id0 >= 0 ? all & 0xffffu : 0) | (id1 >= 0 ? all & 0xffff0000u : 0);
-      const size_t b0 = block_of(a.c, id0 < 0 ? 0 : id0, h), b1 = block_of(a.c, id1 < 0 ? 0 : id1, h);
+      valid = (on0 ? all & 0xffffu : 0) | (on1 ? all & 0xffff0000u : 0);
+      const size_t b0 = block_of(a.c, on0 ? e0 : 0, h), b1 = block_of(a.c, on1 ? e1 : 0, h);
       vp0 = vc + b0 + size_t(p & mask) * D;
       vp1 = vc + b1 + size_t((p + 16) & mask) * D;
-      kp = kc + (key & 16 ? b1 : b0) + size_t((p + key) & mask) * X;
+      kp = kc + (key & 16 ? b1 : b0) + (size_t((p + key) & mask) + (size_t(h2) << shift)) * X;
     };
-    auto k_pack = [&](const T* p, int k) { return load16<Frag>(p + ((size_t(2 * k + h2) << shift) * X)); };
+    auto pages = [&](int p) {
+      const int e0 = entry(p), e1 = entry(p + 16);
+      set_pages(p, uniform(e0), uniform(e1));
+    };
+    auto k_pack = [&](const T* p, int k) { return load16<Frag>(p + (2 * k * X << shift)); };
     auto v_pack = [&](int q, int k) {
       return load16<Frag>((q < NS / 2 ? vp0 : vp1) + ((2 * (q % (NS / 2)) + h2) * D + k * 32 + n32) * X);
     };
@@ -497,26 +502,58 @@ __global__ __launch_bounds__(kThreads, (stream_groups<T, D>())) void attend_stre
         }
       }
     }
-    // slots of the tree, the end of the cache and pages that are left out
-    for (; p0 < last; p0 += kStreamKeys) {
-      pages(p0);
+    // slots of the tree, the end of the cache and pages that are left out, and
+    // all keys where the registers do not hold a tile ahead: packs load a group
+    // ahead of their products, the next tile's first keys behind the last values
+    constexpr int kG = NK < 4 ? NK : 4;
+    Frag kf[2][kG], vf[2][D / 32];
+    auto k_group = [&](Frag (&f)[kG], int n) {
+#pragma unroll
+      for (int k = 0; k < kG; ++k) f[k] = k_pack(kp, n * kG + k);
+    };
+    auto v_row = [&](Frag (&f)[D / 32], int q) {
+#pragma unroll
+      for (int k = 0; k < D / 32; ++k) f[k] = v_pack(q, k);
+    };
+    if (p0 < last) k_group(kf[0], 0);
+    while (p0 < last) {
+      const int e0 = entry(p0 + kStreamKeys), e1 = entry(p0 + kStreamKeys + 16);
       f32x16 acc = {};
 #pragma unroll
-      for (int k = 0; k < NK; ++k) acc = Mt::mma(k_pack(kp, k), st.q[k], acc);
+      for (int n = 0; n < NK / kG; ++n) {
+        if (n + 1 < NK / kG) k_group(kf[(n + 1) & 1], n + 1);
+        else v_row(vf[0], 0);
+        __builtin_amdgcn_sched_barrier(0);
+#pragma unroll
+        for (int k = 0; k < kG; ++k) acc = Mt::mma(kf[n & 1][k], st.q[n * kG + k], acc);
+        __builtin_amdgcn_sched_barrier(0);
+      }
       const bool masked = p0 + 32 > ctx || valid != ~0u;
       const unsigned seen = masked ? unsigned(seen_bits(a, m, b, at.slot, ctx, p0)) & valid : ~0u;
+      const unsigned there = valid;
       float s[1][16];
 #pragma unroll
       for (int i = 0; i < 16; ++i) s[0][i] = where_seen(acc[i], seen >> (h2 * X), i / X * 2 * X + i % X);
       st.template softmax<1>(s, c);
       bool left = false;
+      const int now = p0;
 #pragma unroll
       for (int q = 0; q < NS; ++q) {
+        if (q + 1 < NS) {
+          v_row(vf[(q + 1) & 1], q + 1);
+        } else {
+          p0 += kStreamKeys;
+          if (p0 < last) {
+            set_pages(p0, uniform(e0), uniform(e1));
+            k_group(kf[0], 0);
+          }
+        }
+        __builtin_amdgcn_sched_barrier(0);
         const Frag p = Mt::pack(&s[0][q * X]);
-        const unsigned ok = valid >> (q * 2 * X + h2 * X);
+        const unsigned ok = there >> (q * 2 * X + h2 * X);
 #pragma unroll
         for (int k = 0; k < D / 32; ++k) {
-          Frag f = v_pack(q, k);
+          Frag f = vf[q & 1][k];
           if (masked) {  // a masked weight is 0, and must stay so whatever it meets
 #pragma unroll
             for (int e = 0; e < X; ++e)
@@ -527,9 +564,9 @@ __global__ __launch_bounds__(kThreads, (stream_groups<T, D>())) void attend_stre
           }
           st.o[k] = Mt::mma(f, p, st.o[k]);
         }
-        __builtin_amdgcn_sched_barrier(0);  // one row of value packs in registers at a time
+        __builtin_amdgcn_sched_barrier(0);
       }
-      if (from == INT_MAX && __any(left)) from = p0;
+      if (from == INT_MAX && __any(left)) from = now;
     }
 
     // join the waves
