@@ -54,6 +54,11 @@ struct Mat<BF16> {
     for (int e = 0; e < 8; ++e) f[e] = (__bf16)p[e];
     return f;
   }
+  // whether any value is infinite or NaN: a full exponent reaches the sign's place
+  static __device__ __forceinline__ bool odd(Frag f) {
+    const u32x4 t = (__builtin_bit_cast(u32x4, f) & 0x7f807f80u) + 0x00800080u;
+    return (t[0] | t[1] | t[2] | t[3]) & 0x80008000u;
+  }
   // bits of value e, and the pack without it
   static __device__ __forceinline__ unsigned bits(Frag f, int e) {
     return __builtin_bit_cast(u32x4, f)[e / 2] << (e & 1 ? 0 : 16) & 0xffff0000u;
@@ -776,6 +781,8 @@ __global__ __launch_bounds__(kThreads, Tile<D>::kPerCu) void attend_tile_kernel(
       // the keys of the next tile and the values of this one are there, the
       // buffers of their predecessors are free
       const u64 valid = __ballot(id >= 0);
+      u64 seen = ~u64(0);
+      if (p0 + KT > ctx) seen = seen_bits(a, m, b, at.slot, ctx, p0);
       asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
       __syncthreads();
       id = id1;
@@ -793,21 +800,20 @@ __global__ __launch_bounds__(kThreads, Tile<D>::kPerCu) void attend_tile_kernel(
         for (int q = tid; q < Tl::kPacks; q += kThreads) {
           const unsigned ok = unsigned(valid >> (q / D * 8)) & 0xffu;
           Frag y = load16<Frag>(sv + q);
-          bool change = false;
+          if (ok == 0xffu && !Mt::odd(y)) continue;
 #pragma unroll
           for (int e = 0; e < 8; ++e) {
             const bool on = (ok >> e) & 1;
             if (!on || (Mt::bits(y, e) & kExp) == kExp) {
               mine = mine || on;
-              change = true;
               y = Mt::without(y, e);
             }
           }
-          if (change) *reinterpret_cast<Frag*>(const_cast<uint4*>(sv + q)) = y;
+          *reinterpret_cast<Frag*>(const_cast<uint4*>(sv + q)) = y;
         }
         if (mine) atomicMin(s_from, p0);
         __syncthreads();
-        const u64 seen = seen_bits(a, m, b, at.slot, ctx, p0) & valid;
+        seen &= valid;
 #pragma unroll
         for (int nb = 0; nb < NB; ++nb)
 #pragma unroll
