@@ -375,7 +375,15 @@ __device__ void add_not_finite(const AttnArgs& a, const MetaPtrs& m, int b, int 
 // ---------------------------------------------------------------------------
 // Few rows: a workgroup's four waves share a tile of 32 rows and take 32 keys
 // each of a tile of 128.  Keys and values go from memory to the operand
-// registers (512 contiguous bytes per 32 lanes), a tile ahead of their use.
+// registers (512 contiguous bytes per 32 lanes), ahead of their use.
+//
+// Bound by the bytes of the cache (32 x 1 token, 32 + 8 heads of 128 in bf16,
+// up to 8 k tokens: 656 MB in 117 us, 5.6 TB/s; a large copy reaches 5.1), with
+// a short cache by the chain lengths - pages - keys - values - parts (10 us),
+// in fp32 by the products, which take 8 times those of bf16: 6 x 14 nodes,
+// 48 + 8 heads of 128, 9 k tokens 159 us, of which about 136 are products (a
+// quarter on rows that fill up the tiles); 8 x 99 nodes, 16 + 4 heads of 64,
+// 1 k tokens 45 us, 27 of them products.
 // ---------------------------------------------------------------------------
 constexpr int kThreads = 256;
 constexpr int kWaves = kThreads / kWave;
@@ -386,8 +394,9 @@ constexpr size_t stream_lds() {
   return sizeof(float) * kWaves * 32 * (D + 4) + sizeof(float2) * kWaves * 32 + 16;
 }
 
-// Registers of a wave: Q, K, V of 32 keys and O take D (2 X 4 / X^2 ..) each;
-// a workgroup per SIMD wave pair up to here, one above.
+// Workgroups a CU: two where the registers allow (Q, O and 32 keys and values
+// ahead).  fp32 heads of 64 dims, 8 x 99 nodes: 45 us, 55 with one; bf16 of 128,
+// 16 x 1 token over 8 k: 40.8 and 42.0, over 600 (4 x 1): 13.1 and 12.2.
 template <typename T, int D>
 constexpr int stream_groups() {
   return D * int(sizeof(T)) <= 256 ? 2 : 1;
@@ -396,7 +405,10 @@ constexpr int stream_groups() {
 template <typename T, int D>
 __global__ __launch_bounds__(kThreads, (stream_groups<T, D>())) void attend_stream_kernel(AttnArgs a, int S, Parts ws) {
   constexpr int X = Pack<T>::kN, NK = D / (2 * X), NS = 32 / (2 * X);
-  constexpr bool kAhead = D * int(sizeof(T)) <= 512;  // registers for a tile of keys and values ahead
+  // A whole tile of keys and values ahead, where registers hold it: fp32 heads
+  // of 128 dims 159 us (167 without; 6 x 14 nodes, 9 k tokens).  bf16 heads of
+  // 256, which it fits only with spills: 49 us, 42 without (16 x 1, 8 k).
+  constexpr bool kAhead = D <= 128;
   typedef Mat<T> Mt;
   typedef typename Mt::Frag Frag;
   extern __shared__ __align__(16) char s_raw[];
@@ -645,7 +657,16 @@ __global__ __launch_bounds__(kThreads, (stream_groups<T, D>())) void attend_stre
 // the exponentials of this one, a product and the work of 256 / d scores in
 // turn: the matrix units run while the others do.  Operands come from LDS a
 // group ahead of their products (left to itself the compiler waits for each).
-// Up to d = 128 two workgroups a CU; at 256 one, with the registers of both.
+// Up to d = 128 two workgroups a CU (16 x 128 nodes over 8 k tokens 240 us, 299
+// with one; 16 x 16 nodes 62.8 and 58.9); at 256 one, with the registers of both.
+//
+// Bound by the matrix units at the clock that they leave: 32 + 8 heads of 128,
+// 16 x 128 nodes, up to 8 k tokens 177 GFLOP in 240 us with the join, 740
+// TFLOP/s (a large bf16 product reaches 1180).  A tile takes a pair of waves
+// 2600 clocks, 2048 of them products; the first tile and the outputs of a run
+// take as long as seven tiles, which is what bounds the short calls (27 x 90
+// nodes over 850 tokens 26 us).  Heads of 256, two chunks of 512 over 12 k
+// tokens: 156 GFLOP in 228 us.
 // ---------------------------------------------------------------------------
 template <int D>
 struct Tile {
@@ -981,7 +1002,8 @@ int after_launch() {
 
 // Runs for `blocks` workgroups per run on `slots` workgroup places: as many as
 // fill the places, in up to four rounds where fewer would leave more than a
-// tenth of them empty.
+// tenth of them empty (a key head and row tile count that does not divide the
+// places; calls whose count does are the same with one round).
 int runs_for(long long blocks, long long slots) {
   long long best = 1;
   double fill = 0.0;
@@ -1056,6 +1078,9 @@ int launch_tile(const AttnArgs& a, hipStream_t stream) {
 
 template <int D>
 int launch_dim(const AttnArgs& a, hipStream_t stream) {
+  // One tile of rows: every wave would load and multiply three empty ones.  4 key
+  // heads of 128, 16 sequences of 8 k tokens: 8 rows 40.8 us, 45.2 with shared
+  // tiles; 32 rows 47.4, 48.7; 64 rows 53.7 and 54.4; 128 rows 73.4 and 62.8.
   if (a.dtype != GDN_BF16) return launch_stream<float, D>(a, stream);
   if (a.T * (a.Hq / a.c.Hkv) > 32) return launch_tile<D>(a, stream);
   return launch_stream<BF16, D>(a, stream);

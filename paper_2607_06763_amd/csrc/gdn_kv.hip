@@ -43,9 +43,10 @@ __device__ __forceinline__ void turn(u32x4& x, u32x4& y, const float2* cs) {
 // fp32), so that a value pack whose 8 tokens are all new is written whole.
 // Bound by bytes, and by the chain in front of them (length and depths, then
 // pages and angles): the queries, most of the bytes, are on their way before
-// it.  32 x 128 slots, 24 + 4 heads of 256, cold caches: 44 us for 120 MB (64
-// with every load behind the checks, 50 with ordinary loads; non-temporal
-// stores took 42, but the rows are read again by the attention).
+// it.  32 x 128 slots, 24 + 4 heads of 256, cold caches: 44 to 49 us for 120 MB
+// (64 with every load behind the checks, 50 with ordinary loads where this
+// took 44; non-temporal stores took 42, but the rows are read again by the
+// attention).  One token: 5 us, the chain.
 // ---------------------------------------------------------------------------
 template <typename T>
 __global__ __launch_bounds__(kThreads) void append_kernel(AttnArgs a, int qparts, int kparts) {
@@ -256,6 +257,11 @@ __global__ __launch_bounds__(kThreads) void append_kernel(AttnArgs a, int qparts
 // row's old one: all rows of a pack (keys) or of a channel (values) are
 // loaded before any of them is stored, a barrier between.  One workgroup per
 // (slice of channels, key head, sequence); slice 0 is the keys.
+//
+// Bound by its chain (status and lengths, ancestors, pages, rows) and, with many
+// sequences, by the bytes around the rows: a value's row is 2 or 4 bytes of a
+// 16-byte pack, one pack a channel, so a row of 128 fp32 values touches 128
+// packs.  8 x 64 nodes 10 us, 32 x 128 nodes, fp32, 8 heads of 128: 16 us.
 // ---------------------------------------------------------------------------
 constexpr int kHold = 2;       // rows a thread holds between the load and the store
 constexpr int kSliceV = 64;    // value channels of a workgroup

@@ -25,6 +25,12 @@ namespace {
 // stay in vocabulary order; no cut at all takes the last of these only.
 // Rows for which LDS is too small (thousands of equal logits) take the cuts by
 // halving the value.
+//
+// Bound by instructions, not bytes: a logit is read once or twice and costs 10
+// to 20 of them.  512 rows of 131072 in bf16, every kind of cut: 113 us, 1.2
+// TB/s of logits; 1056 rows of 50001 in fp32 with top_p: 112 us, 1.7 TB/s (a
+// third of the slots is padding).  One row of 131072: 21 us, four trips over a
+// chip's one workgroup.
 // ---------------------------------------------------------------------------
 constexpr int kBins = 1024;
 constexpr float kBinsPerOctave = kBins / 32.0f;  // w is 0 beyond 32 octaves
@@ -798,7 +804,8 @@ __global__ __launch_bounds__(NT, 4) void sample_kernel(SampleArgs a) {
 // ---------------------------------------------------------------------------
 // Acceptance: one workgroup per tree.  A slot is taken if its draft token was
 // sampled at its parent and no lower slot of that parent has it too; the
-// accepted node is the deepest whose ancestors are all taken.
+// accepted node is the deepest whose ancestors are all taken.  A chain of three
+// loads (parents, their tokens, ancestors): 4 to 5 us, 8 x 64 and 32 x 33 slots.
 // ---------------------------------------------------------------------------
 __global__ __launch_bounds__(GDN_MAX_T) void accept_kernel(int B, int T, const void* meta, const int32_t* draft,
                                                           const int32_t* token, int32_t* accepted,
