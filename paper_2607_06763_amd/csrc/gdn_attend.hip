@@ -386,7 +386,7 @@ __device__ void add_not_finite(const AttnArgs& a, const MetaPtrs& m, int b, int 
 // registers (512 contiguous bytes per 32 lanes), ahead of their use.
 //
 // Bound by the bytes of the cache (32 x 1 token, 32 + 8 heads of 128 in bf16,
-// up to 8 k tokens: 656 MB in 117 us, 5.6 TB/s; a large copy reaches 5.1), with
+// up to 8 k tokens: 656 MB in 117 to 120 us, 5.5 TB/s; a large copy reaches 5.1), with
 // a short cache by the chain lengths - pages - keys - values - parts (10 us),
 // in fp32 by the products, which take 8 times those of bf16: 6 x 14 nodes,
 // 48 + 8 heads of 128, 9 k tokens 159 us, of which about 136 are products (a
@@ -669,8 +669,8 @@ __global__ __launch_bounds__(kThreads, (stream_groups<T, D>())) void attend_stre
 // with one; 16 x 16 nodes 62.8 and 58.9); at 256 one, with the registers of both.
 //
 // Bound by the matrix units at the clock that they leave: 32 + 8 heads of 128,
-// 16 x 128 nodes, up to 8 k tokens 177 GFLOP in 240 us with the join, 740
-// TFLOP/s (a large bf16 product reaches 1180).  A tile takes a pair of waves
+// 16 x 128 nodes, up to 8 k tokens 177 GFLOP in 229 us with the join, 774
+// TFLOP/s (a large bf16 product reaches 1120 to 1180).  A tile takes a pair of waves
 // 2600 clocks, 2048 of them products; the first tile and the outputs of a run
 // take as long as seven tiles, which is what bounds the short calls (27 x 90
 // nodes over 850 tokens 26 us).  Heads of 256, two chunks of 512 over 12 k

@@ -26,11 +26,13 @@ namespace {
 // Rows for which LDS is too small (thousands of equal logits) take the cuts by
 // halving the value.
 //
-// Bound by instructions, not bytes: a logit is read once or twice and costs 10
-// to 20 of them.  512 rows of 131072 in bf16, every kind of cut: 113 us, 1.2
-// TB/s of logits; 1056 rows of 50001 in fp32 with top_p: 112 us, 1.7 TB/s (a
-// third of the slots is padding).  One row of 131072: 21 us, four trips over a
-// chip's one workgroup.
+// Bound by the passes of a row in turn, not by bytes: under top_p a logit is
+// read three times at 10 to 20 instructions, with barriers and the bins'
+// bookkeeping between.  512 rows of 131072 in bf16, every kind of cut: 113 to
+// 117 us, 1.2 TB/s of logits (1.7 times these fetched, vector units 22 % busy);
+// 1056 rows of 50001 in fp32 with top_p: 112 to 121 us, 1.6 TB/s (padding slots,
+// up to a third of a tree, left out).  One row of 131072: 21 to 25 us, the
+// passes of one workgroup.
 // ---------------------------------------------------------------------------
 constexpr int kBins = 1024;
 constexpr float kBinsPerOctave = kBins / 32.0f;  // w is 0 beyond 32 octaves
@@ -868,6 +870,7 @@ int after_launch(const char* who) {
 // Threads for a row.  Between the passes over a row every wave takes part in
 // the same bookkeeping, so with many rows fewer waves a row are faster (4096
 // rows of 8000, top_k: 82 us with 256 threads, 142 and 282 with 512 and 1024),
+// but not yet for 1056 rows of 50001 (top_p and accept: 123 us with 512, 143 with 256),
 // with few rows more (one row of 131072, top_p: 117, 70, 59 us).  A short row
 // leaves many threads nothing to load.
 template <typename T>
