@@ -1235,45 +1235,4 @@ int launch_verify_noalloc(const VerifyArgs& a, hipStream_t stream) {
   return launch_large(a, ws, ord, stream);
 }
 
-// ---------------------------------------------------------------------------
-// Workspace of the T > 128 path: one device buffer per (device, stream),
-// grown on demand and kept until the process ends.
-// ---------------------------------------------------------------------------
-void* stream_workspace(size_t bytes, hipStream_t stream, int* rc) {
-  static std::mutex mu;
-  static std::map<std::pair<int, hipStream_t>, std::pair<void*, size_t>> bufs;
-  *rc = GDN_OK;
-  int dev = 0;
-  if (hipGetDevice(&dev) != hipSuccess) {
-    *rc = set_error(GDN_EHIP, "workspace: hipGetDevice failed");
-    return nullptr;
-  }
-  std::lock_guard<std::mutex> lock(mu);
-  auto& e = bufs[{dev, stream}];
-  if (e.second >= bytes) return e.first;
-  hipStreamCaptureStatus cs = hipStreamCaptureStatusNone;
-  if (hipStreamIsCapturing(stream, &cs) != hipSuccess || cs != hipStreamCaptureStatusNone) {
-    *rc = set_error(GDN_EUNSUPPORTED,
-                    "workspace: %zu bytes needed while the stream is captured; run the same sizes once "
-                    "uncaptured first",
-                    bytes);
-    return nullptr;
-  }
-  if (e.first) {  // only this stream used it
-    if (hipStreamSynchronize(stream) != hipSuccess || hipFree(e.first) != hipSuccess) {
-      *rc = set_error(GDN_EHIP, "workspace: release of %zu bytes failed", e.second);
-      return nullptr;
-    }
-    e.first = nullptr;
-    e.second = 0;
-  }
-  if (hipMalloc(&e.first, bytes) != hipSuccess) {
-    e.first = nullptr;
-    *rc = set_error(GDN_EHIP, "workspace: hipMalloc of %zu bytes failed", bytes);
-    return nullptr;
-  }
-  e.second = bytes;
-  return e.first;
-}
-
 }  // namespace gdn
