@@ -26,9 +26,18 @@
  * --------------------------------------
  *  * All tensor pointers are DEVICE pointers, contiguous row-major, owned by
  *    the caller.  Work is enqueued on the caller's stream and is ordered with
- *    it; nothing synchronises the host except a workspace allocation (trees
- *    above 128 slots, see gdn_tree_verify).  Pointers must be 16-byte
- *    aligned.
+ *    it; nothing synchronises the host except a workspace allocation (see
+ *    Workspaces below).  Pointers must be 16-byte aligned.
+ *  * Workspaces.  gdn_tree_verify and gdn_tree_step above 128 slots,
+ *    gdn_tree_verify_chunked and gdn_tree_attend pass intermediate results
+ *    through a device buffer that the library allocates on the first call that
+ *    needs it and keeps per (device, stream).  A call that needs more gets a
+ *    larger buffer (hipMalloc) in its place; one that was handed out is not
+ *    released before the process ends, so that a captured graph may go on
+ *    using it.  All buffers of a stream together stay below four times its
+ *    largest need.  A call under stream capture that would need a larger
+ *    buffer returns GDN_EUNSUPPORTED: run the same sizes once uncaptured on
+ *    that stream first.
  *  * Recurrence orientation: the stored state of (sequence b, value head h) is
  *    S[b][h] in R^{dv x dk} (dk contiguous), the transpose of the paper's
  *    S in R^{dk x dv}; one step is S <- alpha S (I - beta k k^T) + beta v k^T
@@ -137,10 +146,8 @@ int gdn_tree_prepare(const gdn_dims* dims, const int32_t* parent, void* meta,
  * 128 the post-conv features go through a device workspace of
  * B T (2 C + 4 Hv) bytes (fp16 features, fp32 scales of the value rows;
  * C = 2 Hk dk + Hv dv, the first part rounded up to 256 bytes) and 6 T bytes
- * per tree (its depth-first order, T rounded up to 16) that the
- * library allocates on the first call that needs it and keeps per
- * (device, stream) until the process ends (a call under stream capture that
- * would have to grow it returns GDN_EUNSUPPORTED).
+ * per tree (its depth-first order, T rounded up to 16) that the library
+ * keeps (see Workspaces above).
  *   meta        written by gdn_tree_prepare for the same B, T
  *   q, k        in_dtype [B][T][Hk][dk]   raw (pre-conv) queries / keys
  *   v           in_dtype [B][T][Hv][dv]   raw values
@@ -184,8 +191,8 @@ int gdn_tree_verify_noalloc(const gdn_dims* dims, const void* meta, const void* 
  * diagonal-block inverses on fp32 MFMA, features in fp32.  Arguments,
  * layouts, outputs and errors are those of gdn_tree_verify (any supported
  * dk, dv and T).  Needs a workspace of about B (T (C + Hv dv) + 1024 n (2 Hv +
- * (n - 1) Hk)) 4 bytes, n = ceil(T / 32), cached per (device, stream) like
- * gdn_tree_verify's above 128 slots (the pairs of blocks without an ancestor
+ * (n - 1) Hk)) 4 bytes, n = ceil(T / 32), which the library keeps (see
+ * Workspaces above; the pairs of blocks without an ancestor
  * have room in it, too).  Its cost grows with the pairs of 32-slot blocks of
  * which one holds an ancestor of a node of the other; gdn_tree_verify's up to
  * 128 slots with the sum of the path lengths, above with the number of 16-node
@@ -325,11 +332,10 @@ int gdn_kv_append(const gdn_attn_dims* dims, const void* meta, const int32_t* n_
  * Keys of a page whose entry is outside [0, n_pages) are left out.  A row of
  * a slot that is not visible to a query does not reach it, whatever it holds
  * (infinities and NaN included), nor do cache rows past the last slot.
- * Work is split over the cached length when there are few rows; the parts
- * are joined through a workspace that the library keeps per (device, stream)
- * as for gdn_tree_verify above 128 slots (a call under stream capture that
- * would have to grow it returns GDN_EUNSUPPORTED: run the same sizes once
- * uncaptured first). */
+ * Work is split over the cached length, at one token too; the parts are
+ * joined through a workspace that the library keeps (see Workspaces above),
+ * 2 S Hkv T (Hq / Hkv) (d + 2) 4 bytes for S splits: about 2 MB for one token
+ * and 68 MB for 16 trees of 128 slots, 32 + 8 heads of 128. */
 int gdn_tree_attend(const gdn_attn_dims* dims, const void* meta, const int32_t* n_new, const void* q,
                     const void* k_cache, const void* v_cache, const int32_t* page_table,
                     const int32_t* ctx_len, void* out, hipStream_t stream);

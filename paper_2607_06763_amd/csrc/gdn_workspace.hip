@@ -1,6 +1,6 @@
 // gdn_workspace.hip -- device memory that the library keeps for the kernels of
-// a call: one buffer per (device, stream), grown on demand and kept until the
-// process ends.
+// a call: one buffer per (device, stream), replaced by a larger one on demand;
+// none is released before the process ends.
 #include <map>
 #include <mutex>
 #include <utility>
@@ -29,21 +29,19 @@ void* stream_workspace(size_t bytes, hipStream_t stream, int* rc) {
                     bytes);
     return nullptr;
   }
-  if (e.first) {  // only this stream used it
-    if (hipStreamSynchronize(stream) != hipSuccess || hipFree(e.first) != hipSuccess) {
-      *rc = set_error(GDN_EHIP, "workspace: release of %zu bytes failed", e.second);
-      return nullptr;
-    }
-    e.first = nullptr;
-    e.second = 0;
-  }
-  if (hipMalloc(&e.first, bytes) != hipSuccess) {
-    e.first = nullptr;
+  // A captured graph keeps the address that its calls were given, so a buffer
+  // stays when a larger one takes its place.  Each is twice the one before, if
+  // there is room: all of them together stay below four times the largest need.
+  void* p = nullptr;
+  size_t size = bytes > 2 * e.second ? bytes : 2 * e.second;
+  hipError_t err = hipMalloc(&p, size);
+  if (err != hipSuccess && size > bytes) err = hipMalloc(&p, size = bytes);
+  if (err != hipSuccess) {
     *rc = set_error(GDN_EHIP, "workspace: hipMalloc of %zu bytes failed", bytes);
     return nullptr;
   }
-  e.second = bytes;
-  return e.first;
+  e = {p, size};
+  return p;
 }
 
 }  // namespace gdn
