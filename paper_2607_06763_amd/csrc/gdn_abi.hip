@@ -10,6 +10,7 @@
 #include <utility>
 
 #include "gdn_internal.h"
+#include "gdn_workspace.h"
 
 namespace gdn {
 
@@ -64,6 +65,7 @@ static int verify_any(const VerifyArgs& a, hipStream_t stream) {
   const size_t bytes =
       large_order_offset(large_workspace_bytes(a.B, a.T, a.Hk, a.Hv, a.dk, a.dv)) + large_order_bytes(a.B, a.T);
   int rc = GDN_OK;
+  const StreamOrder order(stream);
   void* ws = stream_workspace(bytes, stream, &rc);
   if (!ws) return rc;
   return launch_verify_large(a, ws, bytes, stream);
@@ -186,6 +188,7 @@ int gdn_tree_verify_chunked(const gdn_dims* dims, const void* meta, const void* 
   a.S0 = S0;
   a.out = out;
   const size_t bytes = chunked_workspace_bytes(a.B, a.T, a.Hk, a.Hv, a.dk, a.dv);
+  const StreamOrder order(stream);
   void* ws = stream_workspace(bytes, stream, &rc);
   if (!ws) return rc;
   return launch_verify_chunked(a, ws, bytes, stream);

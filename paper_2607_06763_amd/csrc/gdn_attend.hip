@@ -22,6 +22,7 @@
 #include <algorithm>
 
 #include "gdn_attn.h"
+#include "gdn_workspace.h"
 
 namespace gdn {
 namespace {
@@ -1098,6 +1099,7 @@ int launch_dim(const AttnArgs& a, hipStream_t stream) {
 }  // namespace
 
 int launch_attend(const AttnArgs& a, hipStream_t stream) {
+  const StreamOrder order(stream);  // the parts, then their join
   switch (a.c.d) {
     case 32: return launch_dim<32>(a, stream);
     case 64: return launch_dim<64>(a, stream);

@@ -365,7 +365,8 @@ inline size_t large_order_bytes(int B, int T) { return size_t(B) * 3 * large_ord
 int launch_verify_large(const VerifyArgs& a, void* ws, size_t ws_bytes, hipStream_t stream);
 // A device buffer of at least bytes for work on stream, cached per (device,
 // stream) and replaced by a larger one on demand (never while the stream is
-// being captured); one that was handed out is never released.
+// being captured); one that was handed out is never released.  The caller holds
+// the stream's StreamOrder (gdn_workspace.h).
 void* stream_workspace(size_t bytes, hipStream_t stream, int* rc);
 // gdn_tree_verify without any allocation: the workspace of T > 128 is the
 // library's static device array

@@ -1,6 +1,7 @@
 """The device buffers that the library keeps for the kernels of a call, on the
 host (no GPU): gdn_workspace.hip against a fake runtime, with AddressSanitizer
 and UndefinedBehaviorSanitizer."""
+import glob
 import os
 import shutil
 import subprocess
@@ -12,8 +13,9 @@ SAN = os.path.join(ROOT, "tests", "sanitize")
 CSRC = os.path.join(ROOT, "paper_2607_06763_amd", "csrc")
 HIPCC = os.environ.get("HIPCC", "/opt/rocm/bin/hipcc")
 CLANGXX = "/opt/rocm/llvm/bin/clang++"
+NM = shutil.which("nm")
 
-pytestmark = pytest.mark.skipif(not (shutil.which(HIPCC) and shutil.which(CLANGXX)), reason="needs hipcc")
+pytestmark = pytest.mark.skipif(not (shutil.which(HIPCC) and shutil.which(CLANGXX) and NM), reason="needs hipcc and nm")
 
 
 def run_driver(tmp_path, driver, sources):
@@ -37,3 +39,22 @@ def run_driver(tmp_path, driver, sources):
 
 def test_buffers_that_were_handed_out_stay(tmp_path):
     run_driver(tmp_path, "workspace_driver.cpp", ["gdn_workspace.hip"])
+
+
+def test_calls_of_two_threads_on_one_stream(tmp_path):
+    """The whole library's host side: kernels that share a stream's workspace are enqueued call by call."""
+    objs = []
+    flags = ["--offload-arch=gfx950", "--offload-host-only", "-O0", "-std=c++17", "-I", os.path.join(ROOT, "include"), "-I", CSRC]
+    for src in [os.path.join(SAN, "threads_driver.cpp"), *glob.glob(os.path.join(CSRC, "*.hip"))]:
+        objs.append(str(tmp_path / (os.path.basename(src) + ".o")))
+        r = subprocess.run([HIPCC, *flags, "-c", "-x", "hip", src, "-o", objs[-1]], capture_output=True, text=True, timeout=300)
+        assert r.returncode == 0, r.stderr
+    # the device code that the host side names: there is none here
+    r = subprocess.run([NM, "-u", *objs], capture_output=True, text=True, timeout=60)
+    absent = sorted({w for w in r.stdout.split() if w.startswith("__hip_fatbin")})
+    exe = str(tmp_path / "driver")
+    r = subprocess.run([CLANGXX, *objs, *(f"-Wl,--defsym={s}=0" for s in absent), "-lpthread", "-o", exe],
+                       capture_output=True, text=True, timeout=300)
+    assert r.returncode == 0, r.stderr
+    r = subprocess.run([exe], capture_output=True, text=True, timeout=120)
+    assert r.returncode == 0 and "0 failed checks" in r.stdout, r.stdout + r.stderr
