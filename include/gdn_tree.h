@@ -39,6 +39,7 @@
  *    buffer returns GDN_EUNSUPPORTED: run the same sizes once uncaptured on
  *    that stream first.  Several host threads may make calls on one stream:
  *    the kernels of each such call are enqueued together.
+ *    hipStreamPerThread has a buffer for every thread that uses it.
  *  * Recurrence orientation: the stored state of (sequence b, value head h) is
  *    S[b][h] in R^{dv x dk} (dk contiguous), the transpose of the paper's
  *    S in R^{dk x dv}; one step is S <- alpha S (I - beta k k^T) + beta v k^T

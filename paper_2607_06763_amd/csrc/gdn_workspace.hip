@@ -6,12 +6,13 @@
 #include <utility>
 
 #include "gdn_internal.h"
+#include "gdn_workspace.h"
 
 namespace gdn {
 
 void* stream_workspace(size_t bytes, hipStream_t stream, int* rc) {
   static std::mutex mu;
-  static std::map<std::pair<int, hipStream_t>, std::pair<void*, size_t>> bufs;
+  static std::map<std::pair<int, StreamKey>, std::pair<void*, size_t>> bufs;
   *rc = GDN_OK;
   int dev = 0;
   if (hipGetDevice(&dev) != hipSuccess) {
@@ -19,7 +20,7 @@ void* stream_workspace(size_t bytes, hipStream_t stream, int* rc) {
     return nullptr;
   }
   std::lock_guard<std::mutex> lock(mu);
-  auto& e = bufs[{dev, stream}];
+  auto& e = bufs[{dev, stream_key(stream)}];
   if (e.second >= bytes) return e.first;
   hipStreamCaptureStatus cs = hipStreamCaptureStatusNone;
   if (hipStreamIsCapturing(stream, &cs) != hipSuccess || cs != hipStreamCaptureStatusNone) {

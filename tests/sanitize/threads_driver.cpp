@@ -125,6 +125,8 @@ int main() {
   // calls on two streams do not wait for each other
   both([&] { return calls[0](streams[1]); }, [&] { return calls[0](streams[2]); });
   CHECK(g_met);
+  both([&] { return calls[0](hipStreamPerThread); }, [&] { return calls[0](hipStreamPerThread); });  // two streams
+  CHECK(g_met);
   printf("threads driver: %d failed checks\n", fails);
   return fails != 0;
 }

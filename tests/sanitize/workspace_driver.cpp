@@ -9,6 +9,7 @@
 #include <stdlib.h>
 #include <string.h>
 
+#include <thread>
 #include <vector>
 
 #include "gdn_internal.h"
@@ -120,11 +121,21 @@ static void out_of_memory() {
   g_limit = SIZE_MAX;
 }
 
+// hipStreamPerThread names another stream in every host thread.
+static void streams_per_thread() {
+  void *a = get(100, hipStreamPerThread), *b = nullptr, *c = nullptr;
+  std::thread([&] { b = get(100, hipStreamPerThread); }).join();
+  std::thread([&] { c = get(100, hipStreamPerThread); }).join();  // kernels of the ended thread's may still run
+  CHECK(a != b && a != c && b != c);
+  CHECK(a == get(100, hipStreamPerThread));
+}
+
 int main() {
   buffers_stay();
   streams_and_devices_apart();
   capture();
   out_of_memory();
+  streams_per_thread();
   printf("workspace driver: %d failed checks\n", fails);
   return fails != 0;
 }
