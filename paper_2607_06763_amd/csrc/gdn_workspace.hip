@@ -24,6 +24,7 @@ void* stream_workspace(size_t bytes, hipStream_t stream, int* rc) {
   if (e.second >= bytes) return e.first;
   hipStreamCaptureStatus cs = hipStreamCaptureStatusNone;
   if (hipStreamIsCapturing(stream, &cs) != hipSuccess || cs != hipStreamCaptureStatusNone) {
+    (void)hipGetLastError();
     *rc = set_error(GDN_EUNSUPPORTED,
                     "workspace: %zu bytes needed while the stream is captured; run the same sizes once "
                     "uncaptured first",
@@ -36,8 +37,10 @@ void* stream_workspace(size_t bytes, hipStream_t stream, int* rc) {
   void* p = nullptr;
   size_t size = bytes > 2 * e.second ? bytes : 2 * e.second;
   hipError_t err = hipMalloc(&p, size);
+  if (err != hipSuccess) (void)hipGetLastError();  // or the next launch's check reports it
   if (err != hipSuccess && size > bytes) err = hipMalloc(&p, size = bytes);
   if (err != hipSuccess) {
+    (void)hipGetLastError();
     *rc = set_error(GDN_EHIP, "workspace: hipMalloc of %zu bytes failed", bytes);
     return nullptr;
   }

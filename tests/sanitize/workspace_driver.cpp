@@ -28,6 +28,7 @@ static int fails = 0;
 // ---------------------------------------------------------------------------
 static int g_device = 0;
 static bool g_capturing = false;
+static hipError_t g_last = hipSuccess;
 static size_t g_held = 0;          // bytes allocated
 static size_t g_limit = SIZE_MAX;  // bytes that there are
 
@@ -38,13 +39,16 @@ hipError_t hipStreamIsCapturing(hipStream_t, hipStreamCaptureStatus* s) {
 }
 hipError_t hipStreamSynchronize(hipStream_t) { return hipSuccess; }
 hipError_t hipMalloc(void** p, size_t n) {
-  if (n > g_limit - g_held) return hipErrorOutOfMemory;
+  if (n > g_limit - g_held) return g_last = hipErrorOutOfMemory;
   g_held += n;
   *p = malloc(n);
   return hipSuccess;
 }
 hipError_t hipFree(void* p) { return free(p), hipSuccess; }
-hipError_t hipGetLastError(void) { return hipSuccess; }
+hipError_t hipGetLastError(void) {
+  const hipError_t e = g_last;
+  return g_last = hipSuccess, e;
+}
 }
 
 namespace gdn {
@@ -114,7 +118,9 @@ static void out_of_memory() {
   g_limit = g_held + (3 << 15);
   // no room for more than is asked for: as much as that
   void* b = get(3 << 15, stream(6));
+  CHECK(g_last == hipSuccess);  // the next launch's check would report what is left
   CHECK(!stream_workspace(1 << 20, stream(6), &rc) && rc == GDN_EHIP);
+  CHECK(g_last == hipSuccess);
   CHECK(get(3 << 15, stream(6)) == b);  // what is there stays in use
   memset(a, 1, 1 << 16);
   memset(b, 1, 3 << 15);
