@@ -40,6 +40,10 @@
  *    that stream first.  Several host threads may make calls on one stream:
  *    the kernels of each such call are enqueued together.
  *    hipStreamPerThread has a buffer for every thread that uses it.
+ *    A captured graph works in the buffer of the stream it was captured on,
+ *    whichever stream replays it: it must not run at the same time as other
+ *    such calls of that stream, or as another graph captured there.  Graphs
+ *    that are to run side by side are captured on streams of their own.
  *  * Recurrence orientation: the stored state of (sequence b, value head h) is
  *    S[b][h] in R^{dv x dk} (dk contiguous), the transpose of the paper's
  *    S in R^{dk x dv}; one step is S <- alpha S (I - beta k k^T) + beta v k^T

@@ -10,6 +10,11 @@ A decode step of a model that has both kinds of layers::
     A.sample(logits, u, token, temperature=t, top_p=p, meta=meta)             # once per step
     A.accept(draft, token, accepted, n_emitted, emitted, meta=meta)
     A.kv_commit(d, accepted, table, ctx_len, kc, vc, new_len, meta=meta)      # attention layers
+
+``attend`` works in a buffer that the library keeps per stream (the header's
+"Workspaces"): before a capture the same sizes run once uncaptured on the
+capture stream, and a graph must not run at the same time as other calls of
+that stream, or as another graph captured there.
 """
 from __future__ import annotations
 
