@@ -670,7 +670,8 @@ __global__ __launch_bounds__(NT, 4) void sample_kernel(SampleArgs a) {
     for (int w = 0; w < NT / kWave; ++w) low = fminf(low, s.redf[w]);
     if (n >= u64(o.k)) floor = low;  // else fewer than k threads have any logit
   } else if (!o.use_k && !o.use_p && o.use_m) {
-    const float down = (log2f(fminf(o.least, 1.0f)) - 0.01f) / c;
+    // a mass that rounds to thr may be up to a half below it
+    const float down = (log2f(float(o.thr) - 0.5f) - 31.0f - 0.01f) / c;
     floor = fmaxf(-3.4028235e38f, top + down - 1e-6f * (fabsf(top) + fabsf(down)));
   }
   bool listed = floor > -INFINITY;
