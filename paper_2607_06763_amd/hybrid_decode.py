@@ -81,8 +81,8 @@ class HybridModel:
 
 class Decoder:
     """B sequences, draft trees of up to T slots.  Every sequence has
-    max_pages pages of the caches to itself; u float32 [B][positions] holds
-    the random number of each position."""
+    max_pages pages of the caches to itself; u float32 [B][n] holds the random
+    number of each position, for sequences of up to n tokens."""
 
     def __init__(self, model: HybridModel, B: int, T: int, u: np.ndarray, max_pages: int = 32, page: int = 16,
                  dtype: str = "f32", temperature=None, top_k=None, top_p=None, min_p=None, device="cuda"):
@@ -99,11 +99,14 @@ class Decoder:
         row = lambda x, t: None if x is None else up(np.broadcast_to(x, (B,)), t)
         self.sampling = dict(temperature=row(temperature, torch.float32), top_k=row(top_k, torch.int32),
                              top_p=row(top_p, torch.float32), min_p=row(min_p, torch.float32))
+        if np.ndim(u) != 2 or len(u) != B:
+            raise ValueError(f"u: shape {np.shape(u)}, expected [{B}][positions]")
         self.u = up(u, torch.float32)
         # pages in an order of their own, as an allocator would hand them out
         order = np.random.default_rng(B * max_pages).permutation(B * max_pages)
         self.table = up(order.reshape(B, max_pages), torch.int32)
         self.ctx_len = torch.zeros(B, dtype=torch.int32, device=device)
+        self.lengths = np.zeros(B, np.int64)  # the same on the host
         kc, vc = A.cache_shapes(self._attn(T))
         C = 2 * model.Hk * model.dk + model.Hv * model.dv
         zeros = lambda *s, t=torch.float32: torch.zeros(*s, dtype=t, device=device)
@@ -192,6 +195,7 @@ class Decoder:
             _, _, st = self._layers(torch.from_numpy(tok).to(self.device), meta, lengths, gdn)
             self._check(statuses + st, "prompt")
             self.ctx_len = self.ctx_len + lengths
+            self.lengths += n
 
     def step(self, trees: List[D.Tree]) -> List[List[int]]:
         """One step: the tokens that each sequence emits, given its draft tree (root: the last emitted token)."""
@@ -202,6 +206,8 @@ class Decoder:
             parent[b, :n], tok[b, :n] = t.parent, t.tokens
             for s in range(1, n):
                 depth[b, s] = depth[b, t.parent[s]] + 1
+            if n and self.lengths[b] + depth[b].max() + 1 >= self.u.shape[1]:
+                raise ValueError(f"step: no random number for position {self.lengths[b] + depth[b].max() + 1} of sequence {b}")
         d, i32 = self._gdn(T), torch.int32
         dev = lambda a: torch.from_numpy(a).to(self.device)
         new = lambda *s: torch.empty(*s, dtype=i32, device=self.device)
@@ -224,7 +230,7 @@ class Decoder:
 
         x, inputs, st = self._layers(draft, meta, None, gdn)
         logits = self._norm(x) @ self.unembed
-        # the number of the position after a node's
+        # the number of the position after a node's (that of an absent slot is not used)
         u = torch.gather(self.u, 1, (self.ctx_len.long()[:, None] + dev(depth) + 1).clamp_max(self.u.shape[1] - 1))
         token, accepted, n_emitted, emitted = new(B, T), new(B), new(B), new(B, T)
         A.sample(logits.contiguous(), u, token, meta=meta, **self.sampling)
@@ -239,6 +245,7 @@ class Decoder:
         self.ctx_len = new_len if "attn" in m.kinds else self.ctx_len + n_emitted
         self.last = (meta, accepted, inputs)
         rows, n = emitted.cpu().numpy(), n_emitted.cpu().numpy()
+        self.lengths += n
         return [[int(t) for t in rows[b, :n[b]]] for b in range(B)]
 
 
