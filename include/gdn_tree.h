@@ -412,8 +412,9 @@ int gdn_tree_sample(const gdn_sample_dims* dims, const void* meta, const void* l
  *              empty tree or one with a non-zero status
  *   n_emitted  int32 [B]     written: depth(accepted) + 1
  *   emitted    int32 [B][T]  written: the tokens below the root, then the one
- *              sampled at the accepted node, then -1; must not overlap draft
- *              or token
+ *              sampled at the accepted node (-1 if it has none; n_emitted
+ *              counts it all the same), then -1; must not overlap draft or
+ *              token
  * A negative token matches no draft. */
 int gdn_tree_accept(const gdn_dims* dims, const void* meta, const int32_t* draft,
                     const int32_t* token, int32_t* accepted, int32_t* n_emitted, int32_t* emitted,

@@ -246,6 +246,9 @@ class Decoder:
         self.last = (meta, accepted, inputs)
         rows, n = emitted.cpu().numpy(), n_emitted.cpu().numpy()
         self.lengths += n
+        for b in range(B):
+            if n[b] and rows[b, n[b] - 1] < 0:
+                raise RuntimeError(f"step: no token for sequence {b}: none of its logits is above -inf")
         return [[int(t) for t in rows[b, :n[b]]] for b in range(B)]
 
 
