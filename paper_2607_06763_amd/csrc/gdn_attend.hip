@@ -49,6 +49,9 @@ struct Mat<BF16> {
   }
   // key of row m: bits 2 and 3 traded
   static __device__ __forceinline__ int key_of(int m) { return (m & 0x13) | ((m & 4) << 1) | ((m & 8) >> 1); }
+  // weights as the second product's operand: bf16, as the instruction takes them
+  // (at most 2^-8 of each; sums and maxima stay in 32 bits).  Outputs are off by
+  // 0.0023 of their norm, 0.0017 of it from their own rounding.
   static __device__ __forceinline__ Frag pack(const float* p) {
     Frag f;
 #pragma unroll
@@ -389,10 +392,15 @@ __device__ void add_not_finite(const AttnArgs& a, const MetaPtrs& m, int b, int 
 // Bound by the bytes of the cache (32 x 1 token, 32 + 8 heads of 128 in bf16,
 // up to 8 k tokens: 656 MB in 117 to 120 us, 5.5 TB/s; a large copy reaches 5.1), with
 // a short cache by the chain lengths - pages - keys - values - parts (10 us),
-// in fp32 by the products, which take 8 times those of bf16: 6 x 14 nodes,
+// in fp32 by the products, which take 16 times those of bf16: 6 x 14 nodes,
 // 48 + 8 heads of 128, 9 k tokens 159 us, of which about 136 are products (a
 // quarter on rows that fill up the tiles); 8 x 99 nodes, 16 + 4 heads of 64,
-// 1 k tokens 45 us, 27 of them products.
+// 1 k tokens 45 us, of which the products (2.6 GFLOP with the rows that fill up
+// the tiles) take 17 at the matrix units' rate and the join 6: a run is 5 or 6
+// key tiles behind the chain.  32 x 1 token in fp32: 1312 MB in 245 us.
+//
+// Scalar registers spill into lanes of vector registers (up to 121 of them);
+// to memory only fp32 heads of 256 do, two registers.
 // ---------------------------------------------------------------------------
 constexpr int kThreads = 256;
 constexpr int kWaves = kThreads / kWave;
@@ -669,13 +677,17 @@ __global__ __launch_bounds__(kThreads, (stream_groups<T, D>())) void attend_stre
 // Up to d = 128 two workgroups a CU (16 x 128 nodes over 8 k tokens 240 us, 299
 // with one; 16 x 16 nodes 62.8 and 58.9); at 256 one, with the registers of both.
 //
-// Bound by the matrix units at the clock that they leave: 32 + 8 heads of 128,
-// 16 x 128 nodes, up to 8 k tokens 177 GFLOP in 229 us with the join, 774
-// TFLOP/s (a large bf16 product reaches 1120 to 1180).  A tile takes a pair of waves
-// 2600 clocks, 2048 of them products; the first tile and the outputs of a run
-// take as long as seven tiles, which is what bounds the short calls (27 x 90
-// nodes over 850 tokens 26 us).  Heads of 256, two chunks of 512 over 12 k
-// tokens: 156 GFLOP in 228 us.
+// 32 + 8 heads of 128, 16 x 128 nodes, up to 8 k tokens: 177 GFLOP in 239 to
+// 255 us with the join (20), 690 to 740 TFLOP/s; a large bf16 product reaches
+// 1270.  The matrix units are busy 39 % of the time and the vector units 44 %
+// (counters), so neither bounds it alone: a tile takes the two waves of a SIMD
+// 5300 clocks, 2048 of them products.  Each product has an operand read of its
+// own from LDS, 1 KB (5.6 M of each), because a wave holds 32 rows: products
+// without a pause on all four SIMDs would take the 128 bytes a clock that LDS
+// gives, before the tiles' own way into it.  The first tile and the outputs of a
+// run are not overlapped, which is what the short calls wait for (27 x 90 nodes
+// over 850 tokens 26 us).  Heads of 256, two chunks of 512 over 12 k tokens: 156
+// GFLOP in 228 to 235 us, one wave a SIMD, matrix units 27 % busy.
 // ---------------------------------------------------------------------------
 template <int D>
 struct Tile {

@@ -41,9 +41,10 @@ __device__ __forceinline__ void turn(u32x4& x, u32x4& y, const float2* cs) {
 // Workgroups of queries hold a share of 8 slots' (head, pack) units; those of
 // keys and values hold a group of 8 positions (one value pack in bf16, two in
 // fp32), so that a value pack whose 8 tokens are all new is written whole.
-// Bound by bytes, and by the chain in front of them (length and depths, then
-// pages and angles): the queries, most of the bytes, are on their way before
-// it.  32 x 128 slots, 24 + 4 heads of 256, cold caches: 44 to 49 us for 120 MB
+// Bound by the chain in front of the bytes (length and depths, then pages and
+// angles), which every workgroup goes through; the queries, most of the bytes,
+// are on their way before it.  32 x 128 slots, 24 + 4 heads of 256, cold caches:
+// 44 to 50 us for 120 MB, 58 for the 238 MB of fp32
 // (64 with every load behind the checks, 50 with ordinary loads where this
 // took 44; non-temporal stores took 42, but the rows are read again by the
 // attention).  One token: 5 us, the chain.

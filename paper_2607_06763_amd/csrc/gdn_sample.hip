@@ -29,10 +29,14 @@ namespace {
 // Bound by the passes of a row in turn, not by bytes: under top_p a logit is
 // read three times at 10 to 20 instructions, with barriers and the bins'
 // bookkeeping between.  512 rows of 131072 in bf16, every kind of cut: 113 to
-// 117 us, 1.2 TB/s of logits (1.7 times these fetched, vector units 22 % busy);
+// 117 us, 1.2 TB/s of logits (1.7 times these fetched, vector units 22 % busy: one
+// round of workgroups, in which greedy and min_p rows leave their places empty);
 // 1056 rows of 50001 in fp32 with top_p: 112 to 121 us, 1.6 TB/s (padding slots,
 // up to a third of a tree, left out).  One row of 131072: 21 to 25 us, the
 // passes of one workgroup.
+//
+// The kernel is held to 128 registers, for 16 waves a CU: in fp32 8 to 12 of
+// them spill to memory, in bf16 5 with 1024 threads and none with fewer.
 // ---------------------------------------------------------------------------
 constexpr int kBins = 1024;
 constexpr float kBinsPerOctave = kBins / 32.0f;  // w is 0 beyond 32 octaves
@@ -869,11 +873,18 @@ int after_launch(const char* who) {
 }  // namespace
 
 // Threads for a row.  Between the passes over a row every wave takes part in
-// the same bookkeeping, so with many rows fewer waves a row are faster (4096
-// rows of 8000, top_k: 82 us with 256 threads, 142 and 282 with 512 and 1024),
-// but not yet for 1056 rows of 50001 (top_p and accept: 123 us with 512, 143 with 256),
-// with few rows more (one row of 131072, top_p: 117, 70, 59 us).  A short row
-// leaves many threads nothing to load.
+// the same bookkeeping, so with many rows fewer waves a row are faster.  In us
+// with 256 / 512 / 1024 threads, without the acceptance:
+//   one row of 131072 in fp32, top_p            104 /  62 /  55
+//   256 rows of 131072 in bf16, top_p           124 /  78 /  72
+//   528 rows of 131072 in bf16, top_p           209 / 172 / 170
+//   1056 rows of 50001 in fp32, top_p           145 / 131 / 173
+//   2048 rows of 17000 in bf16, top_p            77 / 108 / 211
+//   2048 rows of 17000 in fp32, top_k            60 /  79 / 144
+//   4096 rows of 33000 in bf16, top_p           204 / 275 / 513
+//   4096 rows of 8000 in fp32, top_k             72 / 127 / 269
+// From 2048 rows on only rows of 65000 in fp32 do better with 512 (287 and 268).
+// A short row leaves many threads nothing to load: one of 8000 takes 15 / 14 / 17.
 template <typename T>
 static int launch_type(const SampleArgs& a, hipStream_t stream) {
   const long long rows = (long long)(a.B) * a.T, vectors = a.V / Pack<T>::kN;
