@@ -34,10 +34,11 @@
  *    needs it and keeps per (device, stream).  A call that needs more gets a
  *    larger buffer (hipMalloc) in its place; one that was handed out is not
  *    released before the process ends, so that a captured graph may go on
- *    using it.  All buffers of a stream together stay below four times its
- *    largest need.  A call under stream capture that would need a larger
- *    buffer returns GDN_EUNSUPPORTED: run the same sizes once uncaptured on
- *    that stream first.  Several host threads may make calls on one stream:
+ *    using it.  Each is at least twice the one before if memory allows, so
+ *    that all buffers of a stream together stay below four times its largest
+ *    need.  A call under stream capture that would need a larger buffer
+ *    returns GDN_EUNSUPPORTED: run the same sizes once uncaptured on that
+ *    stream first.  Several host threads may make calls on one stream:
  *    the kernels of each such call are enqueued together.
  *    hipStreamPerThread has a buffer for every thread that uses it.
  *    A captured graph works in the buffer of the stream it was captured on,
