@@ -99,7 +99,8 @@ enum {
   GDN_TREE_BAD_ACCEPTED = 5, /* commit only: accepted outside [-1,T) or padding */
   GDN_KV_BAD_LEN = 6,  /* paged cache: ctx_len or n_new out of range, or no room in the page table */
   GDN_KV_BAD_PAGE = 7, /* paged cache: a needed page-table entry outside [0, n_pages) */
-  GDN_KV_BAD_POS = 8   /* paged cache: a position without a row in the rotation table */
+  GDN_KV_BAD_POS = 8,  /* paged cache: a position without a row in the rotation table */
+  GDN_CHAIN_BAD_LEN = 9 /* chain: a length outside [0, T], or rows outside the tensors */
 };
 
 /* Problem sizes.  B sequences, T node slots per tree (padded tree size),
@@ -420,6 +421,120 @@ int gdn_tree_sample(const gdn_sample_dims* dims, const void* meta, const void* l
 int gdn_tree_accept(const gdn_dims* dims, const void* meta, const int32_t* draft,
                     const int32_t* token, int32_t* accepted, int32_t* n_emitted, int32_t* emitted,
                     hipStream_t stream);
+
+/* ------------------------------------------------------------------------
+ * Layers without draft trees: sequences of any length through the gated
+ * delta rule, and the norms around a block
+ *
+ * gdn_chain takes whole sequences (prompts, single tokens) through one GDN
+ * layer: outputs of every token, the state and the conv state behind the last
+ * one, in one call.  gdn_gate_norm norms and gates its outputs head by head,
+ * gdn_add_norm adds a block's result to the residual stream and norms that
+ * for the next block. */
+
+/* Rows of a call: sequence b has tokens in rows
+ *   padded (start NULL)  b T .. b T + n_new[b] - 1   (n_new NULL: T of them)
+ *   packed               start[b] .. start[b + 1] - 1
+ * of q, k, v, alpha, beta and out, whose other rows are neither read nor
+ * written. */
+typedef struct {
+  int32_t B, T;      /* sequences, the most tokens of one (<= GDN_MAX_CHAIN_T)   */
+  int32_t Hk, Hv;    /* key and value heads, Hv % Hk == 0                        */
+  int32_t dk, dv;    /* 16, 32, 64 or 128                                        */
+  int32_t in_dtype;  /* q, k, v, alpha, beta: GDN_F32 or GDN_BF16                */
+  int32_t out_dtype; /* out: GDN_F32 or GDN_BF16                                 */
+  int64_t rows;      /* packed: rows of the tensors; not read otherwise (B T)    */
+  float scale;       /* of the readout; 0 selects 1 / sqrt(dk)                   */
+} gdn_chain_dims;
+
+#define GDN_MAX_CHAIN_T (1 << 24)
+
+/* The gated delta rule over sequences (Eq. 7-8 along a chain of any length),
+ * with the short convolution, activation and norms of gdn_tree_verify.
+ *   start      int32 [B + 1] or NULL (padded), see above; not with n_new
+ *   n_new      int32 [B] or NULL
+ *   q, k, v, alpha, beta   in_dtype [rows][Hk][dk], [rows][Hk][dk],
+ *              [rows][Hv][dv], [rows][Hv], [rows][Hv]
+ *   conv_w     fp32 [C][4], C = 2 Hk dk + Hv dv
+ *   conv_state fp32 [B][3][C]   read-only: raw inputs before the first token
+ *   conv_state_out  fp32 [B][3][C]  written: those before the next token; must
+ *              not overlap conv_state
+ *   S          fp32 [B][Hv][dv][dk]  in/out
+ *   out        out_dtype [rows][Hv][dv]  written: o_t = scale S_t q_t; must not
+ *              overlap an input
+ *   status     int32 [B] (may be NULL): GDN_CHAIN_BAD_LEN for a sequence whose
+ *              length is negative or above T, or whose rows are outside
+ *              [0, rows); 0 otherwise
+ * A sequence without tokens, or with a non-zero status, keeps S and gets
+ * conv_state_out = conv_state.  A decay below the smallest normal float counts
+ * as that in the chunked form.
+ * Short sequences (T <= GDN_CHAIN_STEP_T) go token by token with the state in
+ * registers and need no workspace.  Longer ones go in chunks of 64 tokens, all
+ * products in 32 bits (fp16 pairs, three products, fp32 sums), through a
+ * workspace that the library keeps (see Workspaces above), at most
+ * GDN_CHAIN_WORKSPACE bytes or what one chunk of one sequence needs:
+ * a chunk takes about Hk 512 dk + Hv (256 dk + 256 dv + 13312) bytes
+ * (dk, dv rounded up to 32 and 16). */
+#define GDN_CHAIN_STEP_T 16
+#define GDN_CHAIN_WORKSPACE (1u << 29)
+int gdn_chain(const gdn_chain_dims* dims, const int32_t* start, const int32_t* n_new, const void* q,
+              const void* k, const void* v, const void* alpha, const void* beta,
+              const float* conv_w, const float* conv_state, float* conv_state_out, float* S,
+              void* out, int32_t* status, hipStream_t stream);
+
+typedef enum { GDN_SILU = 0, GDN_SIGMOID = 1 } gdn_act;
+
+/* Problem sizes of gdn_gate_norm: N rows of H heads of d channels.  ldx, ldg:
+ * elements from one row of x (of gate) to the next, 0 selects H d. */
+typedef struct {
+  int64_t N;
+  int32_t H, d; /* 1 <= d <= GDN_MAX_NORM_D, H d <= GDN_MAX_ROW       */
+  int32_t x_dtype, gate_dtype, out_dtype;
+  int32_t act; /* GDN_SILU or GDN_SIGMOID                              */
+  int64_t ldx, ldg;
+  float eps; /* positive and not subnormal                             */
+} gdn_gate_norm_dims;
+
+#define GDN_MAX_NORM_D 16384
+#define GDN_MAX_ROW (1 << 24)
+
+/* Norm of every head, times a gate:
+ *   out[n][h] = x[n][h] / sqrt(mean(x[n][h]^2) + eps) * weight * act(gate[n][h])
+ *   x       x_dtype [N][ldx]
+ *   gate    gate_dtype [N][ldg], or NULL: no gate
+ *   weight  fp32 [d], or NULL: 1
+ *   out     out_dtype [N][H d]  written; may be x itself where types and rows
+ *           are the same (any other overlap is not allowed)
+ * These pointers need the alignment of their elements only; rows that all
+ * begin at multiples of 16 bytes, d a multiple of 8, are read in whole packs.
+ * In 32 bits: the squares of a head have to sum to less than 2^128. */
+int gdn_gate_norm(const gdn_gate_norm_dims* dims, const void* x, const void* gate,
+                  const float* weight, void* out, hipStream_t stream);
+
+/* Problem sizes of gdn_add_norm: N contiguous rows of D channels. */
+typedef struct {
+  int64_t N;
+  int32_t D; /* 1 <= D <= GDN_MAX_NORM_D                               */
+  int32_t x_dtype, res_dtype, out_dtype;
+  int32_t post; /* non-zero: x is normed before it is added            */
+  float eps;    /* positive and not subnormal                          */
+} gdn_add_norm_dims;
+
+/* The residual stream from one block to the next:
+ *   y = x, or with post  x / sqrt(mean(x^2) + eps) * post_weight
+ *   r = residual + scale * y             (written to res_out)
+ *   out = r / sqrt(mean(r^2) + eps) * weight     (of r before it is rounded)
+ *   x            x_dtype [N][D]
+ *   residual     res_dtype [N][D], or NULL: 0
+ *   weight, post_weight, scale   fp32 [D], or NULL: 1
+ *   res_out      res_dtype [N][D], or NULL; may be residual itself
+ *   out          out_dtype [N][D], or NULL (one of the two is needed); may be
+ *                x itself where their types are the same
+ * Any other overlap of an output is not allowed.  Alignment and range as for
+ * gdn_gate_norm. */
+int gdn_add_norm(const gdn_add_norm_dims* dims, const void* x, const void* residual,
+                 const float* weight, const float* post_weight, const float* scale, void* res_out,
+                 void* out, hipStream_t stream);
 
 /* Message describing the last non-OK return on the calling thread. */
 const char* gdn_last_error(void);

@@ -1,0 +1,738 @@
+// gdn_chain_chunk.hip -- the gated delta rule in chunks of 64 tokens, for
+// sequences of any length.
+//
+// Inside a chunk, with g_i the sum of log(alpha) up to token i and S0 the state
+// before it,
+//   (I + A) [U | W] = diag(beta) [V | diag(e^g) K],  A_ij = beta_i k_i.k_j e^(g_i - g_j), j < i
+//   V' = U - W S0^T,   O = scale (diag(e^g) Q S0^T + Y V'),  Y_ij = q_i.k_j e^(g_i - g_j), j <= i
+//   S  = e^g_last S0 + V'^T diag(e^(g_last - g)) K.
+// Everything but V', O and S is independent of the state, and is computed for
+// many chunks at once (chunk_kernel); the rest goes chunk by chunk
+// (scan_kernel), with the state in registers: a wave holds 16 value channels,
+// the columns of its matrix tiles, and needs nothing from the other waves.
+//
+// Products.  The outputs have 32-bit accuracy, so each operand is a pair of fp16
+// values, hi + lo, 22 bits together, and a product is three on the matrix units
+// (hi hi, hi lo, lo hi) with 32-bit sums: 2^-22 of an operand is lost.  Scales are powers of
+// two, exact: 2^10 for what is at most 1 (unit keys, queries, Y), else by the
+// largest value of the operand's row or column.
+//
+// Operand order.  A tile's accumulators hold rows 4 q + r (q = lane / 16) of
+// column lane % 16, and an operand 8 values of one row or column.  Two tiles of
+// 16 rows are taken as the 32 products of a step in the order
+// 16 (j / 4) + 4 q + j % 4 (slot 8 q + j), so that accumulators become
+// operands without leaving their lane; what multiplies them is stored in that
+// order.  (I + A) is inverted in blocks of 16, each by substitution.
+#include <algorithm>
+
+#include "gdn_layer.h"
+#include "gdn_workspace.h"
+
+namespace gdn {
+namespace {
+
+typedef _Float16 f16x4 __attribute__((ext_vector_type(4)));
+
+constexpr int kC = 64;          // tokens of a chunk
+constexpr int kPrepThreads = 512;
+constexpr int kPrepWaves = kPrepThreads / kWave;
+constexpr int kHeads = 3;       // value heads that are inverted at once
+constexpr int kLd = kC + 4;     // floats of a row of a chunk's matrix in LDS
+constexpr float kUnit = 1024.0f;  // scale of what is at most 1
+constexpr int kFrag = 1024;     // bytes of an operand tile: 64 lanes of 8 fp16 values
+
+// ---------------------------------------------------------------------------
+// Workspace of a slot (a chunk of a sequence).  Operand tiles of a pair: hi,
+// then lo.
+// ---------------------------------------------------------------------------
+__host__ __device__ constexpr int padded_dk(int dk) { return dk < 32 ? 32 : dk; }
+
+struct SlotLayout {
+  int ks;        // steps of 32 key channels
+  size_t key;    // bytes of a key head: Q [ks][4 token tiles], K^T [2 ks][2 token steps]
+  size_t value;  // of a value head: W [ks][4], Y [6], scalars, U [dv / 16][4] (fp32 accumulators)
+  size_t total;
+  __host__ __device__ size_t q_bytes() const { return size_t(ks) * 8 * kFrag; }
+  __host__ __device__ size_t y_at() const { return q_bytes(); }
+  __host__ __device__ size_t scalars_at() const { return y_at() + 12 * kFrag; }
+  __host__ __device__ size_t u_at() const { return scalars_at() + 1024; }
+};
+
+__host__ __device__ inline SlotLayout slot_layout(int Hk, int Hv, int dk, int dv) {
+  SlotLayout l;
+  l.ks = padded_dk(dk) / 32;
+  l.key = 2 * l.q_bytes();
+  l.value = l.u_at() + size_t(dv / 16) * 4 * kFrag;
+  l.total = Hk * l.key + Hv * l.value;
+  return l;
+}
+
+// What a launch takes: chunks c0 .. c0 + M - 1 of sequences b0 .. b0 + G - 1.
+struct Part {
+  int b0, G, c0, M;
+  char* ws;
+};
+
+__device__ __forceinline__ char* slot_at(const ChainArgs& a, const Part& p, int g, int m) {
+  return p.ws + (size_t(g) * p.M + m) * slot_layout(a.Hk, a.Hv, a.dk, a.dv).total;
+}
+__device__ __forceinline__ char* key_at(const ChainArgs& a, char* slot, int hk) {
+  return slot + hk * slot_layout(a.Hk, a.Hv, a.dk, a.dv).key;
+}
+__device__ __forceinline__ char* value_at(const ChainArgs& a, char* slot, int h) {
+  const SlotLayout l = slot_layout(a.Hk, a.Hv, a.dk, a.dv);
+  return slot + a.Hk * l.key + h * l.value;
+}
+
+// Step s of token tile t of a lower triangular operand (6 of them: a step holds
+// the columns of two tiles).
+__device__ __forceinline__ constexpr int lower_step(int t, int s) { return t < 2 ? t : 2 + (t - 2) * 2 + s; }
+__device__ __forceinline__ constexpr int lower_tile(int u) { return u < 2 ? u : 2 + (u - 2) / 2; }
+__device__ __forceinline__ constexpr int lower_col(int u) { return u < 2 ? 0 : (u - 2) % 2; }
+
+// ---------------------------------------------------------------------------
+// fp16 pairs
+// ---------------------------------------------------------------------------
+struct Pair {
+  f16x8 hi, lo;
+};
+
+__device__ __forceinline__ Pair split(const float (&x)[8], float scale) {
+  Pair p;
+#pragma unroll
+  for (int e = 0; e < 8; ++e) {
+    const float y = x[e] * scale;
+    p.hi[e] = (_Float16)y;
+    p.lo[e] = (_Float16)(y - (float)p.hi[e]);
+  }
+  return p;
+}
+
+__device__ __forceinline__ f32x4 mma(f16x8 a, f16x8 b, f32x4 c) { return __builtin_amdgcn_mfma_f32_16x16x32_f16(a, b, c, 0, 0, 0); }
+
+__device__ __forceinline__ f32x4 mma3(const Pair& a, const Pair& b, f32x4 c) {
+  c = mma(a.lo, b.hi, c);
+  c = mma(a.hi, b.lo, c);
+  return mma(a.hi, b.hi, c);
+}
+
+// Power of two that takes m to 2^13 .. 2^14, and its inverse (both normal
+// floats: m is clamped to 2^-113 .. 2^126).
+__device__ __forceinline__ void f16_scale(float m, float& scale, float& inv) {
+  int ex = int((__float_as_uint(m) >> 23) & 0xffu);
+  ex = ex < 14 ? 14 : ex > 253 ? 253 : ex;
+  scale = __uint_as_float(unsigned(267 - ex) << 23);
+  inv = __uint_as_float(unsigned(ex - 13) << 23);
+}
+
+// Over the four lanes of a column (lane % 16).
+__device__ __forceinline__ float column_max(float x) {
+  x = fmaxf(x, __shfl_xor(x, 16));
+  return fmaxf(x, __shfl_xor(x, 32));
+}
+__device__ __forceinline__ float column_sum(float x) {
+  x += __shfl_xor(x, 16);
+  return x + __shfl_xor(x, 32);
+}
+
+__device__ __forceinline__ Pair load_pair(const char* p, int tile, int lane) {
+  const char* q = p + size_t(tile) * 2 * kFrag + lane * 16;
+  return {*reinterpret_cast<const f16x8*>(q), *reinterpret_cast<const f16x8*>(q + kFrag)};
+}
+__device__ __forceinline__ void store_pair(char* p, int tile, int lane, const Pair& x) {
+  char* q = p + size_t(tile) * 2 * kFrag + lane * 16;
+  *reinterpret_cast<f16x8*>(q) = x.hi;
+  *reinterpret_cast<f16x8*>(q + kFrag) = x.lo;
+}
+
+// ---------------------------------------------------------------------------
+// Raw inputs
+// ---------------------------------------------------------------------------
+// 8 channels of a row.
+__device__ __forceinline__ void fetch8(const float* p, float (&x)[8]) {
+  const float4 y = ld4(p), z = ld4(p + 4);
+  x[0] = y.x, x[1] = y.y, x[2] = y.z, x[3] = y.w, x[4] = z.x, x[5] = z.y, x[6] = z.z, x[7] = z.w;
+}
+__device__ __forceinline__ void fetch8(const BF16* p, float (&x)[8]) {
+  const u32x4 u = *reinterpret_cast<const u32x4*>(p);
+#pragma unroll
+  for (int e = 0; e < 4; ++e) {
+    x[2 * e] = __uint_as_float(u[e] << 16);
+    x[2 * e + 1] = __uint_as_float(u[e] & 0xffff0000u);
+  }
+}
+
+template <int DKP>
+struct Prep {
+  static constexpr int kPacks = DKP / 8, kKs = DKP / 32;
+  static constexpr int kPlane = kPacks * (kC + 1) * 16;       // bytes of hi or lo of K or Q: [pack][token]
+  static constexpr int kMat = kC * kLd * int(sizeof(float));  // a chunk's matrix
+  static constexpr int kRows = 4 * kPlane > kHeads * kMat ? 4 * kPlane : kHeads * kMat;
+  static constexpr int kKt = DKP / 16 * 4 * kFrag;
+  static constexpr int kLds = kRows + kKt + kMat + kHeads * kC * 24;
+};
+
+// ---------------------------------------------------------------------------
+// What does not depend on the state.  One workgroup per (key head, chunk) with
+// all of its value heads: keys and queries are convolved once.
+// ---------------------------------------------------------------------------
+template <typename TIn, int DKP>
+__global__ __launch_bounds__(kPrepThreads, 2) void chunk_kernel(ChainArgs a, Part part) {
+  typedef Prep<DKP> P;
+  constexpr int kKs = P::kKs, kPacks = P::kPacks;
+  extern __shared__ __align__(16) char s_raw[];
+  char* s_kq = s_raw;                                        // K hi, K lo, Q hi, Q lo; then the heads' matrices
+  float* s_t = reinterpret_cast<float*>(s_raw);              // [head][64][kLd]
+  char* s_kt = s_raw + P::kRows;                             // operand tiles of K^T
+  float* s_g = reinterpret_cast<float*>(s_kt + P::kKt);      // [64][kLd]: k_i.k_j
+  double* s_log = reinterpret_cast<double*>(s_g + kC * kLd);  // [head][64]
+  float* s_decay = reinterpret_cast<float*>(s_log + kHeads * kC);  // e^g
+  float* s_beta = s_decay + kHeads * kC;
+  float* s_row = s_beta + kHeads * kC;                       // 1 / scale of a row of W
+  const int tid = threadIdx.x, lane = tid % kWave, w = __builtin_amdgcn_readfirstlane(tid / kWave);
+  const int n16 = lane & 15, q4 = lane >> 4;
+  const int hk = blockIdx.x, m = blockIdx.y, b = part.b0 + blockIdx.z;
+  const Tokens tk = tokens_of(a, b);
+  const int n0 = (part.c0 + m) * kC, nt = min(kC, tk.n - n0);
+  if (nt <= 0) return;
+  const int dk = a.dk, dv = a.dv, per = a.Hv / a.Hk, C = 2 * a.Hk * dk + a.Hv * dv;
+  char* slot = slot_at(a, part, blockIdx.z, m);
+  const float* cs = a.conv_state + size_t(b) * 3 * C;
+
+  // keys and queries: 8 channels a thread, kLpt threads a token
+  {
+    constexpr int kLpt = kPacks, kGroups = kPrepThreads / kLpt, kTok = kC > kGroups ? kC / kGroups : 1;
+    const int p = tid % kLpt, t0 = tid / kLpt * kTok;
+#pragma unroll
+    for (int isq = 0; isq < 2; ++isq) {
+      const TIn* x = reinterpret_cast<const TIn*>(isq ? a.q : a.k);
+      const int c0 = (isq ? hk : a.Hk + hk) * dk + p * 8;  // conv channel
+      const bool in = p * 8 < dk && t0 < kC;
+      float win[kTok + 3][8], cw[8][4];
+#pragma unroll
+      for (int i = 0; i < kTok + 3; ++i) {
+        const int t = t0 - 3 + i;  // of the chunk
+#pragma unroll
+        for (int e = 0; e < 8; ++e) win[i][e] = 0.0f;
+        if (!in || t >= nt) continue;
+        if (n0 + t >= 0) fetch8(x + (size_t(tk.first + n0 + t) * a.Hk + hk) * dk + p * 8, win[i]);
+        else fetch8(cs + size_t(n0 + t + 3) * C + c0, win[i]);
+      }
+#pragma unroll
+      for (int e = 0; e < 8; ++e) {
+        const float4 y = in ? *reinterpret_cast<const float4*>(a.conv_w + size_t(c0 + e) * 4) : make_float4(0, 0, 0, 0);
+        cw[e][0] = y.x, cw[e][1] = y.y, cw[e][2] = y.z, cw[e][3] = y.w;
+      }
+#pragma unroll
+      for (int i = 0; i < kTok; ++i) {
+        float y[8], sum = 0.0f;
+#pragma unroll
+        for (int e = 0; e < 8; ++e) {
+          y[e] = silu(cw[e][0] * win[i][e] + cw[e][1] * win[i + 1][e] + cw[e][2] * win[i + 2][e] + cw[e][3] * win[i + 3][e]);
+          sum += y[e] * y[e];
+        }
+        const float inv = t0 + i < nt ? rsqrt_hw(group_sum<kLpt>(sum) + 1e-6f) * kUnit : 0.0f;
+        const Pair x8 = split(y, inv);
+        if (t0 < kC) {
+          char* d = s_kq + isq * 2 * P::kPlane + (p * (kC + 1) + t0 + i) * 16;
+          *reinterpret_cast<f16x8*>(d) = x8.hi;
+          *reinterpret_cast<f16x8*>(d + P::kPlane) = x8.lo;
+        }
+      }
+    }
+  }
+  __syncthreads();
+
+  auto rows_of = [&](int isq, int t, int s) {  // operand rows: 16 tokens, 32 channels in order
+    const char* d = s_kq + isq * 2 * P::kPlane + ((4 * s + q4) * (kC + 1) + 16 * t + n16) * 16;
+    return Pair{*reinterpret_cast<const f16x8*>(d), *reinterpret_cast<const f16x8*>(d + P::kPlane)};
+  };
+  auto gram = [&](int isq, int ti, int tj) {  // rows: keys of tile ti, columns: keys or queries of tile tj
+    f32x4 c = {};
+#pragma unroll
+    for (int s = 0; s < kKs; ++s) c = mma3(rows_of(0, ti, s), rows_of(isq, tj, s), c);
+    return c;
+  };
+  // k_j.q_i with the queries as columns: unit w of Y, two tiles of keys
+  f32x4 kq[2] = {};
+  if (w < 6) {
+    kq[0] = gram(1, 2 * lower_col(w), lower_tile(w));
+    if (2 * lower_col(w) + 1 <= lower_tile(w)) kq[1] = gram(1, 2 * lower_col(w) + 1, lower_tile(w));
+  }
+  // k_i.k_j, the ten tiles of the lower triangle
+  for (int u = w < 4 ? w : w >= 6 ? 4 + (w - 6) * 3 : 10, n = w < 4 ? 1 : w >= 6 ? 3 : 0; n > 0; --n, ++u) {
+    const int ti = u < 1 ? 0 : u < 3 ? 1 : u < 6 ? 2 : 3, tj = u - ti * (ti + 1) / 2;
+    const f32x4 c = gram(0, ti, tj);
+#pragma unroll
+    for (int r = 0; r < 4; ++r) s_g[(16 * ti + 4 * q4 + r) * kLd + 16 * tj + n16] = c[r] * (1.0f / (kUnit * kUnit));
+  }
+  // K^T: rows are channels, 32 tokens; Q: rows are tokens, 32 channels; both in
+  // the order of accumulators
+  char* kws = key_at(a, slot, hk);
+  const size_t kt_at = size_t(kKs) * 8 * kFrag;
+  for (int u = w; u < DKP / 16 * 2; u += kPrepWaves) {
+    const int c = u / 2 * 16 + n16, s = u % 2;
+    Pair x;
+#pragma unroll
+    for (int j = 0; j < 8; ++j) {
+      const int t = 32 * s + 16 * (j / 4) + 4 * q4 + j % 4;
+      const char* d = s_kq + (c / 8 * (kC + 1) + t) * 16 + c % 8 * 2;
+      x.hi[j] = *reinterpret_cast<const _Float16*>(d);
+      x.lo[j] = *reinterpret_cast<const _Float16*>(d + P::kPlane);
+    }
+    store_pair(s_kt, u, lane, x);
+    store_pair(kws + kt_at, u, lane, x);
+  }
+  for (int u = w; u < kKs * 4; u += kPrepWaves) {
+    const int s = u / 4, t = u % 4;
+    Pair x;
+#pragma unroll
+    for (int hl = 0; hl < 2; ++hl) {
+      f16x4 y[2];
+#pragma unroll
+      for (int e = 0; e < 2; ++e)
+        y[e] = *reinterpret_cast<const f16x4*>(s_kq + (2 + hl) * P::kPlane +
+                                               ((4 * s + 2 * e + q4 / 2) * (kC + 1) + 16 * t + n16) * 16 + q4 % 2 * 8);
+      const f16x8 z = {y[0][0], y[0][1], y[0][2], y[0][3], y[1][0], y[1][1], y[1][2], y[1][3]};
+      if (hl) x.lo = z;
+      else x.hi = z;
+    }
+    store_pair(kws, u, lane, x);
+  }
+
+  for (int r0 = 0; r0 < per; r0 += kHeads) {
+    const int nr = min(kHeads, per - r0);
+    __syncthreads();  // K and Q, or the last heads' matrices, are read
+    if (w < nr) {     // decays of a head, a token a lane
+      const size_t at = size_t(tk.first + n0 + (lane < nt ? lane : 0)) * a.Hv + hk * per + r0 + w;
+      const float al = lane < nt ? to_f32(reinterpret_cast<const TIn*>(a.alpha)[at]) : 1.0f;
+      const float be = lane < nt ? to_f32(reinterpret_cast<const TIn*>(a.beta)[at]) : 0.0f;
+      // 64-bit sums: far into a chunk of strong decays the difference of two of
+      // them is small
+      double g = double(logf(al < 0x1p-126f ? 0x1p-126f : al));
+#pragma unroll
+      for (int d = 1; d < kWave; d *= 2) {
+        const double x = __shfl_up(g, d);
+        if (lane >= d) g += x;
+      }
+      s_log[w * kC + lane] = g;
+      s_decay[w * kC + lane] = __expf(float(g));
+      s_beta[w * kC + lane] = be;
+    }
+    __syncthreads();
+    for (int u = tid; u < nr * kC * kC; u += kPrepThreads) {
+      const int r = u / (kC * kC), i = u / kC % kC, j = u % kC;
+      s_t[(r * kC + i) * kLd + j] =
+          j < i ? s_beta[r * kC + i] * s_g[i * kLd + j] * __expf(float(s_log[r * kC + i] - s_log[r * kC + j])) : 0.0f;
+    }
+    __syncthreads();
+    // inverses of the blocks of the diagonal: a block per 16 lanes, a column a lane
+    if (w < nr) {
+      float* x = s_t + (w * kC + 16 * q4) * kLd + 16 * q4;
+      float t[16];
+#pragma unroll
+      for (int i = 0; i < 16; ++i) {
+        float y = i == n16 ? 1.0f : 0.0f;
+#pragma unroll
+        for (int j = 0; j < i; j += 4) {
+          const float4 l = *reinterpret_cast<const float4*>(x + i * kLd + j);
+          y -= l.x * t[j];
+          if (j + 1 < i) y -= l.y * t[j + 1];
+          if (j + 2 < i) y -= l.z * t[j + 2];
+          if (j + 3 < i) y -= l.w * t[j + 3];
+        }
+        t[i] = y;
+      }
+      __builtin_amdgcn_wave_barrier();  // rows are read before they are replaced
+#pragma unroll
+      for (int i = 0; i < 16; ++i) x[i * kLd + n16] = t[i];
+    }
+    __syncthreads();
+    // blocks below: X_j = T_jj, X_i = -T_ii sum_k A_ik X_k down the column of
+    // blocks j; two waves a head, columns 0, and 1 and 2
+    f32x4 low[3];  // blocks (1, 0), (2, 0), (3, 0), or (2, 1), (3, 1), (3, 2)
+    if (w < 2 * nr) {
+      const float* x = s_t + w / 2 * kC * kLd;
+      auto block = [&](int i, int k) { return *reinterpret_cast<const f32x4*>(x + (16 * i + n16) * kLd + 16 * k + 4 * q4); };
+      auto diagonal = [&](int j) {
+        f32x4 c;
+#pragma unroll
+        for (int r = 0; r < 4; ++r) c[r] = x[(16 * j + 4 * q4 + r) * kLd + 16 * j + n16];
+        return c;
+      };
+      auto times = [&](f32x4 y, f32x4 z, f32x4 c) {
+#pragma unroll
+        for (int r = 0; r < 4; ++r) c = __builtin_amdgcn_mfma_f32_16x16x4f32(y[r], z[r], c, 0, 0, 0);
+        return c;
+      };
+      const f32x4 zero = {};
+      if (w % 2 == 0) {
+        const f32x4 x0 = diagonal(0);
+        low[0] = -times(block(1, 1), times(block(1, 0), x0, zero), zero);
+        low[1] = -times(block(2, 2), times(block(2, 1), low[0], times(block(2, 0), x0, zero)), zero);
+        low[2] = -times(block(3, 3), times(block(3, 2), low[1], times(block(3, 1), low[0], times(block(3, 0), x0, zero))), zero);
+      } else {
+        const f32x4 x1 = diagonal(1), x2 = diagonal(2);
+        low[0] = -times(block(2, 2), times(block(2, 1), x1, zero), zero);
+        low[1] = -times(block(3, 3), times(block(3, 2), low[0], times(block(3, 1), x1, zero)), zero);
+        low[2] = -times(block(3, 3), times(block(3, 2), x2, zero), zero);
+      }
+    }
+    __syncthreads();
+    if (w < 2 * nr) {
+      float* x = s_t + w / 2 * kC * kLd;
+#pragma unroll
+      for (int n = 0; n < 3; ++n) {
+        const int i = w % 2 == 0 ? n + 1 : n == 0 ? 2 : 3, j = w % 2 == 0 ? 0 : n == 2 ? 2 : 1;
+#pragma unroll
+        for (int r = 0; r < 4; ++r) x[(16 * i + 4 * q4 + r) * kLd + 16 * j + n16] = low[n][r];
+      }
+    }
+    __syncthreads();
+
+    for (int r = 0; r < nr; ++r) {
+      const int h = hk * per + r0 + r;
+      char* vws = value_at(a, slot, h);
+      const float *t = s_t + r * kC * kLd, *beta = s_beta + r * kC, *decay = s_decay + r * kC;
+      const double* lg = s_log + r * kC;
+      // values of channel 16 w + n16 in operand order
+      float v[2][8] = {};
+      if (16 * w < dv) {
+        const int c = h * dv + 16 * w + n16;
+        const TIn* x = reinterpret_cast<const TIn*>(a.v) + size_t(tk.first + n0) * a.Hv * dv + c;
+        const float4 cw = *reinterpret_cast<const float4*>(a.conv_w + (size_t(2) * a.Hk * dk + c) * 4);
+#pragma unroll
+        for (int s = 0; s < 2; ++s)
+#pragma unroll
+          for (int e = 0; e < 2; ++e) {
+            const int t0 = 32 * s + 16 * e + 4 * q4;
+            float win[7];
+#pragma unroll
+            for (int i = 0; i < 7; ++i) {
+              const int n = t0 - 3 + i;
+              win[i] = 0.0f;
+              if (n >= nt) continue;
+              if (n0 + n >= 0) win[i] = to_f32(x[(long long)(n) * a.Hv * dv]);
+              else win[i] = cs[size_t(n0 + n + 3) * C + 2 * a.Hk * dk + c];
+            }
+#pragma unroll
+            for (int i = 0; i < 4; ++i)
+              v[s][4 * e + i] = t0 + i < nt ? silu(cw.x * win[i] + cw.y * win[i + 1] + cw.z * win[i + 2] + cw.w * win[i + 3]) : 0.0f;
+          }
+      }
+      // (I + A)^-1 diag(beta): rows n16 of tile t, columns in operand order
+      float inv[6][8];
+#pragma unroll
+      for (int u = 0; u < 6; ++u) {
+        const int i = 16 * lower_tile(u) + n16, j = 32 * lower_col(u) + 4 * q4;
+#pragma unroll
+        for (int e = 0; e < 2; ++e) {
+          const float4 x = *reinterpret_cast<const float4*>(t + i * kLd + j + 16 * e);
+          const float4 y = *reinterpret_cast<const float4*>(beta + j + 16 * e);
+          inv[u][4 * e] = x.x * y.x, inv[u][4 * e + 1] = x.y * y.y, inv[u][4 * e + 2] = x.z * y.z, inv[u][4 * e + 3] = x.w * y.w;
+        }
+      }
+      if (16 * w < dv) {  // U: rows are tokens, columns this wave's channels
+        float mt = 0.0f, mv = 0.0f, st, it, sv, iv;
+#pragma unroll
+        for (int u = 0; u < 6; ++u)
+#pragma unroll
+          for (int e = 0; e < 8; ++e) mt = fmaxf(mt, fabsf(inv[u][e]));
+#pragma unroll
+        for (int e = 0; e < 8; ++e) mv = fmaxf(mv, fmaxf(fabsf(v[0][e]), fabsf(v[1][e])));
+        f16_scale(column_max(group_max<16>(mt)), st, it);
+        f16_scale(column_max(mv), sv, iv);
+        const Pair v0 = split(v[0], sv), v1 = split(v[1], sv);
+        char* u_out = vws + slot_layout(a.Hk, a.Hv, dk, dv).u_at() + size_t(w) * 4 * kFrag;
+#pragma unroll
+        for (int tt = 0; tt < 4; ++tt) {
+          f32x4 c = mma3(split(inv[lower_step(tt, 0)], st), v0, f32x4{});
+          if (tt >= 2) c = mma3(split(inv[lower_step(tt, 1)], st), v1, c);
+          c *= it;  // the two scales apart: their product may leave the range
+          c *= iv;
+          *reinterpret_cast<f32x4*>(u_out + tt * kFrag + lane * 16) = c;
+        }
+      }
+      // (I + A)^-1 diag(beta e^g), and W = that times K: |W| of a row is at most
+      // the sum of the row
+      float bound[4] = {}, sw[4], iw[4];
+#pragma unroll
+      for (int u = 0; u < 6; ++u)
+#pragma unroll
+        for (int e = 0; e < 2; ++e) {
+          const float4 y = *reinterpret_cast<const float4*>(decay + 32 * lower_col(u) + 4 * q4 + 16 * e);
+          inv[u][4 * e] *= y.x, inv[u][4 * e + 1] *= y.y, inv[u][4 * e + 2] *= y.z, inv[u][4 * e + 3] *= y.w;
+#pragma unroll
+          for (int i = 0; i < 4; ++i) bound[lower_tile(u)] += fabsf(inv[u][4 * e + i]);
+        }
+#pragma unroll
+      for (int tt = 0; tt < 4; ++tt) {
+        f16_scale(column_sum(bound[tt]), sw[tt], iw[tt]);
+        if (w == 0 && q4 == 0) s_row[r * kC + 16 * tt + n16] = iw[tt];
+      }
+      if (w < 2 * kKs) {
+        const int s = w / 2;
+        auto w_tile = [&](int tt, float scale, const Pair& x0, const Pair& x1) {
+          f32x4 c[2];
+#pragma unroll
+          for (int e = 0; e < 2; ++e) {
+            c[e] = mma3(load_pair(s_kt, (2 * s + e) * 2, lane), x0, f32x4{});
+            if (tt >= 2) c[e] = mma3(load_pair(s_kt, (2 * s + e) * 2 + 1, lane), x1, c[e]);
+          }
+          const float y[8] = {c[0][0], c[0][1], c[0][2], c[0][3], c[1][0], c[1][1], c[1][2], c[1][3]};
+          store_pair(vws, s * 4 + tt, lane, split(y, 1.0f / kUnit));
+        };
+        if (w % 2 == 0) {
+          w_tile(0, sw[0], split(inv[0], sw[0]), Pair{});
+          w_tile(3, sw[3], split(inv[4], sw[3]), split(inv[5], sw[3]));
+        } else {
+          w_tile(1, sw[1], split(inv[1], sw[1]), Pair{});
+          w_tile(2, sw[2], split(inv[2], sw[2]), split(inv[3], sw[2]));
+        }
+      }
+      if (w < 6) {  // Y
+        const int i = 16 * lower_tile(w) + n16;
+        float y[8];
+#pragma unroll
+        for (int e = 0; e < 8; ++e) {
+          const int j = 32 * lower_col(w) + 16 * (e / 4) + 4 * q4 + e % 4;
+          y[e] = j <= i ? kq[e / 4][e % 4] * __expf(float(lg[i] - lg[j])) : 0.0f;
+        }
+        store_pair(vws + slot_layout(a.Hk, a.Hv, dk, dv).y_at(), w, lane, split(y, 1.0f / kUnit));
+      }
+      if (w == 7) {  // a token a lane; the decay to the chunk's end
+        float* sc = reinterpret_cast<float*>(vws + slot_layout(a.Hk, a.Hv, dk, dv).scalars_at());
+        sc[kC + lane] = decay[lane];
+        sc[2 * kC + lane] = __expf(float(lg[kC - 1] - lg[lane]));
+        if (lane == 0) sc[3 * kC] = decay[kC - 1];
+      }
+      if (w == 0) {
+        float* sc = reinterpret_cast<float*>(vws + slot_layout(a.Hk, a.Hv, dk, dv).scalars_at());
+        sc[lane] = s_row[r * kC + lane];
+      }
+    }
+  }
+}
+
+// ---------------------------------------------------------------------------
+// The chunks of a sequence in turn.  A wave holds the state of 16 value
+// channels; the waves of a workgroup share the chunk's operands in LDS.
+// ---------------------------------------------------------------------------
+template <int DKP>
+struct Scan {
+  static constexpr int kKs = DKP / 32;
+  static constexpr int kQ = kKs * 8 * kFrag;  // W first, the scalars behind Y
+  static constexpr int kLds = 3 * kQ + 13 * kFrag;
+};
+
+__device__ __forceinline__ void to_lds(const char* src, char* dst, int lane) {
+  __builtin_amdgcn_global_load_lds((const __attribute__((address_space(1))) void*)(src + lane * 16),
+                                   (__attribute__((address_space(3))) void*)(dst), 16, 0, 0);
+}
+
+template <typename TOut, int DKP, int NW>
+__global__ __launch_bounds__(NW * kWave) void scan_kernel(ChainArgs a, Part part) {
+  typedef Scan<DKP> S;
+  constexpr int kKs = S::kKs;
+  extern __shared__ __align__(16) char s_raw[];
+  char *s_w = s_raw, *s_y = s_w + S::kQ, *s_q = s_y + 13 * kFrag, *s_kt = s_q + S::kQ;
+  const float* s_sc = reinterpret_cast<const float*>(s_y + 12 * kFrag);
+  const int tid = threadIdx.x, lane = tid % kWave, w = __builtin_amdgcn_readfirstlane(tid / kWave);
+  const int n16 = lane & 15, q4 = lane >> 4;
+  const int group = blockIdx.x * NW + w, h = blockIdx.y, b = part.b0 + blockIdx.z, hk = h / (a.Hv / a.Hk);
+  const Tokens tk = tokens_of(a, b);
+  const int dk = a.dk, dv = a.dv, end = min(part.c0 + part.M, (tk.n + kC - 1) / kC);
+  if (part.c0 >= end) return;
+  const SlotLayout l = slot_layout(a.Hk, a.Hv, dk, dv);
+  const int ch = group * 16 + n16;  // value channel
+  float* state = a.S + ((size_t(b) * a.Hv + h) * dv + ch) * dk + 4 * q4;
+  f32x4 st[DKP / 16];  // key channels 16 n + 4 q4 ..
+#pragma unroll
+  for (int n = 0; n < DKP / 16; ++n) st[n] = 16 * n < dk ? *reinterpret_cast<const f32x4*>(state + 16 * n) : f32x4{};
+  TOut* out = reinterpret_cast<TOut*>(a.out) + (size_t(tk.first) * a.Hv + h) * dv + ch;
+
+  for (int c = part.c0; c < end; ++c) {
+    char* slot = slot_at(a, part, blockIdx.z, c - part.c0);
+    const char *vws = value_at(a, slot, h), *kws = key_at(a, slot, hk);
+    __syncthreads();  // the last chunk's operands are read
+    for (int u = w; u < S::kQ / kFrag + 13; u += NW) to_lds(vws + u * kFrag, s_w + u * kFrag, lane);
+    for (int u = w; u < 2 * S::kQ / kFrag; u += NW) to_lds(kws + u * kFrag, s_q + u * kFrag, lane);
+    f32x4 x[4];  // U, then V'
+#pragma unroll
+    for (int t = 0; t < 4; ++t) x[t] = *reinterpret_cast<const f32x4*>(vws + l.u_at() + (size_t(group) * 4 + t) * kFrag + lane * 16);
+
+    // the state as an operand
+    float m = 0.0f, ss, is;
+#pragma unroll
+    for (int n = 0; n < DKP / 16; ++n)
+#pragma unroll
+      for (int r = 0; r < 4; ++r) m = fmaxf(m, fabsf(st[n][r]));
+    f16_scale(column_max(m), ss, is);
+    Pair sp[kKs];
+#pragma unroll
+    for (int s = 0; s < kKs; ++s) {
+      const float y[8] = {st[2 * s][0], st[2 * s][1], st[2 * s][2], st[2 * s][3],
+                          st[2 * s + 1][0], st[2 * s + 1][1], st[2 * s + 1][2], st[2 * s + 1][3]};
+      sp[s] = split(y, ss);
+    }
+    asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
+    __syncthreads();
+
+    // V' = U - W S^T
+    float mv = 0.0f, md = 0.0f, sv, iv, sd, id;
+    f32x4 xd[4];  // decayed to the chunk's end
+#pragma unroll
+    for (int t = 0; t < 4; ++t) {
+      f32x4 p = {};
+#pragma unroll
+      for (int s = 0; s < kKs; ++s) p = mma3(load_pair(s_w, s * 4 + t, lane), sp[s], p);
+      const f32x4 rs = *reinterpret_cast<const f32x4*>(s_sc + 16 * t + 4 * q4);
+      const f32x4 dec = *reinterpret_cast<const f32x4*>(s_sc + 2 * kC + 16 * t + 4 * q4);
+#pragma unroll
+      for (int r = 0; r < 4; ++r) {
+        x[t][r] -= p[r] * rs[r] * is;
+        xd[t][r] = x[t][r] * dec[r];
+        mv = fmaxf(mv, fabsf(x[t][r]));
+        md = fmaxf(md, fabsf(xd[t][r]));
+      }
+    }
+    f16_scale(column_max(mv), sv, iv);
+    f16_scale(column_max(md), sd, id);
+    Pair vp[2], vd[2];
+#pragma unroll
+    for (int s = 0; s < 2; ++s) {
+      const float y[8] = {x[2 * s][0], x[2 * s][1], x[2 * s][2], x[2 * s][3],
+                          x[2 * s + 1][0], x[2 * s + 1][1], x[2 * s + 1][2], x[2 * s + 1][3]};
+      const float z[8] = {xd[2 * s][0], xd[2 * s][1], xd[2 * s][2], xd[2 * s][3],
+                          xd[2 * s + 1][0], xd[2 * s + 1][1], xd[2 * s + 1][2], xd[2 * s + 1][3]};
+      vp[s] = split(y, sv);
+      vd[s] = split(z, sd);
+    }
+    // outputs
+    iv *= 1.0f / kUnit;
+    const float io = is * (1.0f / kUnit);
+#pragma unroll
+    for (int t = 0; t < 4; ++t) {
+      f32x4 o = {}, y = {};
+#pragma unroll
+      for (int s = 0; s < kKs; ++s) o = mma3(load_pair(s_q, s * 4 + t, lane), sp[s], o);
+      y = mma3(load_pair(s_y, lower_step(t, 0), lane), vp[0], y);
+      if (t >= 2) y = mma3(load_pair(s_y, lower_step(t, 1), lane), vp[1], y);
+      const f32x4 dec = *reinterpret_cast<const f32x4*>(s_sc + kC + 16 * t + 4 * q4);
+#pragma unroll
+      for (int r = 0; r < 4; ++r) {
+        const int i = c * kC + 16 * t + 4 * q4 + r;
+        if (i < tk.n) put(out + size_t(i) * a.Hv * dv, a.scale * (o[r] * dec[r] * io + y[r] * iv));
+      }
+    }
+    // the state behind the chunk
+    const float last = s_sc[3 * kC];
+    id *= 1.0f / kUnit;
+#pragma unroll
+    for (int n = 0; n < DKP / 16; ++n) {
+      f32x4 p = {};
+#pragma unroll
+      for (int s = 0; s < 2; ++s) p = mma3(load_pair(s_kt, n * 2 + s, lane), vd[s], p);
+#pragma unroll
+      for (int r = 0; r < 4; ++r) st[n][r] = last * st[n][r] + p[r] * id;
+    }
+  }
+#pragma unroll
+  for (int n = 0; n < DKP / 16; ++n)
+    if (16 * n < dk) *reinterpret_cast<f32x4*>(state + 16 * n) = st[n];
+}
+
+// The conv state behind the last token, and the statuses.
+template <typename TIn>
+__global__ __launch_bounds__(256) void tail_kernel(ChainArgs a) {
+  const int b = blockIdx.y, nq = a.Hk * a.dk, nv = a.Hv * a.dv, C = 2 * nq + nv;
+  const Tokens tk = tokens_of(a, b);
+  if (a.status && blockIdx.x == 0 && threadIdx.x == 0) a.status[b] = tk.status;
+  const int c = blockIdx.x * 256 + threadIdx.x;
+  if (c >= C) return;
+  const size_t at = size_t(b) * 3 * C + c;
+#pragma unroll
+  for (int s = 0; s < 3; ++s) {
+    const int t = tk.n - 3 + s;
+    float x;
+    if (t < 0) x = a.conv_state[at + size_t(t + 3) * C];
+    else if (c < nq) x = to_f32(reinterpret_cast<const TIn*>(a.q)[size_t(tk.first + t) * nq + c]);
+    else if (c < 2 * nq) x = to_f32(reinterpret_cast<const TIn*>(a.k)[size_t(tk.first + t) * nq + c - nq]);
+    else x = to_f32(reinterpret_cast<const TIn*>(a.v)[size_t(tk.first + t) * nv + c - 2 * nq]);
+    a.conv_state_out[at + size_t(s) * C] = x;
+  }
+}
+
+int after_launch() {
+  const hipError_t e = hipGetLastError();
+  return e == hipSuccess ? GDN_OK : set_error(GDN_EHIP, "chain: launch: %s", hipGetErrorString(e));
+}
+
+template <typename TIn, int DKP>
+int launch_prep(const ChainArgs& a, const Part& p, hipStream_t stream) {
+  constexpr int lds = Prep<DKP>::kLds;
+  const int rc = ensure_dynamic_lds(reinterpret_cast<const void*>(chunk_kernel<TIn, DKP>), lds, "chain");
+  if (rc != GDN_OK) return rc;
+  chunk_kernel<TIn, DKP><<<dim3(a.Hk, p.M, p.G), kPrepThreads, lds, stream>>>(a, p);
+  return after_launch();
+}
+
+template <typename TOut, int DKP, int NW>
+int launch_waves(const ChainArgs& a, const Part& p, hipStream_t stream) {
+  constexpr int lds = Scan<DKP>::kLds;
+  const int rc = ensure_dynamic_lds(reinterpret_cast<const void*>(scan_kernel<TOut, DKP, NW>), lds, "chain");
+  if (rc != GDN_OK) return rc;
+  scan_kernel<TOut, DKP, NW><<<dim3(a.dv / 16 / NW, a.Hv, p.G), NW * kWave, lds, stream>>>(a, p);
+  return after_launch();
+}
+
+template <typename TOut, int DKP>
+int launch_scan(const ChainArgs& a, const Part& p, hipStream_t stream) {
+  // waves of a workgroup: as many as share a head, but a workgroup a CU
+  const int groups = a.dv / 16;
+  int nw = groups;
+  while (nw > 1 && (long long)(p.G) * a.Hv * (groups / nw) < 192) nw /= 2;
+  if (nw >= 8) return launch_waves<TOut, DKP, 8>(a, p, stream);
+  if (nw == 4) return launch_waves<TOut, DKP, 4>(a, p, stream);
+  if (nw == 2) return launch_waves<TOut, DKP, 2>(a, p, stream);
+  return launch_waves<TOut, DKP, 1>(a, p, stream);
+}
+
+template <int DKP>
+int launch_part(const ChainArgs& a, const Part& p, hipStream_t stream) {
+  int rc = a.in_dtype == GDN_BF16 ? launch_prep<BF16, DKP>(a, p, stream) : launch_prep<float, DKP>(a, p, stream);
+  if (rc != GDN_OK) return rc;
+  return a.out_dtype == GDN_BF16 ? launch_scan<BF16, DKP>(a, p, stream) : launch_scan<float, DKP>(a, p, stream);
+}
+
+}  // namespace
+
+int launch_chain_chunks(const ChainArgs& a, hipStream_t stream) {
+  const StreamOrder order(stream);
+  const size_t slot = slot_layout(a.Hk, a.Hv, a.dk, a.dv).total;
+  const int chunks = (a.T + kC - 1) / kC;
+  const long long slots = std::max<long long>(1, (long long)(GDN_CHAIN_WORKSPACE / slot));
+  Part p;
+  p.G = int(std::min<long long>(a.B, slots));
+  p.M = int(std::min<long long>(chunks, slots / p.G));
+  if (p.M > 65535) p.M = 65535;
+  int rc = GDN_OK;
+  p.ws = static_cast<char*>(stream_workspace(slot * p.G * p.M, stream, &rc));
+  if (!p.ws) return rc;
+  const int C = 2 * a.Hk * a.dk + a.Hv * a.dv, G = p.G;
+  if (a.in_dtype == GDN_BF16) tail_kernel<BF16><<<dim3((C + 255) / 256, a.B), 256, 0, stream>>>(a);
+  else tail_kernel<float><<<dim3((C + 255) / 256, a.B), 256, 0, stream>>>(a);
+  if ((rc = after_launch()) != GDN_OK) return rc;
+  for (p.b0 = 0; p.b0 < a.B; p.b0 += G) {
+    p.G = std::min(G, a.B - p.b0);
+    for (p.c0 = 0; p.c0 < chunks; p.c0 += p.M) {
+      rc = padded_dk(a.dk) == 32 ? launch_part<32>(a, p, stream)
+           : a.dk == 64          ? launch_part<64>(a, p, stream)
+                                 : launch_part<128>(a, p, stream);
+      if (rc != GDN_OK) return rc;
+    }
+  }
+  return GDN_OK;
+}
+
+}  // namespace gdn

@@ -19,12 +19,13 @@ GDN_OK, GDN_EINVAL, GDN_EUNSUPPORTED, GDN_EHIP = 0, -1, -2, -3
 GDN_F32, GDN_BF16 = 0, 1
 TREE_OK, TREE_NO_ROOT, TREE_MULTI_ROOT, TREE_BAD_PARENT, TREE_CYCLE, TREE_BAD_ACCEPTED = range(6)
 KV_BAD_LEN, KV_BAD_PAGE, KV_BAD_POS = range(6, 9)
+CHAIN_BAD_LEN = 9
 MAX_T = 512
 
 EXPORTS = ("gdn_tree_meta_bytes", "gdn_tree_prepare", "gdn_tree_verify",
            "gdn_tree_verify_noalloc", "gdn_tree_verify_chunked", "gdn_tree_commit",
            "gdn_tree_step", "gdn_kv_append", "gdn_tree_attend", "gdn_kv_commit", "gdn_tree_sample",
-           "gdn_tree_accept", "gdn_last_error", "gdn_version")
+           "gdn_tree_accept", "gdn_chain", "gdn_gate_norm", "gdn_add_norm", "gdn_last_error", "gdn_version")
 NOALLOC_SCRATCH_BYTES = 64 << 20  # GDN_NOALLOC_SCRATCH_BYTES of gdn_tree.h
 
 
@@ -79,7 +80,8 @@ def lib() -> ctypes.CDLL:
         L.gdn_tree_step.restype = ctypes.c_int
         L.gdn_tree_step.argtypes = [ctypes.POINTER(Dims)] + [vp] * 20
         for name, n in (("gdn_kv_append", 14), ("gdn_tree_attend", 10), ("gdn_kv_commit", 10),
-                        ("gdn_tree_sample", 10), ("gdn_tree_accept", 8)):  # dims, pointers, stream
+                        ("gdn_tree_sample", 10), ("gdn_tree_accept", 8), ("gdn_chain", 15), ("gdn_gate_norm", 6),
+                        ("gdn_add_norm", 9)):  # dims, pointers, stream
             fn = getattr(L, name)
             fn.restype = ctypes.c_int
             fn.argtypes = [vp] * n
