@@ -34,7 +34,7 @@ namespace {
 typedef _Float16 f16x4 __attribute__((ext_vector_type(4)));
 
 constexpr int kC = 64;          // tokens of a chunk
-constexpr int kPrepThreads = 512;
+constexpr int kPrepThreads = 256;
 constexpr int kPrepWaves = kPrepThreads / kWave;
 constexpr int kHeads = 3;       // value heads that are inverted at once
 constexpr int kLd = kC + 4;     // floats of a row of a chunk's matrix in LDS
@@ -101,7 +101,10 @@ __device__ __forceinline__ Pair split(const float (&x)[8], float scale) {
   Pair p;
 #pragma unroll
   for (int e = 0; e < 8; ++e) {
-    const float y = x[e] * scale;
+    // the product as a value of its own: fused into the conversion it would be
+    // rounded once there and twice for the difference, and hi would differ
+    float y = x[e] * scale;
+    asm("" : "+v"(y));
     p.hi[e] = (_Float16)y;
     p.lo[e] = (_Float16)(y - (float)p.hi[e]);
   }
@@ -167,28 +170,34 @@ struct Prep {
   static constexpr int kPacks = DKP / 8, kKs = DKP / 32;
   static constexpr int kPlane = kPacks * (kC + 1) * 16;       // bytes of hi or lo of K or Q: [pack][token]
   static constexpr int kMat = kC * kLd * int(sizeof(float));  // a chunk's matrix
-  static constexpr int kRows = 4 * kPlane > kHeads * kMat ? 4 * kPlane : kHeads * kMat;
-  static constexpr int kKt = DKP / 16 * 4 * kFrag;
-  static constexpr int kLds = kRows + kKt + kMat + kHeads * kC * 24;
+  static constexpr int kRows = 4 * kPlane > (kHeads + 1) * kMat ? 4 * kPlane : (kHeads + 1) * kMat;
+  static constexpr int kLds = kRows + kHeads * kC * 20;
 };
+
+// Two channels of a row as they are, and one of them.
+__device__ __forceinline__ float2 fetch2(const float* p) { return *reinterpret_cast<const float2*>(p); }
+__device__ __forceinline__ unsigned fetch2(const BF16* p) { return *reinterpret_cast<const unsigned*>(p); }
+__device__ __forceinline__ float one_of(float2 x, int c) { return c ? x.y : x.x; }
+__device__ __forceinline__ float one_of(unsigned x, int c) { return __uint_as_float(c ? x & 0xffff0000u : x << 16); }
 
 // ---------------------------------------------------------------------------
 // What does not depend on the state.  One workgroup per (key head, chunk) with
-// all of its value heads: keys and queries are convolved once.
+// all of its value heads: keys and queries are convolved once.  Loads have no
+// branch around them (rows are clamped and values selected): a branch each made
+// them wait for one another.
 // ---------------------------------------------------------------------------
 template <typename TIn, int DKP>
 __global__ __launch_bounds__(kPrepThreads, 2) void chunk_kernel(ChainArgs a, Part part) {
   typedef Prep<DKP> P;
   constexpr int kKs = P::kKs, kPacks = P::kPacks;
   extern __shared__ __align__(16) char s_raw[];
-  char* s_kq = s_raw;                                        // K hi, K lo, Q hi, Q lo; then the heads' matrices
-  float* s_t = reinterpret_cast<float*>(s_raw);              // [head][64][kLd]
-  char* s_kt = s_raw + P::kRows;                             // operand tiles of K^T
-  float* s_g = reinterpret_cast<float*>(s_kt + P::kKt);      // [64][kLd]: k_i.k_j
-  double* s_log = reinterpret_cast<double*>(s_g + kC * kLd);  // [head][64]
+  char* s_kq = s_raw;                               // K hi, K lo, Q hi, Q lo; then
+  float* s_g = reinterpret_cast<float*>(s_raw);     // [64][kLd]: k_i.k_j, and
+  float* s_t = s_g + kC * kLd;                      // [head][64][kLd]
+  double* s_log = reinterpret_cast<double*>(s_raw + P::kRows);  // [head][64]
   float* s_decay = reinterpret_cast<float*>(s_log + kHeads * kC);  // e^g
   float* s_beta = s_decay + kHeads * kC;
-  float* s_row = s_beta + kHeads * kC;                       // 1 / scale of a row of W
+  float* s_row = s_beta + kHeads * kC;  // 1 / scale of a row of W
   const int tid = threadIdx.x, lane = tid % kWave, w = __builtin_amdgcn_readfirstlane(tid / kWave);
   const int n16 = lane & 15, q4 = lane >> 4;
   const int hk = blockIdx.x, m = blockIdx.y, b = part.b0 + blockIdx.z;
@@ -196,48 +205,64 @@ __global__ __launch_bounds__(kPrepThreads, 2) void chunk_kernel(ChainArgs a, Par
   const int n0 = (part.c0 + m) * kC, nt = min(kC, tk.n - n0);
   if (nt <= 0) return;
   const int dk = a.dk, dv = a.dv, per = a.Hv / a.Hk, C = 2 * a.Hk * dk + a.Hv * dv;
+  const SlotLayout layout = slot_layout(a.Hk, a.Hv, dk, dv);
   char* slot = slot_at(a, part, blockIdx.z, m);
   const float* cs = a.conv_state + size_t(b) * 3 * C;
+  const size_t row0 = size_t(tk.first) + n0;  // of the chunk's first token
+
+  // decays and strengths of a head, a token a lane
+  float al = 1.0f, be = 0.0f;
+  auto fetch_gates = [&](int r0, int nr) {
+    const size_t at = (row0 + min(lane, nt - 1)) * a.Hv + hk * per + r0 + min(w, nr - 1);
+    al = to_f32(reinterpret_cast<const TIn*>(a.alpha)[at]);
+    be = to_f32(reinterpret_cast<const TIn*>(a.beta)[at]);
+    if (lane >= nt) al = 1.0f, be = 0.0f;
+  };
+  fetch_gates(0, min(kHeads, per));
 
   // keys and queries: 8 channels a thread, kLpt threads a token
   {
-    constexpr int kLpt = kPacks, kGroups = kPrepThreads / kLpt, kTok = kC > kGroups ? kC / kGroups : 1;
-    const int p = tid % kLpt, t0 = tid / kLpt * kTok;
+    constexpr int kLpt = kPacks, kGroups = kPrepThreads / kLpt, kTok = kC / kGroups;
+    static_assert(kTok * kGroups == kC, "every thread has tokens");
+    const int p = tid % kLpt, t0 = tid / kLpt * kTok, c8 = min(p * 8, dk - 8);
+    const bool in = p * 8 < dk;
+    float win[2][kTok + 3][8];
 #pragma unroll
     for (int isq = 0; isq < 2; ++isq) {
-      const TIn* x = reinterpret_cast<const TIn*>(isq ? a.q : a.k);
-      const int c0 = (isq ? hk : a.Hk + hk) * dk + p * 8;  // conv channel
-      const bool in = p * 8 < dk && t0 < kC;
-      float win[kTok + 3][8], cw[8][4];
+      const TIn* x = reinterpret_cast<const TIn*>(isq ? a.q : a.k) + hk * dk + c8;
 #pragma unroll
       for (int i = 0; i < kTok + 3; ++i) {
-        const int t = t0 - 3 + i;  // of the chunk
-#pragma unroll
-        for (int e = 0; e < 8; ++e) win[i][e] = 0.0f;
-        if (!in || t >= nt) continue;
-        if (n0 + t >= 0) fetch8(x + (size_t(tk.first + n0 + t) * a.Hk + hk) * dk + p * 8, win[i]);
-        else fetch8(cs + size_t(n0 + t + 3) * C + c0, win[i]);
+        const int t = min(max(t0 - 3 + i, n0 ? -3 : 0), nt - 1);
+        fetch8(x + (long long)(row0 + t) * a.Hk * dk, win[isq][i]);
       }
+    }
+    if (n0 == 0 && t0 < 3) {  // before the sequence's first token
 #pragma unroll
-      for (int e = 0; e < 8; ++e) {
-        const float4 y = in ? *reinterpret_cast<const float4*>(a.conv_w + size_t(c0 + e) * 4) : make_float4(0, 0, 0, 0);
-        cw[e][0] = y.x, cw[e][1] = y.y, cw[e][2] = y.z, cw[e][3] = y.w;
-      }
+      for (int isq = 0; isq < 2; ++isq)
+#pragma unroll
+        for (int i = 0; i < 3; ++i)
+          if (t0 + i < 3) fetch8(cs + size_t(t0 + i) * C + (isq ? hk : a.Hk + hk) * dk + c8, win[isq][i]);
+    }
+#pragma unroll
+    for (int isq = 0; isq < 2; ++isq) {
+      float4 cw[8];
+#pragma unroll
+      for (int e = 0; e < 8; ++e)
+        cw[e] = *reinterpret_cast<const float4*>(a.conv_w + size_t((isq ? hk : a.Hk + hk) * dk + c8 + e) * 4);
 #pragma unroll
       for (int i = 0; i < kTok; ++i) {
         float y[8], sum = 0.0f;
 #pragma unroll
         for (int e = 0; e < 8; ++e) {
-          y[e] = silu(cw[e][0] * win[i][e] + cw[e][1] * win[i + 1][e] + cw[e][2] * win[i + 2][e] + cw[e][3] * win[i + 3][e]);
+          const auto& x = win[isq];
+          y[e] = silu(cw[e].x * x[i][e] + cw[e].y * x[i + 1][e] + cw[e].z * x[i + 2][e] + cw[e].w * x[i + 3][e]);
+          if (!in || t0 + i >= nt) y[e] = 0.0f;
           sum += y[e] * y[e];
         }
-        const float inv = t0 + i < nt ? rsqrt_hw(group_sum<kLpt>(sum) + 1e-6f) * kUnit : 0.0f;
-        const Pair x8 = split(y, inv);
-        if (t0 < kC) {
-          char* d = s_kq + isq * 2 * P::kPlane + (p * (kC + 1) + t0 + i) * 16;
-          *reinterpret_cast<f16x8*>(d) = x8.hi;
-          *reinterpret_cast<f16x8*>(d + P::kPlane) = x8.lo;
-        }
+        const Pair x8 = split(y, rsqrt_hw(group_sum<kLpt>(sum) + 1e-6f) * kUnit);
+        char* d = s_kq + isq * 2 * P::kPlane + (p * (kC + 1) + t0 + i) * 16;
+        *reinterpret_cast<f16x8*>(d) = x8.hi;
+        *reinterpret_cast<f16x8*>(d + P::kPlane) = x8.lo;
       }
     }
   }
@@ -253,35 +278,42 @@ __global__ __launch_bounds__(kPrepThreads, 2) void chunk_kernel(ChainArgs a, Par
     for (int s = 0; s < kKs; ++s) c = mma3(rows_of(0, ti, s), rows_of(isq, tj, s), c);
     return c;
   };
-  // k_j.q_i with the queries as columns: unit w of Y, two tiles of keys
-  f32x4 kq[2] = {};
-  if (w < 6) {
-    kq[0] = gram(1, 2 * lower_col(w), lower_tile(w));
-    if (2 * lower_col(w) + 1 <= lower_tile(w)) kq[1] = gram(1, 2 * lower_col(w) + 1, lower_tile(w));
-  }
-  // k_i.k_j, the ten tiles of the lower triangle
-  for (int u = w < 4 ? w : w >= 6 ? 4 + (w - 6) * 3 : 10, n = w < 4 ? 1 : w >= 6 ? 3 : 0; n > 0; --n, ++u) {
-    const int ti = u < 1 ? 0 : u < 3 ? 1 : u < 6 ? 2 : 3, tj = u - ti * (ti + 1) / 2;
-    const f32x4 c = gram(0, ti, tj);
+  // k_j.q_i with the queries as columns: units w and w + 4 of Y, two tiles of
+  // keys each (what is above the diagonal stays 0)
+  f32x4 kq[2][2] = {};
 #pragma unroll
-    for (int r = 0; r < 4; ++r) s_g[(16 * ti + 4 * q4 + r) * kLd + 16 * tj + n16] = c[r] * (1.0f / (kUnit * kUnit));
+  for (int n = 0; n < 2; ++n) {
+    const int u = w + 4 * n;
+    if (u >= 6) continue;
+    kq[n][0] = gram(1, 2 * lower_col(u), lower_tile(u));
+    if (2 * lower_col(u) + 1 <= lower_tile(u)) kq[n][1] = gram(1, 2 * lower_col(u) + 1, lower_tile(u));
+  }
+  // k_i.k_j, the ten tiles of the lower triangle: 2, 1, 3 and 4 of them
+  f32x4 kk[4];
+  const int first_kk = w == 0 ? 0 : w == 1 ? 2 : w == 2 ? 3 : 6, many_kk = w == 0 ? 2 : w == 1 ? 1 : w + 1;
+#pragma unroll
+  for (int n = 0; n < 4; ++n) {
+    const int u = first_kk + n, ti = u < 1 ? 0 : u < 3 ? 1 : u < 6 ? 2 : 3;
+    if (n < many_kk) kk[n] = gram(0, ti, u - ti * (ti + 1) / 2);
   }
   // K^T: rows are channels, 32 tokens; Q: rows are tokens, 32 channels; both in
-  // the order of accumulators
+  // the order of accumulators.  A wave keeps the channels of one step of W.
   char* kws = key_at(a, slot, hk);
   const size_t kt_at = size_t(kKs) * 8 * kFrag;
-  for (int u = w; u < DKP / 16 * 2; u += kPrepWaves) {
-    const int c = u / 2 * 16 + n16, s = u % 2;
-    Pair x;
+  Pair kt[4];  // [tile of 16 channels][token step]
+  if (w < kKs) {
 #pragma unroll
-    for (int j = 0; j < 8; ++j) {
-      const int t = 32 * s + 16 * (j / 4) + 4 * q4 + j % 4;
-      const char* d = s_kq + (c / 8 * (kC + 1) + t) * 16 + c % 8 * 2;
-      x.hi[j] = *reinterpret_cast<const _Float16*>(d);
-      x.lo[j] = *reinterpret_cast<const _Float16*>(d + P::kPlane);
+    for (int u = 0; u < 4; ++u) {
+      const int c = 32 * w + u / 2 * 16 + n16, s = u % 2;
+#pragma unroll
+      for (int j = 0; j < 8; ++j) {
+        const int t = 32 * s + 16 * (j / 4) + 4 * q4 + j % 4;
+        const char* d = s_kq + (c / 8 * (kC + 1) + t) * 16 + c % 8 * 2;
+        kt[u].hi[j] = *reinterpret_cast<const _Float16*>(d);
+        kt[u].lo[j] = *reinterpret_cast<const _Float16*>(d + P::kPlane);
+      }
+      store_pair(kws + kt_at, w * 4 + u, lane, kt[u]);
     }
-    store_pair(s_kt, u, lane, x);
-    store_pair(kws + kt_at, u, lane, x);
   }
   for (int u = w; u < kKs * 4; u += kPrepWaves) {
     const int s = u / 4, t = u % 4;
@@ -299,14 +331,19 @@ __global__ __launch_bounds__(kPrepThreads, 2) void chunk_kernel(ChainArgs a, Par
     }
     store_pair(kws, u, lane, x);
   }
+  __syncthreads();  // K and Q are read
+#pragma unroll
+  for (int n = 0; n < 4; ++n) {
+    const int u = first_kk + n, ti = u < 1 ? 0 : u < 3 ? 1 : u < 6 ? 2 : 3, tj = u - ti * (ti + 1) / 2;
+    if (n >= many_kk) continue;
+#pragma unroll
+    for (int r = 0; r < 4; ++r) s_g[(16 * ti + 4 * q4 + r) * kLd + 16 * tj + n16] = kk[n][r] * (1.0f / (kUnit * kUnit));
+  }
 
   for (int r0 = 0; r0 < per; r0 += kHeads) {
     const int nr = min(kHeads, per - r0);
-    __syncthreads();  // K and Q, or the last heads' matrices, are read
-    if (w < nr) {     // decays of a head, a token a lane
-      const size_t at = size_t(tk.first + n0 + (lane < nt ? lane : 0)) * a.Hv + hk * per + r0 + w;
-      const float al = lane < nt ? to_f32(reinterpret_cast<const TIn*>(a.alpha)[at]) : 1.0f;
-      const float be = lane < nt ? to_f32(reinterpret_cast<const TIn*>(a.beta)[at]) : 0.0f;
+    if (r0) fetch_gates(r0, nr);
+    if (w < nr) {
       // 64-bit sums: far into a chunk of strong decays the difference of two of
       // them is small
       double g = double(logf(al < 0x1p-126f ? 0x1p-126f : al));
@@ -320,39 +357,41 @@ __global__ __launch_bounds__(kPrepThreads, 2) void chunk_kernel(ChainArgs a, Par
       s_beta[w * kC + lane] = be;
     }
     __syncthreads();
-    for (int u = tid; u < nr * kC * kC; u += kPrepThreads) {
-      const int r = u / (kC * kC), i = u / kC % kC, j = u % kC;
-      s_t[(r * kC + i) * kLd + j] =
-          j < i ? s_beta[r * kC + i] * s_g[i * kLd + j] * __expf(float(s_log[r * kC + i] - s_log[r * kC + j])) : 0.0f;
-    }
-    __syncthreads();
-    // inverses of the blocks of the diagonal: a block per 16 lanes, a column a lane
-    if (w < nr) {
-      float* x = s_t + (w * kC + 16 * q4) * kLd + 16 * q4;
-      float t[16];
+    for (int r = 0; r < nr; ++r) {  // a column a lane, every fourth row a wave
+      const double lj = s_log[r * kC + lane];
 #pragma unroll
-      for (int i = 0; i < 16; ++i) {
-        float y = i == n16 ? 1.0f : 0.0f;
-#pragma unroll
-        for (int j = 0; j < i; j += 4) {
-          const float4 l = *reinterpret_cast<const float4*>(x + i * kLd + j);
-          y -= l.x * t[j];
-          if (j + 1 < i) y -= l.y * t[j + 1];
-          if (j + 2 < i) y -= l.z * t[j + 2];
-          if (j + 3 < i) y -= l.w * t[j + 3];
-        }
-        t[i] = y;
+      for (int n = 0; n < kC / kPrepWaves; ++n) {
+        const int i = n * kPrepWaves + w;
+        s_t[(r * kC + i) * kLd + lane] =
+            lane < i ? s_beta[r * kC + i] * s_g[i * kLd + lane] * __expf(float(s_log[r * kC + i] - lj)) : 0.0f;
       }
-      __builtin_amdgcn_wave_barrier();  // rows are read before they are replaced
-#pragma unroll
-      for (int i = 0; i < 16; ++i) x[i * kLd + n16] = t[i];
     }
     __syncthreads();
-    // blocks below: X_j = T_jj, X_i = -T_ii sum_k A_ik X_k down the column of
-    // blocks j; two waves a head, columns 0, and 1 and 2
-    f32x4 low[3];  // blocks (1, 0), (2, 0), (3, 0), or (2, 1), (3, 1), (3, 2)
-    if (w < 2 * nr) {
-      const float* x = s_t + w / 2 * kC * kLd;
+    // (I + A)^-1 of a head by one wave
+    if (w < nr) {
+      // blocks of the diagonal: a block per 16 lanes, a column a lane
+      float* x = s_t + w * kC * kLd;
+      {
+        float *d = x + 16 * q4 * kLd + 16 * q4, t[16];
+#pragma unroll
+        for (int i = 0; i < 16; ++i) {
+          float y = i == n16 ? 1.0f : 0.0f;
+#pragma unroll
+          for (int j = 0; j < i; j += 4) {
+            const float4 l = *reinterpret_cast<const float4*>(d + i * kLd + j);
+            y -= l.x * t[j];
+            if (j + 1 < i) y -= l.y * t[j + 1];
+            if (j + 2 < i) y -= l.z * t[j + 2];
+            if (j + 3 < i) y -= l.w * t[j + 3];
+          }
+          t[i] = y;
+        }
+        __builtin_amdgcn_wave_barrier();  // rows are read before they are replaced
+#pragma unroll
+        for (int i = 0; i < 16; ++i) d[i * kLd + n16] = t[i];
+      }
+      __builtin_amdgcn_wave_barrier();
+      // blocks below: X_j = T_jj, X_i = -T_ii sum_k A_ik X_k down a column of blocks
       auto block = [&](int i, int k) { return *reinterpret_cast<const f32x4*>(x + (16 * i + n16) * kLd + 16 * k + 4 * q4); };
       auto diagonal = [&](int j) {
         f32x4 c;
@@ -365,28 +404,21 @@ __global__ __launch_bounds__(kPrepThreads, 2) void chunk_kernel(ChainArgs a, Par
         for (int r = 0; r < 4; ++r) c = __builtin_amdgcn_mfma_f32_16x16x4f32(y[r], z[r], c, 0, 0, 0);
         return c;
       };
-      const f32x4 zero = {};
-      if (w % 2 == 0) {
-        const f32x4 x0 = diagonal(0);
-        low[0] = -times(block(1, 1), times(block(1, 0), x0, zero), zero);
-        low[1] = -times(block(2, 2), times(block(2, 1), low[0], times(block(2, 0), x0, zero)), zero);
-        low[2] = -times(block(3, 3), times(block(3, 2), low[1], times(block(3, 1), low[0], times(block(3, 0), x0, zero))), zero);
-      } else {
-        const f32x4 x1 = diagonal(1), x2 = diagonal(2);
-        low[0] = -times(block(2, 2), times(block(2, 1), x1, zero), zero);
-        low[1] = -times(block(3, 3), times(block(3, 2), low[0], times(block(3, 1), x1, zero)), zero);
-        low[2] = -times(block(3, 3), times(block(3, 2), x2, zero), zero);
-      }
-    }
-    __syncthreads();
-    if (w < 2 * nr) {
-      float* x = s_t + w / 2 * kC * kLd;
+      const f32x4 zero = {}, a10 = block(1, 0), a20 = block(2, 0), a21 = block(2, 1), a30 = block(3, 0), a31 = block(3, 1),
+                  a32 = block(3, 2), t1 = block(1, 1), t2 = block(2, 2), t3 = block(3, 3);
+      const f32x4 x0 = diagonal(0), x1 = diagonal(1), x2 = diagonal(2);
+      const f32x4 x10 = -times(t1, times(a10, x0, zero), zero), x21 = -times(t2, times(a21, x1, zero), zero),
+                  x32 = -times(t3, times(a32, x2, zero), zero);
+      const f32x4 x20 = -times(t2, times(a21, x10, times(a20, x0, zero)), zero),
+                  x31 = -times(t3, times(a32, x21, times(a31, x1, zero)), zero);
+      const f32x4 x30 = -times(t3, times(a32, x20, times(a31, x10, times(a30, x0, zero))), zero);
+      __builtin_amdgcn_wave_barrier();
+      auto put_block = [&](int i, int j, f32x4 c) {
 #pragma unroll
-      for (int n = 0; n < 3; ++n) {
-        const int i = w % 2 == 0 ? n + 1 : n == 0 ? 2 : 3, j = w % 2 == 0 ? 0 : n == 2 ? 2 : 1;
-#pragma unroll
-        for (int r = 0; r < 4; ++r) x[(16 * i + 4 * q4 + r) * kLd + 16 * j + n16] = low[n][r];
-      }
+        for (int r = 0; r < 4; ++r) x[(16 * i + 4 * q4 + r) * kLd + 16 * j + n16] = c[r];
+      };
+      put_block(1, 0, x10), put_block(2, 1, x21), put_block(3, 2, x32);
+      put_block(2, 0, x20), put_block(3, 1, x31), put_block(3, 0, x30);
     }
     __syncthreads();
 
@@ -395,33 +427,28 @@ __global__ __launch_bounds__(kPrepThreads, 2) void chunk_kernel(ChainArgs a, Par
       char* vws = value_at(a, slot, h);
       const float *t = s_t + r * kC * kLd, *beta = s_beta + r * kC, *decay = s_decay + r * kC;
       const double* lg = s_log + r * kC;
-      // values of channel 16 w + n16 in operand order
-      float v[2][8] = {};
-      if (16 * w < dv) {
-        const int c = h * dv + 16 * w + n16;
-        const TIn* x = reinterpret_cast<const TIn*>(a.v) + size_t(tk.first + n0) * a.Hv * dv + c;
-        const float4 cw = *reinterpret_cast<const float4*>(a.conv_w + (size_t(2) * a.Hk * dk + c) * 4);
+      // raw values of channels 32 w + 2 n16 and the next (16 channels: of 0 .. 15
+      // twice), on their way while W and Y are computed
+      const bool own_v = 32 * w < dv;
+      const int c2 = h * dv + (dv == 16 ? 2 * (n16 % 8) : 32 * w + 2 * n16);
+      decltype(fetch2(static_cast<const TIn*>(nullptr))) raw[2][2][7];
+      if (own_v) {
+        // rows from 3 before the chunk, by 32-bit offsets (67 rows stay below 2^32 bytes)
+        const char* x = reinterpret_cast<const char*>(reinterpret_cast<const TIn*>(a.v) + ((long long)(row0) - 3) * a.Hv * dv);
+        const unsigned stride = unsigned(a.Hv) * dv * sizeof(TIn);
 #pragma unroll
         for (int s = 0; s < 2; ++s)
 #pragma unroll
-          for (int e = 0; e < 2; ++e) {
-            const int t0 = 32 * s + 16 * e + 4 * q4;
-            float win[7];
+          for (int e = 0; e < 2; ++e)
 #pragma unroll
             for (int i = 0; i < 7; ++i) {
-              const int n = t0 - 3 + i;
-              win[i] = 0.0f;
-              if (n >= nt) continue;
-              if (n0 + n >= 0) win[i] = to_f32(x[(long long)(n) * a.Hv * dv]);
-              else win[i] = cs[size_t(n0 + n + 3) * C + 2 * a.Hk * dk + c];
+              const unsigned n = min(max(32 * s + 16 * e + 4 * q4 + i, n0 ? 0 : 3), nt + 2);
+              raw[s][e][i] = fetch2(reinterpret_cast<const TIn*>(x + size_t(n * stride + c2 * unsigned(sizeof(TIn)))));
             }
-#pragma unroll
-            for (int i = 0; i < 4; ++i)
-              v[s][4 * e + i] = t0 + i < nt ? silu(cw.x * win[i] + cw.y * win[i + 1] + cw.z * win[i + 2] + cw.w * win[i + 3]) : 0.0f;
-          }
       }
+      __builtin_amdgcn_sched_barrier(0);  // registers: one part after the other
       // (I + A)^-1 diag(beta): rows n16 of tile t, columns in operand order
-      float inv[6][8];
+      float inv[6][8], mt = 0.0f, bound[4] = {}, sw[4], iw[4];
 #pragma unroll
       for (int u = 0; u < 6; ++u) {
         const int i = 16 * lower_tile(u) + n16, j = 32 * lower_col(u) + 4 * q4;
@@ -429,88 +456,120 @@ __global__ __launch_bounds__(kPrepThreads, 2) void chunk_kernel(ChainArgs a, Par
         for (int e = 0; e < 2; ++e) {
           const float4 x = *reinterpret_cast<const float4*>(t + i * kLd + j + 16 * e);
           const float4 y = *reinterpret_cast<const float4*>(beta + j + 16 * e);
+          const float4 z = *reinterpret_cast<const float4*>(decay + j + 16 * e);
           inv[u][4 * e] = x.x * y.x, inv[u][4 * e + 1] = x.y * y.y, inv[u][4 * e + 2] = x.z * y.z, inv[u][4 * e + 3] = x.w * y.w;
+          const float* f = &inv[u][4 * e];
+          mt = fmaxf(mt, fmaxf(fmaxf(fabsf(f[0]), fabsf(f[1])), fmaxf(fabsf(f[2]), fabsf(f[3]))));
+          bound[lower_tile(u)] += fabsf(f[0] * z.x) + fabsf(f[1] * z.y) + (fabsf(f[2] * z.z) + fabsf(f[3] * z.w));
         }
       }
-      if (16 * w < dv) {  // U: rows are tokens, columns this wave's channels
-        float mt = 0.0f, mv = 0.0f, st, it, sv, iv;
-#pragma unroll
-        for (int u = 0; u < 6; ++u)
-#pragma unroll
-          for (int e = 0; e < 8; ++e) mt = fmaxf(mt, fabsf(inv[u][e]));
-#pragma unroll
-        for (int e = 0; e < 8; ++e) mv = fmaxf(mv, fmaxf(fabsf(v[0][e]), fabsf(v[1][e])));
-        f16_scale(column_max(group_max<16>(mt)), st, it);
-        f16_scale(column_max(mv), sv, iv);
-        const Pair v0 = split(v[0], sv), v1 = split(v[1], sv);
-        char* u_out = vws + slot_layout(a.Hk, a.Hv, dk, dv).u_at() + size_t(w) * 4 * kFrag;
-#pragma unroll
-        for (int tt = 0; tt < 4; ++tt) {
-          f32x4 c = mma3(split(inv[lower_step(tt, 0)], st), v0, f32x4{});
-          if (tt >= 2) c = mma3(split(inv[lower_step(tt, 1)], st), v1, c);
-          c *= it;  // the two scales apart: their product may leave the range
-          c *= iv;
-          *reinterpret_cast<f32x4*>(u_out + tt * kFrag + lane * 16) = c;
-        }
-      }
-      // (I + A)^-1 diag(beta e^g), and W = that times K: |W| of a row is at most
-      // the sum of the row
-      float bound[4] = {}, sw[4], iw[4];
-#pragma unroll
-      for (int u = 0; u < 6; ++u)
-#pragma unroll
-        for (int e = 0; e < 2; ++e) {
-          const float4 y = *reinterpret_cast<const float4*>(decay + 32 * lower_col(u) + 4 * q4 + 16 * e);
-          inv[u][4 * e] *= y.x, inv[u][4 * e + 1] *= y.y, inv[u][4 * e + 2] *= y.z, inv[u][4 * e + 3] *= y.w;
-#pragma unroll
-          for (int i = 0; i < 4; ++i) bound[lower_tile(u)] += fabsf(inv[u][4 * e + i]);
-        }
+      // W = (I + A)^-1 diag(beta e^g) K: |W| of a row is at most the sum of the
+      // inverse's
 #pragma unroll
       for (int tt = 0; tt < 4; ++tt) {
         f16_scale(column_sum(bound[tt]), sw[tt], iw[tt]);
         if (w == 0 && q4 == 0) s_row[r * kC + 16 * tt + n16] = iw[tt];
       }
-      if (w < 2 * kKs) {
-        const int s = w / 2;
-        auto w_tile = [&](int tt, float scale, const Pair& x0, const Pair& x1) {
-          f32x4 c[2];
+      if (w < kKs) {
+        float4 z[2][2];
 #pragma unroll
-          for (int e = 0; e < 2; ++e) {
-            c[e] = mma3(load_pair(s_kt, (2 * s + e) * 2, lane), x0, f32x4{});
-            if (tt >= 2) c[e] = mma3(load_pair(s_kt, (2 * s + e) * 2 + 1, lane), x1, c[e]);
+        for (int s = 0; s < 2; ++s)
+#pragma unroll
+          for (int e = 0; e < 2; ++e) z[s][e] = *reinterpret_cast<const float4*>(decay + 32 * s + 4 * q4 + 16 * e);
+#pragma unroll
+        for (int tt = 0; tt < 4; ++tt) {
+          f32x4 c[2] = {};
+#pragma unroll
+          for (int s = 0; s <= tt / 2; ++s) {
+            const float* f = inv[lower_step(tt, s)];
+            const float4 z0 = z[s][0], z1 = z[s][1];
+            const float y[8] = {f[0] * z0.x, f[1] * z0.y, f[2] * z0.z, f[3] * z0.w, f[4] * z1.x, f[5] * z1.y, f[6] * z1.z, f[7] * z1.w};
+            const Pair x = split(y, sw[tt]);
+#pragma unroll
+            for (int e = 0; e < 2; ++e) c[e] = mma3(kt[2 * e + s], x, c[e]);
           }
           const float y[8] = {c[0][0], c[0][1], c[0][2], c[0][3], c[1][0], c[1][1], c[1][2], c[1][3]};
-          store_pair(vws, s * 4 + tt, lane, split(y, 1.0f / kUnit));
-        };
-        if (w % 2 == 0) {
-          w_tile(0, sw[0], split(inv[0], sw[0]), Pair{});
-          w_tile(3, sw[3], split(inv[4], sw[3]), split(inv[5], sw[3]));
-        } else {
-          w_tile(1, sw[1], split(inv[1], sw[1]), Pair{});
-          w_tile(2, sw[2], split(inv[2], sw[2]), split(inv[3], sw[2]));
+          store_pair(vws, w * 4 + tt, lane, split(y, 1.0f / kUnit));
         }
       }
-      if (w < 6) {  // Y
-        const int i = 16 * lower_tile(w) + n16;
+      __builtin_amdgcn_sched_barrier(0);
+#pragma unroll
+      for (int n = 0; n < 2; ++n) {  // Y
+        const int u = w + 4 * n, i = 16 * lower_tile(u) + n16;
+        if (u >= 6) continue;
+        const double li = lg[i];
         float y[8];
 #pragma unroll
         for (int e = 0; e < 8; ++e) {
-          const int j = 32 * lower_col(w) + 16 * (e / 4) + 4 * q4 + e % 4;
-          y[e] = j <= i ? kq[e / 4][e % 4] * __expf(float(lg[i] - lg[j])) : 0.0f;
+          const int j = 32 * lower_col(u) + 16 * (e / 4) + 4 * q4 + e % 4;
+          y[e] = j <= i ? kq[n][e / 4][e % 4] * __expf(float(li - lg[j])) : 0.0f;
         }
-        store_pair(vws + slot_layout(a.Hk, a.Hv, dk, dv).y_at(), w, lane, split(y, 1.0f / kUnit));
+        store_pair(vws + layout.y_at(), u, lane, split(y, 1.0f / kUnit));
       }
-      if (w == 7) {  // a token a lane; the decay to the chunk's end
-        float* sc = reinterpret_cast<float*>(vws + slot_layout(a.Hk, a.Hv, dk, dv).scalars_at());
+      if (w == 3) {  // a token a lane; the decay to the chunk's end
+        float* sc = reinterpret_cast<float*>(vws + layout.scalars_at());
         sc[kC + lane] = decay[lane];
         sc[2 * kC + lane] = __expf(float(lg[kC - 1] - lg[lane]));
         if (lane == 0) sc[3 * kC] = decay[kC - 1];
       }
-      if (w == 0) {
-        float* sc = reinterpret_cast<float*>(vws + slot_layout(a.Hk, a.Hv, dk, dv).scalars_at());
-        sc[lane] = s_row[r * kC + lane];
+      if (w == 0) reinterpret_cast<float*>(vws + layout.scalars_at())[lane] = s_row[r * kC + lane];
+      __builtin_amdgcn_sched_barrier(0);
+      if (own_v) {  // U: rows are tokens, columns this wave's channels
+        float v[2][2][8];  // [channel][step]
+        float2 old[3];     // before the chunk
+#pragma unroll
+        for (int i = 0; i < 3; ++i) old[i] = make_float2(one_of(raw[0][0][i], 0), one_of(raw[0][0][i], 1));
+        if (n0 == 0 && q4 == 0) {
+#pragma unroll
+          for (int i = 0; i < 3; ++i) old[i] = *reinterpret_cast<const float2*>(cs + 2 * a.Hk * dk + c2 + size_t(i) * C);
+        }
+#pragma unroll
+        for (int c = 0; c < 2; ++c) {
+          const float4 cw = *reinterpret_cast<const float4*>(a.conv_w + (size_t(2) * a.Hk * dk + c2 + c) * 4);
+#pragma unroll
+          for (int s = 0; s < 2; ++s)
+#pragma unroll
+            for (int e = 0; e < 2; ++e)
+#pragma unroll
+              for (int i = 0; i < 4; ++i) {
+                auto x = [&](int k) { return s + e == 0 && i + k < 3 ? one_of(old[i + k], c) : one_of(raw[s][e][i + k], c); };
+                v[c][s][4 * e + i] = silu(cw.x * x(0) + cw.y * x(1) + cw.z * x(2) + cw.w * x(3));
+              }
+        }
+        float st, it, sv[2], iv[2];
+        f16_scale(column_max(group_max<16>(mt)), st, it);
+        Pair vp[2][2];
+#pragma unroll
+        for (int c = 0; c < 2; ++c) {
+          float mv = 0.0f;
+#pragma unroll
+          for (int e = 0; e < 8; ++e) mv = fmaxf(mv, fmaxf(fabsf(v[c][0][e]), fabsf(v[c][1][e])));
+          f16_scale(column_max(mv), sv[c], iv[c]);
+#pragma unroll
+          for (int s = 0; s < 2; ++s) vp[c][s] = split(v[c][s], sv[c]);
+        }
+#pragma unroll
+        for (int tt = 0; tt < 4; ++tt) {
+          f32x4 x[2] = {};
+#pragma unroll
+          for (int s = 0; s <= tt / 2; ++s) {
+            const Pair y = split(inv[lower_step(tt, s)], st);
+#pragma unroll
+            for (int c = 0; c < 2; ++c) x[c] = mma3(y, vp[c][s], x[c]);
+          }
+#pragma unroll
+          for (int c = 0; c < 2; ++c) {
+            // the two scales apart: their product may leave the range
+            x[c] *= it;
+            x[c] *= iv[c];
+            const int ch = c2 - h * dv + c;
+            char* d = vws + layout.u_at() + (size_t(ch / 16) * 4 + tt) * kFrag + (16 * q4 + ch % 16) * 16;
+            *reinterpret_cast<f32x4*>(d) = x[c];  // of 16 channels each is written twice, the same
+          }
+        }
       }
     }
+    __syncthreads();  // the matrices are read
   }
 }
 
