@@ -170,7 +170,7 @@ struct Prep {
   static constexpr int kPacks = DKP / 8, kKs = DKP / 32;
   static constexpr int kPlane = kPacks * (kC + 1) * 16;       // bytes of hi or lo of K or Q: [pack][token]
   static constexpr int kMat = kC * kLd * int(sizeof(float));  // a chunk's matrix
-  static constexpr int kRows = 4 * kPlane > (kHeads + 1) * kMat ? 4 * kPlane : (kHeads + 1) * kMat;
+  static constexpr int kRows = 4 * kPlane > kHeads * kMat ? 4 * kPlane : kHeads * kMat;
   static constexpr int kLds = kRows + kHeads * kC * 20;
 };
 
@@ -191,9 +191,8 @@ __global__ __launch_bounds__(kPrepThreads, 2) void chunk_kernel(ChainArgs a, Par
   typedef Prep<DKP> P;
   constexpr int kKs = P::kKs, kPacks = P::kPacks;
   extern __shared__ __align__(16) char s_raw[];
-  char* s_kq = s_raw;                               // K hi, K lo, Q hi, Q lo; then
-  float* s_g = reinterpret_cast<float*>(s_raw);     // [64][kLd]: k_i.k_j, and
-  float* s_t = s_g + kC * kLd;                      // [head][64][kLd]
+  char* s_kq = s_raw;                            // K hi, K lo, Q hi, Q lo; then the heads' matrices
+  float* s_t = reinterpret_cast<float*>(s_raw);  // [head][64][kLd]
   double* s_log = reinterpret_cast<double*>(s_raw + P::kRows);  // [head][64]
   float* s_decay = reinterpret_cast<float*>(s_log + kHeads * kC);  // e^g
   float* s_beta = s_decay + kHeads * kC;
@@ -272,29 +271,25 @@ __global__ __launch_bounds__(kPrepThreads, 2) void chunk_kernel(ChainArgs a, Par
     const char* d = s_kq + isq * 2 * P::kPlane + ((4 * s + q4) * (kC + 1) + 16 * t + n16) * 16;
     return Pair{*reinterpret_cast<const f16x8*>(d), *reinterpret_cast<const f16x8*>(d + P::kPlane)};
   };
-  auto gram = [&](int isq, int ti, int tj) {  // rows: keys of tile ti, columns: keys or queries of tile tj
-    f32x4 c = {};
-#pragma unroll
-    for (int s = 0; s < kKs; ++s) c = mma3(rows_of(0, ti, s), rows_of(isq, tj, s), c);
-    return c;
-  };
-  // k_j.q_i with the queries as columns: units w and w + 4 of Y, two tiles of
-  // keys each (what is above the diagonal stays 0)
-  f32x4 kq[2][2] = {};
+  // k_j.k_i and k_j.q_i, rows j, columns i, in the units of a lower triangular
+  // operand: w and w + 4 (what is above the diagonal stays 0)
+  f32x4 kk[2][2] = {}, kq[2][2] = {};
 #pragma unroll
   for (int n = 0; n < 2; ++n) {
-    const int u = w + 4 * n;
+    const int u = w + 4 * n, t = lower_tile(u);
     if (u >= 6) continue;
-    kq[n][0] = gram(1, 2 * lower_col(u), lower_tile(u));
-    if (2 * lower_col(u) + 1 <= lower_tile(u)) kq[n][1] = gram(1, 2 * lower_col(u) + 1, lower_tile(u));
-  }
-  // k_i.k_j, the ten tiles of the lower triangle: 2, 1, 3 and 4 of them
-  f32x4 kk[4];
-  const int first_kk = w == 0 ? 0 : w == 1 ? 2 : w == 2 ? 3 : 6, many_kk = w == 0 ? 2 : w == 1 ? 1 : w + 1;
 #pragma unroll
-  for (int n = 0; n < 4; ++n) {
-    const int u = first_kk + n, ti = u < 1 ? 0 : u < 3 ? 1 : u < 6 ? 2 : 3;
-    if (n < many_kk) kk[n] = gram(0, ti, u - ti * (ti + 1) / 2);
+    for (int s = 0; s < kKs; ++s) {
+      const Pair k = rows_of(0, t, s), q = rows_of(1, t, s);
+#pragma unroll
+      for (int e = 0; e < 2; ++e) {
+        const int j = 2 * lower_col(u) + e;
+        if (j > t) continue;
+        const Pair x = rows_of(0, j, s);
+        kk[n][e] = mma3(x, k, kk[n][e]);
+        kq[n][e] = mma3(x, q, kq[n][e]);
+      }
+    }
   }
   // K^T: rows are channels, 32 tokens; Q: rows are tokens, 32 channels; both in
   // the order of accumulators.  A wave keeps the channels of one step of W.
@@ -332,13 +327,27 @@ __global__ __launch_bounds__(kPrepThreads, 2) void chunk_kernel(ChainArgs a, Par
     store_pair(kws, u, lane, x);
   }
   __syncthreads();  // K and Q are read
+
+  // raw values of channels 32 w + 2 n16 and the next (16 channels: 0 .. 15
+  // twice) of a head, on their way while others are worked on
+  const bool own_v = 32 * w < dv;
+  const int ch = dv == 16 ? 2 * (n16 % 8) : 32 * w + 2 * n16;
+  decltype(fetch2(static_cast<const TIn*>(nullptr))) raw[2][2][7];
+  auto fetch_values = [&](int h) {
+    // rows from 3 before the chunk, by 32-bit offsets (67 rows stay below 2^32 bytes)
+    const char* x = reinterpret_cast<const char*>(reinterpret_cast<const TIn*>(a.v) + ((long long)(row0) - 3) * a.Hv * dv + h * dv);
+    const unsigned stride = unsigned(a.Hv) * dv * sizeof(TIn);
+    const int t0 = opaque(4 * q4);  // addresses are computed here, not held
 #pragma unroll
-  for (int n = 0; n < 4; ++n) {
-    const int u = first_kk + n, ti = u < 1 ? 0 : u < 3 ? 1 : u < 6 ? 2 : 3, tj = u - ti * (ti + 1) / 2;
-    if (n >= many_kk) continue;
+    for (int s = 0; s < 2; ++s)
 #pragma unroll
-    for (int r = 0; r < 4; ++r) s_g[(16 * ti + 4 * q4 + r) * kLd + 16 * tj + n16] = kk[n][r] * (1.0f / (kUnit * kUnit));
-  }
+      for (int e = 0; e < 2; ++e)
+#pragma unroll
+        for (int i = 0; i < 7; ++i) {
+          const unsigned n = min(max(32 * s + 16 * e + t0 + i, n0 ? 0 : 3), nt + 2);
+          raw[s][e][i] = fetch2(reinterpret_cast<const TIn*>(x + size_t(n * stride + ch * unsigned(sizeof(TIn)))));
+        }
+  };
 
   for (int r0 = 0; r0 < per; r0 += kHeads) {
     const int nr = min(kHeads, per - r0);
@@ -357,20 +366,40 @@ __global__ __launch_bounds__(kPrepThreads, 2) void chunk_kernel(ChainArgs a, Par
       s_beta[w * kC + lane] = be;
     }
     __syncthreads();
-    for (int r = 0; r < nr; ++r) {  // a column a lane, every fourth row a wave
-      const double lj = s_log[r * kC + lane];
+    // A, to be inverted, and Y
+    for (int r = 0; r < nr; ++r) {
+      const double* lg = s_log + r * kC;
+      const int n16 = opaque(lane & 15), q4 = opaque(lane >> 4);
+      char* y_out = value_at(a, slot, hk * per + r0 + r) + layout.y_at();
 #pragma unroll
-      for (int n = 0; n < kC / kPrepWaves; ++n) {
-        const int i = n * kPrepWaves + w;
-        s_t[(r * kC + i) * kLd + lane] =
-            lane < i ? s_beta[r * kC + i] * s_g[i * kLd + lane] * __expf(float(s_log[r * kC + i] - lj)) : 0.0f;
+      for (int n = 0; n < 2; ++n) {
+        const int u = w + 4 * n, i = 16 * lower_tile(u) + n16, j0 = 32 * lower_col(u) + 4 * q4;
+        if (u >= 6) continue;
+        const double li = lg[i];
+        const float bi = s_beta[r * kC + i] * (1.0f / (kUnit * kUnit));
+        float y[8];
+#pragma unroll
+        for (int e = 0; e < 2; ++e) {
+          f32x4 x;
+#pragma unroll
+          for (int k = 0; k < 4; ++k) {
+            const int j = j0 + 16 * e + k;
+            const float f = j <= i ? __expf(float(li - lg[j])) : 0.0f;
+            x[k] = j < i ? bi * kk[n][e][k] * f : 0.0f;
+            y[4 * e + k] = kq[n][e][k] * f;
+          }
+          *reinterpret_cast<f32x4*>(s_t + (r * kC + i) * kLd + j0 + 16 * e) = x;
+        }
+        store_pair(y_out, u, lane, split(y, 1.0f / kUnit));
       }
     }
+    if (own_v) fetch_values(hk * per + r0);
     __syncthreads();
     // (I + A)^-1 of a head by one wave
     if (w < nr) {
       // blocks of the diagonal: a block per 16 lanes, a column a lane
       float* x = s_t + w * kC * kLd;
+      const int n16 = opaque(lane & 15), q4 = opaque(lane >> 4);  // as above
       {
         float *d = x + 16 * q4 * kLd + 16 * q4, t[16];
 #pragma unroll
@@ -427,26 +456,7 @@ __global__ __launch_bounds__(kPrepThreads, 2) void chunk_kernel(ChainArgs a, Par
       char* vws = value_at(a, slot, h);
       const float *t = s_t + r * kC * kLd, *beta = s_beta + r * kC, *decay = s_decay + r * kC;
       const double* lg = s_log + r * kC;
-      // raw values of channels 32 w + 2 n16 and the next (16 channels: of 0 .. 15
-      // twice), on their way while W and Y are computed
-      const bool own_v = 32 * w < dv;
-      const int c2 = h * dv + (dv == 16 ? 2 * (n16 % 8) : 32 * w + 2 * n16);
-      decltype(fetch2(static_cast<const TIn*>(nullptr))) raw[2][2][7];
-      if (own_v) {
-        // rows from 3 before the chunk, by 32-bit offsets (67 rows stay below 2^32 bytes)
-        const char* x = reinterpret_cast<const char*>(reinterpret_cast<const TIn*>(a.v) + ((long long)(row0) - 3) * a.Hv * dv);
-        const unsigned stride = unsigned(a.Hv) * dv * sizeof(TIn);
-#pragma unroll
-        for (int s = 0; s < 2; ++s)
-#pragma unroll
-          for (int e = 0; e < 2; ++e)
-#pragma unroll
-            for (int i = 0; i < 7; ++i) {
-              const unsigned n = min(max(32 * s + 16 * e + 4 * q4 + i, n0 ? 0 : 3), nt + 2);
-              raw[s][e][i] = fetch2(reinterpret_cast<const TIn*>(x + size_t(n * stride + c2 * unsigned(sizeof(TIn)))));
-            }
-      }
-      __builtin_amdgcn_sched_barrier(0);  // registers: one part after the other
+      const int n16 = opaque(lane & 15), q4 = opaque(lane >> 4);
       // (I + A)^-1 diag(beta): rows n16 of tile t, columns in operand order
       float inv[6][8], mt = 0.0f, bound[4] = {}, sw[4], iw[4];
 #pragma unroll
@@ -492,20 +502,6 @@ __global__ __launch_bounds__(kPrepThreads, 2) void chunk_kernel(ChainArgs a, Par
           store_pair(vws, w * 4 + tt, lane, split(y, 1.0f / kUnit));
         }
       }
-      __builtin_amdgcn_sched_barrier(0);
-#pragma unroll
-      for (int n = 0; n < 2; ++n) {  // Y
-        const int u = w + 4 * n, i = 16 * lower_tile(u) + n16;
-        if (u >= 6) continue;
-        const double li = lg[i];
-        float y[8];
-#pragma unroll
-        for (int e = 0; e < 8; ++e) {
-          const int j = 32 * lower_col(u) + 16 * (e / 4) + 4 * q4 + e % 4;
-          y[e] = j <= i ? kq[n][e / 4][e % 4] * __expf(float(li - lg[j])) : 0.0f;
-        }
-        store_pair(vws + layout.y_at(), u, lane, split(y, 1.0f / kUnit));
-      }
       if (w == 3) {  // a token a lane; the decay to the chunk's end
         float* sc = reinterpret_cast<float*>(vws + layout.scalars_at());
         sc[kC + lane] = decay[lane];
@@ -521,11 +517,11 @@ __global__ __launch_bounds__(kPrepThreads, 2) void chunk_kernel(ChainArgs a, Par
         for (int i = 0; i < 3; ++i) old[i] = make_float2(one_of(raw[0][0][i], 0), one_of(raw[0][0][i], 1));
         if (n0 == 0 && q4 == 0) {
 #pragma unroll
-          for (int i = 0; i < 3; ++i) old[i] = *reinterpret_cast<const float2*>(cs + 2 * a.Hk * dk + c2 + size_t(i) * C);
+          for (int i = 0; i < 3; ++i) old[i] = *reinterpret_cast<const float2*>(cs + 2 * a.Hk * dk + h * dv + ch + size_t(i) * C);
         }
 #pragma unroll
         for (int c = 0; c < 2; ++c) {
-          const float4 cw = *reinterpret_cast<const float4*>(a.conv_w + (size_t(2) * a.Hk * dk + c2 + c) * 4);
+          const float4 cw = *reinterpret_cast<const float4*>(a.conv_w + (size_t(2) * a.Hk * dk + h * dv + ch + c) * 4);
 #pragma unroll
           for (int s = 0; s < 2; ++s)
 #pragma unroll
@@ -536,6 +532,7 @@ __global__ __launch_bounds__(kPrepThreads, 2) void chunk_kernel(ChainArgs a, Par
                 v[c][s][4 * e + i] = silu(cw.x * x(0) + cw.y * x(1) + cw.z * x(2) + cw.w * x(3));
               }
         }
+        if (r + 1 < nr) fetch_values(h + 1);
         float st, it, sv[2], iv[2];
         f16_scale(column_max(group_max<16>(mt)), st, it);
         Pair vp[2][2];
@@ -562,8 +559,7 @@ __global__ __launch_bounds__(kPrepThreads, 2) void chunk_kernel(ChainArgs a, Par
             // the two scales apart: their product may leave the range
             x[c] *= it;
             x[c] *= iv[c];
-            const int ch = c2 - h * dv + c;
-            char* d = vws + layout.u_at() + (size_t(ch / 16) * 4 + tt) * kFrag + (16 * q4 + ch % 16) * 16;
+            char* d = vws + layout.u_at() + (size_t(ch / 16) * 4 + tt) * kFrag + (16 * q4 + ch % 16 + c) * 16;
             *reinterpret_cast<f32x4*>(d) = x[c];  // of 16 channels each is written twice, the same
           }
         }
