@@ -572,13 +572,30 @@ __global__ __launch_bounds__(kPrepThreads, 2) void chunk_kernel(ChainArgs a, Par
 // ---------------------------------------------------------------------------
 // The chunks of a sequence in turn.  A wave holds the state of 16 value
 // channels; the waves of a workgroup share the chunk's operands in LDS.
+//
+// Operands come into LDS past the registers, each into the place of the last
+// chunk's as soon as that is read: W and U behind V', Q and Y behind the
+// outputs, K^T behind the state.  A wave's loads and stores complete in order, so
+// each wait names how many were issued after what it needs (or fewer).  The
+// compiler has no loads of its own in the loop: it would wait for all.
 // ---------------------------------------------------------------------------
-template <int DKP>
+template <int DKP, int NW>
 struct Scan {
   static constexpr int kKs = DKP / 32;
-  static constexpr int kQ = kKs * 8 * kFrag;  // W first, the scalars behind Y
-  static constexpr int kLds = 3 * kQ + 13 * kFrag;
+  static constexpr int kQ = kKs * 8 * kFrag;  // bytes of Q, of K^T, of W
+  static constexpr int kY = 16 * kFrag;       // Y, and what follows, so that the waves have the same loads
+  static constexpr int kLds = 3 * kQ + kY + 2 * kFrag + NW * 4 * kFrag;
+  static constexpr int kLoadsQ = kQ / kFrag / NW, kLoadsY = kY / kFrag / NW, kLoadsU = 4 + 1;  // of a wave
 };
+
+// At most N of this wave's loads and stores are on their way, its LDS reads are
+// done; then the workgroup's.
+template <int N, int NW>
+__device__ __forceinline__ void arrive() {
+  asm volatile("s_waitcnt vmcnt(%0) lgkmcnt(0)" ::"i"(N < 63 ? N : 63) : "memory");
+  if constexpr (NW > 1) __builtin_amdgcn_s_barrier();
+  asm volatile("" ::: "memory");
+}
 
 __device__ __forceinline__ void to_lds(const char* src, char* dst, int lane) {
   __builtin_amdgcn_global_load_lds((const __attribute__((address_space(1))) void*)(src + lane * 16),
@@ -587,11 +604,10 @@ __device__ __forceinline__ void to_lds(const char* src, char* dst, int lane) {
 
 template <typename TOut, int DKP, int NW>
 __global__ __launch_bounds__(NW * kWave) void scan_kernel(ChainArgs a, Part part) {
-  typedef Scan<DKP> S;
+  typedef Scan<DKP, NW> S;
   constexpr int kKs = S::kKs;
   extern __shared__ __align__(16) char s_raw[];
-  char *s_w = s_raw, *s_y = s_w + S::kQ, *s_q = s_y + 13 * kFrag, *s_kt = s_q + S::kQ;
-  const float* s_sc = reinterpret_cast<const float*>(s_y + 12 * kFrag);
+  char *s_w = s_raw, *s_q = s_w + S::kQ, *s_kt = s_q + S::kQ, *s_y = s_kt + S::kQ, *s_scalars = s_y + S::kY, *s_u = s_scalars + 2 * kFrag;
   const int tid = threadIdx.x, lane = tid % kWave, w = __builtin_amdgcn_readfirstlane(tid / kWave);
   const int n16 = lane & 15, q4 = lane >> 4;
   const int group = blockIdx.x * NW + w, h = blockIdx.y, b = part.b0 + blockIdx.z, hk = h / (a.Hv / a.Hk);
@@ -600,29 +616,46 @@ __global__ __launch_bounds__(NW * kWave) void scan_kernel(ChainArgs a, Part part
   if (part.c0 >= end) return;
   const SlotLayout l = slot_layout(a.Hk, a.Hv, dk, dv);
   const int ch = group * 16 + n16;  // value channel
+  const char* vws = value_at(a, slot_at(a, part, blockIdx.z, 0), h);
+  const char* kws = key_at(a, slot_at(a, part, blockIdx.z, 0), hk);
+  const size_t u_at = l.u_at() + size_t(group) * 4 * kFrag;
+  char* own_u = s_u + w * 4 * kFrag;
+  auto shared = [&](const char* src, char* to, int loads) {  // of all waves
+#pragma unroll
+    for (int n = 0; n < loads; ++n) to_lds(src + (n * NW + w) * kFrag, to + (n * NW + w) * kFrag, lane);
+  };
+  auto load_wu = [&](int m) {
+    const char* src = vws + size_t(m) * l.total;
+    shared(src, s_w, S::kLoadsQ);
+    to_lds(src + l.scalars_at(), s_scalars + (m & 1) * kFrag, lane);  // by every wave, the same
+#pragma unroll
+    for (int t = 0; t < 4; ++t) to_lds(src + u_at + t * kFrag, own_u + t * kFrag, lane);
+    asm volatile("" ::: "memory");
+  };
+  auto load_qy = [&](int m) {
+    shared(kws + size_t(m) * l.total, s_q, S::kLoadsQ);
+    shared(vws + size_t(m) * l.total + l.y_at(), s_y, S::kLoadsY);
+    asm volatile("" ::: "memory");
+  };
+  load_wu(0);
+  load_qy(0);
+
   float* state = a.S + ((size_t(b) * a.Hv + h) * dv + ch) * dk + 4 * q4;
   f32x4 st[DKP / 16];  // key channels 16 n + 4 q4 ..
 #pragma unroll
   for (int n = 0; n < DKP / 16; ++n) st[n] = 16 * n < dk ? *reinterpret_cast<const f32x4*>(state + 16 * n) : f32x4{};
   TOut* out = reinterpret_cast<TOut*>(a.out) + (size_t(tk.first) * a.Hv + h) * dv + ch;
 
-  for (int c = part.c0; c < end; ++c) {
-    char* slot = slot_at(a, part, blockIdx.z, c - part.c0);
-    const char *vws = value_at(a, slot, h), *kws = key_at(a, slot, hk);
-    __syncthreads();  // the last chunk's operands are read
-    for (int u = w; u < S::kQ / kFrag + 13; u += NW) to_lds(vws + u * kFrag, s_w + u * kFrag, lane);
-    for (int u = w; u < 2 * S::kQ / kFrag; u += NW) to_lds(kws + u * kFrag, s_q + u * kFrag, lane);
-    f32x4 x[4];  // U, then V'
-#pragma unroll
-    for (int t = 0; t < 4; ++t) x[t] = *reinterpret_cast<const f32x4*>(vws + l.u_at() + (size_t(group) * 4 + t) * kFrag + lane * 16);
-
+  for (int m = 0; m < end - part.c0; ++m) {
+    const int next = min(m + 1, end - part.c0 - 1);  // loads go on behind the last chunk, so that waits stay the same
+    const float* s_sc = reinterpret_cast<const float*>(s_scalars + (m & 1) * kFrag);
     // the state as an operand
-    float m = 0.0f, ss, is;
+    float mx = 0.0f, ss, is;
 #pragma unroll
     for (int n = 0; n < DKP / 16; ++n)
 #pragma unroll
-      for (int r = 0; r < 4; ++r) m = fmaxf(m, fabsf(st[n][r]));
-    f16_scale(column_max(m), ss, is);
+      for (int r = 0; r < 4; ++r) mx = fmaxf(mx, fabsf(st[n][r]));
+    f16_scale(column_max(mx), ss, is);
     Pair sp[kKs];
 #pragma unroll
     for (int s = 0; s < kKs; ++s) {
@@ -630,12 +663,13 @@ __global__ __launch_bounds__(NW * kWave) void scan_kernel(ChainArgs a, Part part
                           st[2 * s + 1][0], st[2 * s + 1][1], st[2 * s + 1][2], st[2 * s + 1][3]};
       sp[s] = split(y, ss);
     }
-    asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
-    __syncthreads();
+    arrive<S::kLoadsQ + S::kLoadsY, NW>();  // W, U, scalars; the last chunk's K^T is read
+    shared(kws + size_t(m) * l.total + S::kQ, s_kt, S::kLoadsQ);
+    asm volatile("" ::: "memory");
 
     // V' = U - W S^T
     float mv = 0.0f, md = 0.0f, sv, iv, sd, id;
-    f32x4 xd[4];  // decayed to the chunk's end
+    f32x4 x[4], xd[4];  // xd: decayed to the chunk's end
 #pragma unroll
     for (int t = 0; t < 4; ++t) {
       f32x4 p = {};
@@ -643,9 +677,10 @@ __global__ __launch_bounds__(NW * kWave) void scan_kernel(ChainArgs a, Part part
       for (int s = 0; s < kKs; ++s) p = mma3(load_pair(s_w, s * 4 + t, lane), sp[s], p);
       const f32x4 rs = *reinterpret_cast<const f32x4*>(s_sc + 16 * t + 4 * q4);
       const f32x4 dec = *reinterpret_cast<const f32x4*>(s_sc + 2 * kC + 16 * t + 4 * q4);
+      const f32x4 u = *reinterpret_cast<const f32x4*>(own_u + t * kFrag + lane * 16);
 #pragma unroll
       for (int r = 0; r < 4; ++r) {
-        x[t][r] -= p[r] * rs[r] * is;
+        x[t][r] = u[r] - p[r] * rs[r] * is;
         xd[t][r] = x[t][r] * dec[r];
         mv = fmaxf(mv, fabsf(x[t][r]));
         md = fmaxf(md, fabsf(xd[t][r]));
@@ -663,23 +698,41 @@ __global__ __launch_bounds__(NW * kWave) void scan_kernel(ChainArgs a, Part part
       vp[s] = split(y, sv);
       vd[s] = split(z, sd);
     }
+    arrive<S::kLoadsQ, NW>();  // Q, Y; W and U are read
+    load_wu(next);
     // outputs
-    iv *= 1.0f / kUnit;
-    const float io = is * (1.0f / kUnit);
+    iv *= a.scale * (1.0f / kUnit);
+    const float io = is * (a.scale * (1.0f / kUnit));
+    f32x4 o[4];
 #pragma unroll
     for (int t = 0; t < 4; ++t) {
-      f32x4 o = {}, y = {};
+      f32x4 y = {};
+      o[t] = f32x4{};
 #pragma unroll
-      for (int s = 0; s < kKs; ++s) o = mma3(load_pair(s_q, s * 4 + t, lane), sp[s], o);
+      for (int s = 0; s < kKs; ++s) o[t] = mma3(load_pair(s_q, s * 4 + t, lane), sp[s], o[t]);
       y = mma3(load_pair(s_y, lower_step(t, 0), lane), vp[0], y);
       if (t >= 2) y = mma3(load_pair(s_y, lower_step(t, 1), lane), vp[1], y);
       const f32x4 dec = *reinterpret_cast<const f32x4*>(s_sc + kC + 16 * t + 4 * q4);
 #pragma unroll
-      for (int r = 0; r < 4; ++r) {
-        const int i = c * kC + 16 * t + 4 * q4 + r;
-        if (i < tk.n) put(out + size_t(i) * a.Hv * dv, a.scale * (o[r] * dec[r] * io + y[r] * iv));
-      }
+      for (int r = 0; r < 4; ++r) o[t][r] = o[t][r] * dec[r] * io + y[r] * iv;
     }
+    arrive<S::kLoadsQ + S::kLoadsU, NW>();  // K^T; Q and Y are read
+    const int n0 = (part.c0 + m) * kC;
+    TOut* to = out + size_t(n0 + 4 * q4) * a.Hv * dv;
+    if (n0 + kC <= tk.n) {
+#pragma unroll
+      for (int t = 0; t < 4; ++t)
+#pragma unroll
+        for (int r = 0; r < 4; ++r) put(to + size_t(16 * t + r) * a.Hv * dv, o[t][r]);
+    } else {
+#pragma unroll
+      for (int t = 0; t < 4; ++t)
+#pragma unroll
+        for (int r = 0; r < 4; ++r)
+          if (n0 + 16 * t + 4 * q4 + r < tk.n) put(to + size_t(16 * t + r) * a.Hv * dv, o[t][r]);
+    }
+    asm volatile("" ::: "memory");
+    load_qy(next);
     // the state behind the chunk
     const float last = s_sc[3 * kC];
     id *= 1.0f / kUnit;
@@ -692,6 +745,7 @@ __global__ __launch_bounds__(NW * kWave) void scan_kernel(ChainArgs a, Part part
       for (int r = 0; r < 4; ++r) st[n][r] = last * st[n][r] + p[r] * id;
     }
   }
+  asm volatile("s_waitcnt vmcnt(0)" ::: "memory");  // nothing arrives in LDS after the end
 #pragma unroll
   for (int n = 0; n < DKP / 16; ++n)
     if (16 * n < dk) *reinterpret_cast<f32x4*>(state + 16 * n) = st[n];
@@ -734,7 +788,7 @@ int launch_prep(const ChainArgs& a, const Part& p, hipStream_t stream) {
 
 template <typename TOut, int DKP, int NW>
 int launch_waves(const ChainArgs& a, const Part& p, hipStream_t stream) {
-  constexpr int lds = Scan<DKP>::kLds;
+  constexpr int lds = Scan<DKP, NW>::kLds;
   const int rc = ensure_dynamic_lds(reinterpret_cast<const void*>(scan_kernel<TOut, DKP, NW>), lds, "chain");
   if (rc != GDN_OK) return rc;
   scan_kernel<TOut, DKP, NW><<<dim3(a.dv / 16 / NW, a.Hv, p.G), NW * kWave, lds, stream>>>(a, p);
