@@ -574,10 +574,14 @@ __global__ __launch_bounds__(kPrepThreads, 2) void chunk_kernel(ChainArgs a, Par
 // channels; the waves of a workgroup share the chunk's operands in LDS.
 //
 // Operands come into LDS past the registers, each into the place of the last
-// chunk's as soon as that is read: W and U behind V', Q and Y behind the
-// outputs, K^T behind the state.  A wave's loads and stores complete in order, so
-// each wait names how many were issued after what it needs (or fewer).  The
-// compiler has no loads of its own in the loop: it would wait for all.
+// chunk's as soon as that is read: W, U and Q behind the products with the
+// state, Y and K^T behind those with V'.  A wave's loads and stores complete in
+// order, so each wait names how many were issued after what it needs (or
+// fewer).  The compiler has no loads of its own in the loop: it would wait for all.
+//
+// With one wave a SIMD nothing hides an LDS read but the wave's own products:
+// operand pairs are read a group of four ahead of them, two accumulators in turn
+// (12 products of 16 clocks over about 130 of a read).
 // ---------------------------------------------------------------------------
 template <int DKP, int NW>
 struct Scan {
@@ -624,99 +628,35 @@ __global__ __launch_bounds__(NW * kWave) void scan_kernel(ChainArgs a, Part part
 #pragma unroll
     for (int n = 0; n < loads; ++n) to_lds(src + (n * NW + w) * kFrag, to + (n * NW + w) * kFrag, lane);
   };
-  auto load_wu = [&](int m) {
+  auto load_first = [&](int m) {  // W, U, Q, scalars
     const char* src = vws + size_t(m) * l.total;
     shared(src, s_w, S::kLoadsQ);
+    shared(kws + size_t(m) * l.total, s_q, S::kLoadsQ);
     to_lds(src + l.scalars_at(), s_scalars + (m & 1) * kFrag, lane);  // by every wave, the same
 #pragma unroll
     for (int t = 0; t < 4; ++t) to_lds(src + u_at + t * kFrag, own_u + t * kFrag, lane);
     asm volatile("" ::: "memory");
   };
-  auto load_qy = [&](int m) {
-    shared(kws + size_t(m) * l.total, s_q, S::kLoadsQ);
+  auto load_second = [&](int m) {  // Y, K^T
     shared(vws + size_t(m) * l.total + l.y_at(), s_y, S::kLoadsY);
+    shared(kws + size_t(m) * l.total + S::kQ, s_kt, S::kLoadsQ);
     asm volatile("" ::: "memory");
   };
-  load_wu(0);
-  load_qy(0);
+  load_first(0);
 
   float* state = a.S + ((size_t(b) * a.Hv + h) * dv + ch) * dk + 4 * q4;
   f32x4 st[DKP / 16];  // key channels 16 n + 4 q4 ..
 #pragma unroll
   for (int n = 0; n < DKP / 16; ++n) st[n] = 16 * n < dk ? *reinterpret_cast<const f32x4*>(state + 16 * n) : f32x4{};
   TOut* out = reinterpret_cast<TOut*>(a.out) + (size_t(tk.first) * a.Hv + h) * dv + ch;
+  float mx = 0.0f;  // the largest of this lane's values
+#pragma unroll
+  for (int n = 0; n < DKP / 16; ++n)
+#pragma unroll
+    for (int r = 0; r < 4; ++r) mx = fmaxf(mx, fabsf(st[n][r]));
 
-  for (int m = 0; m < end - part.c0; ++m) {
-    const int next = min(m + 1, end - part.c0 - 1);  // loads go on behind the last chunk, so that waits stay the same
-    const float* s_sc = reinterpret_cast<const float*>(s_scalars + (m & 1) * kFrag);
-    // the state as an operand
-    float mx = 0.0f, ss, is;
-#pragma unroll
-    for (int n = 0; n < DKP / 16; ++n)
-#pragma unroll
-      for (int r = 0; r < 4; ++r) mx = fmaxf(mx, fabsf(st[n][r]));
-    f16_scale(column_max(mx), ss, is);
-    Pair sp[kKs];
-#pragma unroll
-    for (int s = 0; s < kKs; ++s) {
-      const float y[8] = {st[2 * s][0], st[2 * s][1], st[2 * s][2], st[2 * s][3],
-                          st[2 * s + 1][0], st[2 * s + 1][1], st[2 * s + 1][2], st[2 * s + 1][3]};
-      sp[s] = split(y, ss);
-    }
-    arrive<S::kLoadsQ + S::kLoadsY, NW>();  // W, U, scalars; the last chunk's K^T is read
-    shared(kws + size_t(m) * l.total + S::kQ, s_kt, S::kLoadsQ);
-    asm volatile("" ::: "memory");
-
-    // V' = U - W S^T
-    float mv = 0.0f, md = 0.0f, sv, iv, sd, id;
-    f32x4 x[4], xd[4];  // xd: decayed to the chunk's end
-#pragma unroll
-    for (int t = 0; t < 4; ++t) {
-      f32x4 p = {};
-#pragma unroll
-      for (int s = 0; s < kKs; ++s) p = mma3(load_pair(s_w, s * 4 + t, lane), sp[s], p);
-      const f32x4 rs = *reinterpret_cast<const f32x4*>(s_sc + 16 * t + 4 * q4);
-      const f32x4 dec = *reinterpret_cast<const f32x4*>(s_sc + 2 * kC + 16 * t + 4 * q4);
-      const f32x4 u = *reinterpret_cast<const f32x4*>(own_u + t * kFrag + lane * 16);
-#pragma unroll
-      for (int r = 0; r < 4; ++r) {
-        x[t][r] = u[r] - p[r] * rs[r] * is;
-        xd[t][r] = x[t][r] * dec[r];
-        mv = fmaxf(mv, fabsf(x[t][r]));
-        md = fmaxf(md, fabsf(xd[t][r]));
-      }
-    }
-    f16_scale(column_max(mv), sv, iv);
-    f16_scale(column_max(md), sd, id);
-    Pair vp[2], vd[2];
-#pragma unroll
-    for (int s = 0; s < 2; ++s) {
-      const float y[8] = {x[2 * s][0], x[2 * s][1], x[2 * s][2], x[2 * s][3],
-                          x[2 * s + 1][0], x[2 * s + 1][1], x[2 * s + 1][2], x[2 * s + 1][3]};
-      const float z[8] = {xd[2 * s][0], xd[2 * s][1], xd[2 * s][2], xd[2 * s][3],
-                          xd[2 * s + 1][0], xd[2 * s + 1][1], xd[2 * s + 1][2], xd[2 * s + 1][3]};
-      vp[s] = split(y, sv);
-      vd[s] = split(z, sd);
-    }
-    arrive<S::kLoadsQ, NW>();  // Q, Y; W and U are read
-    load_wu(next);
-    // outputs
-    iv *= a.scale * (1.0f / kUnit);
-    const float io = is * (a.scale * (1.0f / kUnit));
-    f32x4 o[4];
-#pragma unroll
-    for (int t = 0; t < 4; ++t) {
-      f32x4 y = {};
-      o[t] = f32x4{};
-#pragma unroll
-      for (int s = 0; s < kKs; ++s) o[t] = mma3(load_pair(s_q, s * 4 + t, lane), sp[s], o[t]);
-      y = mma3(load_pair(s_y, lower_step(t, 0), lane), vp[0], y);
-      if (t >= 2) y = mma3(load_pair(s_y, lower_step(t, 1), lane), vp[1], y);
-      const f32x4 dec = *reinterpret_cast<const f32x4*>(s_sc + kC + 16 * t + 4 * q4);
-#pragma unroll
-      for (int r = 0; r < 4; ++r) o[t][r] = o[t][r] * dec[r] * io + y[r] * iv;
-    }
-    arrive<S::kLoadsQ + S::kLoadsU, NW>();  // K^T; Q and Y are read
+  f32x4 o[4];  // outputs of a chunk
+  auto store = [&](int m) {
     const int n0 = (part.c0 + m) * kC;
     TOut* to = out + size_t(n0 + 4 * q4) * a.Hv * dv;
     if (n0 + kC <= tk.n) {
@@ -732,19 +672,163 @@ __global__ __launch_bounds__(NW * kWave) void scan_kernel(ChainArgs a, Part part
           if (n0 + 16 * t + 4 * q4 + r < tk.n) put(to + size_t(16 * t + r) * a.Hv * dv, o[t][r]);
     }
     asm volatile("" ::: "memory");
-    load_qy(next);
-    // the state behind the chunk
+  };
+
+  for (int m = 0; m < end - part.c0; ++m) {
+    const int next = min(m + 1, end - part.c0 - 1);  // loads go on behind the last chunk, so that waits stay the same
+    const float* s_sc = reinterpret_cast<const float*>(s_scalars + (m & 1) * kFrag);
+    float ss, is;  // the state as an operand
+    f16_scale(column_max(mx), ss, is);
+    Pair sp[kKs];
+#pragma unroll
+    for (int s = 0; s < kKs; ++s) {
+      const float y[8] = {st[2 * s][0], st[2 * s][1], st[2 * s][2], st[2 * s][3],
+                          st[2 * s + 1][0], st[2 * s + 1][1], st[2 * s + 1][2], st[2 * s + 1][3]};
+      sp[s] = split(y, ss);
+    }
+    arrive<0, NW>();  // W, U, Q, scalars; the last chunk's Y and K^T are read
+    if (m) store(m - 1);  // here: the next wait is a part away
+    load_second(m);
+
+    // V' = U - W S^T, and Q S^T.  Group n: token tiles 2 (n / (kKs / 2)) and the
+    // next, steps 2 (n % (kKs / 2)) and the next (one step of two groups' tiles
+    // where there is one step only).
+    constexpr int kPer = kKs > 1 ? kKs / 2 : 1, kGroups = 2 * kPer, kSteps = kKs > 1 ? 2 : 1;
+    Pair f[2][2 * kSteps];
+    auto read = [&](Pair (&f)[2 * kSteps], const char* from, int n) {
+#pragma unroll
+      for (int k = 0; k < 2 * kSteps; ++k)
+        f[k] = load_pair(from, (n % kPer * kSteps + k / 2) * 4 + n / kPer * 2 + k % 2, lane);
+    };
+    auto times = [&](const Pair (&f)[2 * kSteps], f32x4 (&c)[4], int n) {
+      const int t = n / kPer * 2, s = n % kPer * kSteps;
+#pragma unroll
+      for (int k = 0; k < kSteps; ++k) {
+        const Pair& y = sp[s + k];
+        c[t] = mma(f[2 * k].lo, y.hi, c[t]);
+        c[t + 1] = mma(f[2 * k + 1].lo, y.hi, c[t + 1]);
+        c[t] = mma(f[2 * k].hi, y.lo, c[t]);
+        c[t + 1] = mma(f[2 * k + 1].hi, y.lo, c[t + 1]);
+        c[t] = mma(f[2 * k].hi, y.hi, c[t]);
+        c[t + 1] = mma(f[2 * k + 1].hi, y.hi, c[t + 1]);
+      }
+    };
+    f32x4 p[4] = {};
+#pragma unroll
+    for (int t = 0; t < 4; ++t) o[t] = f32x4{};
+    float mv = 0.0f, md = 0.0f, sv, iv, sd, id;
+    f32x4 x[4], xd[4];  // xd: decayed to the chunk's end
+    auto value = [&](int t) {
+      const f32x4 rs = *reinterpret_cast<const f32x4*>(s_sc + 16 * t + 4 * q4);
+      const f32x4 dec = *reinterpret_cast<const f32x4*>(s_sc + 2 * kC + 16 * t + 4 * q4);
+      const f32x4 u = *reinterpret_cast<const f32x4*>(own_u + t * kFrag + lane * 16);
+#pragma unroll
+      for (int r = 0; r < 4; ++r) {
+        x[t][r] = u[r] - p[t][r] * rs[r] * is;
+        xd[t][r] = x[t][r] * dec[r];
+        mv = fmaxf(mv, fabsf(x[t][r]));
+        md = fmaxf(md, fabsf(xd[t][r]));
+      }
+    };
+    read(f[0], s_w, 0);
+#pragma unroll
+    for (int n = 0; n < kGroups; ++n) {
+      if (n + 1 < kGroups) read(f[(n + 1) & 1], s_w, n + 1);
+      else read(f[kGroups & 1], s_q, 0);
+      __builtin_amdgcn_sched_barrier(0);
+      times(f[n & 1], p, n);
+      __builtin_amdgcn_sched_barrier(0);
+    }
+#pragma unroll
+    for (int n = 0; n < kGroups; ++n) {
+      if (n + 1 < kGroups) read(f[(kGroups + n + 1) & 1], s_q, n + 1);
+      __builtin_amdgcn_sched_barrier(0);
+      times(f[(kGroups + n) & 1], o, n);
+#pragma unroll
+      for (int t = n * 4 / kGroups; t < (n + 1) * 4 / kGroups; ++t) value(t);
+      __builtin_amdgcn_sched_barrier(0);
+    }
+    f16_scale(column_max(mv), sv, iv);
+    f16_scale(column_max(md), sd, id);
+    Pair vp[2], vd[2];
+#pragma unroll
+    for (int s = 0; s < 2; ++s) {
+      const float y[8] = {x[2 * s][0], x[2 * s][1], x[2 * s][2], x[2 * s][3],
+                          x[2 * s + 1][0], x[2 * s + 1][1], x[2 * s + 1][2], x[2 * s + 1][3]};
+      const float z[8] = {xd[2 * s][0], xd[2 * s][1], xd[2 * s][2], xd[2 * s][3],
+                          xd[2 * s + 1][0], xd[2 * s + 1][1], xd[2 * s + 1][2], xd[2 * s + 1][3]};
+      vp[s] = split(y, sv);
+      vd[s] = split(z, sd);
+    }
     const float last = s_sc[3 * kC];
+    arrive<0, NW>();  // Y, K^T; W, U and Q are read
+    load_first(next);
+
+    // outputs: rows of Y V' beside those of Q S^T; then the state behind the chunk
+    f32x4 y[4] = {};
+    Pair g[2][4];
+    auto read_y = [&](Pair (&f)[4], int n) {  // tiles 0, 1 and the first step of 2, 3; their second
+#pragma unroll
+      for (int k = 0; k < 4 - 2 * n; ++k) f[k] = load_pair(s_y, n ? lower_step(2 + k, 1) : lower_step(k, 0), lane);
+    };
+    auto read_k = [&](Pair (&f)[4], int n) {
+#pragma unroll
+      for (int k = 0; k < 4; ++k) f[k] = load_pair(s_kt, 4 * n + k, lane);
+    };
+    read_y(g[0], 0);
+    read_y(g[1], 1);
+    __builtin_amdgcn_sched_barrier(0);
+#pragma unroll
+    for (int k = 0; k < 4; ++k) y[k] = mma(g[0][k].lo, vp[0].hi, y[k]);
+#pragma unroll
+    for (int k = 0; k < 4; ++k) y[k] = mma(g[0][k].hi, vp[0].lo, y[k]);
+#pragma unroll
+    for (int k = 0; k < 4; ++k) y[k] = mma(g[0][k].hi, vp[0].hi, y[k]);
+    read_k(g[0], 0);
+    __builtin_amdgcn_sched_barrier(0);
+#pragma unroll
+    for (int k = 0; k < 2; ++k) y[2 + k] = mma(g[1][k].lo, vp[1].hi, y[2 + k]);
+#pragma unroll
+    for (int k = 0; k < 2; ++k) y[2 + k] = mma(g[1][k].hi, vp[1].lo, y[2 + k]);
+#pragma unroll
+    for (int k = 0; k < 2; ++k) y[2 + k] = mma(g[1][k].hi, vp[1].hi, y[2 + k]);
+    iv *= a.scale * (1.0f / kUnit);
+    const float io = is * (a.scale * (1.0f / kUnit));
     id *= 1.0f / kUnit;
+    mx = 0.0f;
 #pragma unroll
-    for (int n = 0; n < DKP / 16; ++n) {
-      f32x4 p = {};
+    for (int n = 0; n < DKP / 32; ++n) {
+      if (n + 1 < DKP / 32) read_k(g[(n + 1) & 1], n + 1);
+      __builtin_amdgcn_sched_barrier(0);
+      f32x4 c[2] = {};
+      const Pair(&f)[4] = g[n & 1];
 #pragma unroll
-      for (int s = 0; s < 2; ++s) p = mma3(load_pair(s_kt, n * 2 + s, lane), vd[s], p);
+      for (int s = 0; s < 2; ++s) {
+        c[0] = mma(f[s].lo, vd[s].hi, c[0]);
+        c[1] = mma(f[2 + s].lo, vd[s].hi, c[1]);
+        c[0] = mma(f[s].hi, vd[s].lo, c[0]);
+        c[1] = mma(f[2 + s].hi, vd[s].lo, c[1]);
+        c[0] = mma(f[s].hi, vd[s].hi, c[0]);
+        c[1] = mma(f[2 + s].hi, vd[s].hi, c[1]);
+      }
+      // outputs of a share of the tiles beside these products
 #pragma unroll
-      for (int r = 0; r < 4; ++r) st[n][r] = last * st[n][r] + p[r] * id;
+      for (int t = n * 4 / (DKP / 32); t < (n + 1) * 4 / (DKP / 32); ++t) {
+        const f32x4 dec = *reinterpret_cast<const f32x4*>(s_sc + kC + 16 * t + 4 * q4);
+#pragma unroll
+        for (int r = 0; r < 4; ++r) o[t][r] = o[t][r] * dec[r] * io + y[t][r] * iv;
+      }
+#pragma unroll
+      for (int e = 0; e < 2; ++e)
+#pragma unroll
+        for (int r = 0; r < 4; ++r) {
+          st[2 * n + e][r] = last * st[2 * n + e][r] + c[e][r] * id;
+          mx = fmaxf(mx, fabsf(st[2 * n + e][r]));
+        }
+      __builtin_amdgcn_sched_barrier(0);
     }
   }
+  store(end - part.c0 - 1);
   asm volatile("s_waitcnt vmcnt(0)" ::: "memory");  // nothing arrives in LDS after the end
 #pragma unroll
   for (int n = 0; n < DKP / 16; ++n)
