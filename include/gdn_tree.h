@@ -476,7 +476,7 @@ typedef struct {
  * a chunk takes about Hk 512 dk + Hv (256 dk + 256 dv + 13312) bytes
  * (dk, dv rounded up to 32 and 16). */
 #define GDN_CHAIN_STEP_T 16
-#define GDN_CHAIN_WORKSPACE (1u << 29)
+#define GDN_CHAIN_WORKSPACE (1u << 28)
 int gdn_chain(const gdn_chain_dims* dims, const int32_t* start, const int32_t* n_new, const void* q,
               const void* k, const void* v, const void* alpha, const void* beta,
               const float* conv_w, const float* conv_state, float* conv_state_out, float* S,

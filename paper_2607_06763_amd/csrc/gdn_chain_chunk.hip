@@ -31,6 +31,7 @@
 namespace gdn {
 namespace {
 
+typedef _Float16 f16x2 __attribute__((ext_vector_type(2)));
 typedef _Float16 f16x4 __attribute__((ext_vector_type(4)));
 
 constexpr int kC = 64;          // tokens of a chunk
@@ -98,17 +99,19 @@ struct Pair {
 };
 
 __device__ __forceinline__ Pair split(const float (&x)[8], float scale) {
-  Pair p;
+  u32x4 hi, lo;
 #pragma unroll
-  for (int e = 0; e < 8; ++e) {
-    // the product as a value of its own: fused into the conversion it would be
-    // rounded once there and twice for the difference, and hi would differ
-    float y = x[e] * scale;
-    asm("" : "+v"(y));
-    p.hi[e] = (_Float16)y;
-    p.lo[e] = (_Float16)(y - (float)p.hi[e]);
+  for (int e = 0; e < 4; ++e) {
+    f16x2 h = {(_Float16)(x[2 * e] * scale), (_Float16)(x[2 * e + 1] * scale)};
+    // a value of its own: were it computed again for the difference, with another
+    // rounding of the product, hi + lo would miss x by a step of hi
+    asm("" : "+v"(h));
+    const f16x2 l = {(_Float16)__builtin_fmaf(x[2 * e], scale, -(float)h[0]),
+                     (_Float16)__builtin_fmaf(x[2 * e + 1], scale, -(float)h[1])};
+    hi[e] = __builtin_bit_cast(unsigned, h);
+    lo[e] = __builtin_bit_cast(unsigned, l);
   }
-  return p;
+  return {__builtin_bit_cast(f16x8, hi), __builtin_bit_cast(f16x8, lo)};
 }
 
 __device__ __forceinline__ f32x4 mma(f16x8 a, f16x8 b, f32x4 c) { return __builtin_amdgcn_mfma_f32_16x16x32_f16(a, b, c, 0, 0, 0); }
@@ -128,14 +131,18 @@ __device__ __forceinline__ void f16_scale(float m, float& scale, float& inv) {
   inv = __uint_as_float(unsigned(ex - 13) << 23);
 }
 
-// Over the four lanes of a column (lane % 16).
+// Over the four lanes of a column (lane % 16): rows of 16 lanes trade places.
 __device__ __forceinline__ float column_max(float x) {
-  x = fmaxf(x, __shfl_xor(x, 16));
-  return fmaxf(x, __shfl_xor(x, 32));
+  auto r = __builtin_amdgcn_permlane16_swap(__float_as_uint(x), __float_as_uint(x), false, false);
+  x = fmaxf(__uint_as_float(r[0]), __uint_as_float(r[1]));
+  r = __builtin_amdgcn_permlane32_swap(__float_as_uint(x), __float_as_uint(x), false, false);
+  return fmaxf(__uint_as_float(r[0]), __uint_as_float(r[1]));
 }
 __device__ __forceinline__ float column_sum(float x) {
-  x += __shfl_xor(x, 16);
-  return x + __shfl_xor(x, 32);
+  auto r = __builtin_amdgcn_permlane16_swap(__float_as_uint(x), __float_as_uint(x), false, false);
+  x = __uint_as_float(r[0]) + __uint_as_float(r[1]);
+  r = __builtin_amdgcn_permlane32_swap(__float_as_uint(x), __float_as_uint(x), false, false);
+  return __uint_as_float(r[0]) + __uint_as_float(r[1]);
 }
 
 __device__ __forceinline__ Pair load_pair(const char* p, int tile, int lane) {
@@ -171,7 +178,7 @@ struct Prep {
   static constexpr int kPlane = kPacks * (kC + 1) * 16;       // bytes of hi or lo of K or Q: [pack][token]
   static constexpr int kMat = kC * kLd * int(sizeof(float));  // a chunk's matrix
   static constexpr int kRows = 4 * kPlane > kHeads * kMat ? 4 * kPlane : kHeads * kMat;
-  static constexpr int kLds = kRows + kHeads * kC * 20;
+  static constexpr int kLds = kRows + kHeads * (kC * 20 + 4);
 };
 
 // Two channels of a row as they are, and one of them.
@@ -197,6 +204,7 @@ __global__ __launch_bounds__(kPrepThreads, 2) void chunk_kernel(ChainArgs a, Par
   float* s_decay = reinterpret_cast<float*>(s_log + kHeads * kC);  // e^g
   float* s_beta = s_decay + kHeads * kC;
   float* s_row = s_beta + kHeads * kC;  // 1 / scale of a row of W
+  float* s_most = s_row + kHeads * kC;  // largest e^g
   const int tid = threadIdx.x, lane = tid % kWave, w = __builtin_amdgcn_readfirstlane(tid / kWave);
   const int n16 = lane & 15, q4 = lane >> 4;
   const int hk = blockIdx.x, m = blockIdx.y, b = part.b0 + blockIdx.z;
@@ -337,16 +345,21 @@ __global__ __launch_bounds__(kPrepThreads, 2) void chunk_kernel(ChainArgs a, Par
     // rows from 3 before the chunk, by 32-bit offsets (67 rows stay below 2^32 bytes)
     const char* x = reinterpret_cast<const char*>(reinterpret_cast<const TIn*>(a.v) + ((long long)(row0) - 3) * a.Hv * dv + h * dv);
     const unsigned stride = unsigned(a.Hv) * dv * sizeof(TIn);
-    const int t0 = opaque(4 * q4);  // addresses are computed here, not held
+    const unsigned t0 = opaque(4 * q4), at = ch * unsigned(sizeof(TIn));  // addresses are computed here, not held
+    auto fetch = [&](auto row) {
 #pragma unroll
-    for (int s = 0; s < 2; ++s)
+      for (int s = 0; s < 2; ++s)
 #pragma unroll
-      for (int e = 0; e < 2; ++e)
+        for (int e = 0; e < 2; ++e)
 #pragma unroll
-        for (int i = 0; i < 7; ++i) {
-          const unsigned n = min(max(32 * s + 16 * e + t0 + i, n0 ? 0 : 3), nt + 2);
-          raw[s][e][i] = fetch2(reinterpret_cast<const TIn*>(x + size_t(n * stride + ch * unsigned(sizeof(TIn)))));
-        }
+          for (int i = 0; i < 7; ++i) raw[s][e][i] = fetch2(reinterpret_cast<const TIn*>(row(32 * s + 16 * e + i)));
+    };
+    if (n0 && nt == kC) {  // a lane's rows are a scalar apart
+      const size_t first = t0 * stride + at;
+      fetch([&](unsigned n) { return x + size_t(n) * stride + first; });
+    } else {
+      fetch([&](unsigned n) { return x + size_t(min(max(n + t0, n0 ? 0u : 3u), unsigned(nt) + 2u) * stride + at); });
+    }
   };
 
   for (int r0 = 0; r0 < per; r0 += kHeads) {
@@ -362,7 +375,10 @@ __global__ __launch_bounds__(kPrepThreads, 2) void chunk_kernel(ChainArgs a, Par
         if (lane >= d) g += x;
       }
       s_log[w * kC + lane] = g;
-      s_decay[w * kC + lane] = __expf(float(g));
+      const float f = __expf(float(g));
+      s_decay[w * kC + lane] = f;
+      const float most = column_max(group_max<16>(f));
+      if (lane == 0) s_most[w] = most;
       s_beta[w * kC + lane] = be;
     }
     __syncthreads();
@@ -458,7 +474,7 @@ __global__ __launch_bounds__(kPrepThreads, 2) void chunk_kernel(ChainArgs a, Par
       const double* lg = s_log + r * kC;
       const int n16 = opaque(lane & 15), q4 = opaque(lane >> 4);
       // (I + A)^-1 diag(beta): rows n16 of tile t, columns in operand order
-      float inv[6][8], mt = 0.0f, bound[4] = {}, sw[4], iw[4];
+      float inv[6][8], bound[4] = {}, sw[4], iw[4];
 #pragma unroll
       for (int u = 0; u < 6; ++u) {
         const int i = 16 * lower_tile(u) + n16, j = 32 * lower_col(u) + 4 * q4;
@@ -466,18 +482,20 @@ __global__ __launch_bounds__(kPrepThreads, 2) void chunk_kernel(ChainArgs a, Par
         for (int e = 0; e < 2; ++e) {
           const float4 x = *reinterpret_cast<const float4*>(t + i * kLd + j + 16 * e);
           const float4 y = *reinterpret_cast<const float4*>(beta + j + 16 * e);
-          const float4 z = *reinterpret_cast<const float4*>(decay + j + 16 * e);
           inv[u][4 * e] = x.x * y.x, inv[u][4 * e + 1] = x.y * y.y, inv[u][4 * e + 2] = x.z * y.z, inv[u][4 * e + 3] = x.w * y.w;
           const float* f = &inv[u][4 * e];
-          mt = fmaxf(mt, fmaxf(fmaxf(fabsf(f[0]), fabsf(f[1])), fmaxf(fabsf(f[2]), fabsf(f[3]))));
-          bound[lower_tile(u)] += fabsf(f[0] * z.x) + fabsf(f[1] * z.y) + (fabsf(f[2] * z.z) + fabsf(f[3] * z.w));
+          bound[lower_tile(u)] += (fabsf(f[0]) + fabsf(f[1])) + (fabsf(f[2]) + fabsf(f[3]));
         }
       }
       // W = (I + A)^-1 diag(beta e^g) K: |W| of a row is at most the sum of the
-      // inverse's
+      // inverse's times the largest e^g
+      const float most = s_most[r];
+      float mt = 0.0f;
 #pragma unroll
       for (int tt = 0; tt < 4; ++tt) {
-        f16_scale(column_sum(bound[tt]), sw[tt], iw[tt]);
+        const float x = column_sum(bound[tt]);
+        mt = fmaxf(mt, x);
+        f16_scale(x * most, sw[tt], iw[tt]);
         if (w == 0 && q4 == 0) s_row[r * kC + 16 * tt + n16] = iw[tt];
       }
       if (w < kKs) {
@@ -534,7 +552,7 @@ __global__ __launch_bounds__(kPrepThreads, 2) void chunk_kernel(ChainArgs a, Par
         }
         if (r + 1 < nr) fetch_values(h + 1);
         float st, it, sv[2], iv[2];
-        f16_scale(column_max(group_max<16>(mt)), st, it);
+        f16_scale(group_max<16>(mt), st, it);
         Pair vp[2][2];
 #pragma unroll
         for (int c = 0; c < 2; ++c) {
@@ -614,7 +632,11 @@ __global__ __launch_bounds__(NW * kWave) void scan_kernel(ChainArgs a, Part part
   char *s_w = s_raw, *s_q = s_w + S::kQ, *s_kt = s_q + S::kQ, *s_y = s_kt + S::kQ, *s_scalars = s_y + S::kY, *s_u = s_scalars + 2 * kFrag;
   const int tid = threadIdx.x, lane = tid % kWave, w = __builtin_amdgcn_readfirstlane(tid / kWave);
   const int n16 = lane & 15, q4 = lane >> 4;
-  const int group = blockIdx.x * NW + w, h = blockIdx.y, b = part.b0 + blockIdx.z, hk = h / (a.Hv / a.Hk);
+  // workgroups go to the 8 XCDs in turn: those of a key head to one, whose L2
+  // gives them Q and K^T
+  const int each = gridDim.x * gridDim.y, id = blockIdx.y * gridDim.x + blockIdx.x;
+  const int place = each % 8 == 0 ? id % 8 * (each / 8) + id / 8 : id;
+  const int group = place % gridDim.x * NW + w, h = place / gridDim.x, b = part.b0 + blockIdx.z, hk = h / (a.Hv / a.Hk);
   const Tokens tk = tokens_of(a, b);
   const int dk = a.dk, dv = a.dv, end = min(part.c0 + part.M, (tk.n + kC - 1) / kC);
   if (part.c0 >= end) return;
