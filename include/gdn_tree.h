@@ -473,8 +473,7 @@ typedef struct {
  * products in 32 bits (fp16 pairs, three products, fp32 sums), through a
  * workspace that the library keeps (see Workspaces above), at most
  * GDN_CHAIN_WORKSPACE bytes or what one chunk of one sequence needs:
- * a chunk takes about Hk 512 dk + Hv (256 dk + 256 dv + 13312) bytes
- * (dk, dv rounded up to 32 and 16). */
+ * a chunk takes 768 Hk dk + 25600 Hv bytes (dk of 16 as 32). */
 #define GDN_CHAIN_STEP_T 16
 #define GDN_CHAIN_WORKSPACE (1u << 28)
 int gdn_chain(const gdn_chain_dims* dims, const int32_t* start, const int32_t* n_new, const void* q,

@@ -3,19 +3,24 @@
 //
 // Inside a chunk, with g_i the sum of log(alpha) up to token i and S0 the state
 // before it,
-//   (I + A) [U | W] = diag(beta) [V | diag(e^g) K],  A_ij = beta_i k_i.k_j e^(g_i - g_j), j < i
-//   V' = U - W S0^T,   O = scale (diag(e^g) Q S0^T + Y V'),  Y_ij = q_i.k_j e^(g_i - g_j), j <= i
-//   S  = e^g_last S0 + V'^T diag(e^(g_last - g)) K.
-// Everything but V', O and S is independent of the state, and is computed for
-// many chunks at once (chunk_kernel); the rest goes chunk by chunk
+//   (I + A) V' = diag(beta) (V - diag(e^g) K S0^T),  A_ij = beta_i k_i.k_j e^(g_i - g_j), j < i
+//   O = scale (diag(e^g) Q S0^T + Y V'),             Y_ij = q_i.k_j e^(g_i - g_j), j <= i
+//   S = e^g_last S0 + V'^T diag(e^(g_last - g)) K.
+// Keys, queries, (I + A)^-1 and Y do not depend on the state and are computed
+// for many chunks at once (chunk_kernel); the rest goes chunk by chunk
 // (scan_kernel), with the state in registers: a wave holds 16 value channels,
 // the columns of its matrix tiles, and needs nothing from the other waves.
 //
+// What passes between the two bounds both: 170 KB a chunk and key head with
+// three value heads of 128.  With (I + A)^-1 diag(beta) applied to V and K
+// beforehand, as first built, it was 295 KB, and chunk_kernel, which then
+// convolves the values too, took three times as long.
+//
 // Products.  The outputs have 32-bit accuracy, so each operand is a pair of fp16
 // values, hi + lo, 22 bits together, and a product is three on the matrix units
-// (hi hi, hi lo, lo hi) with 32-bit sums: 2^-22 of an operand is lost.  Scales are powers of
-// two, exact: 2^10 for what is at most 1 (unit keys, queries, Y), else by the
-// largest value of the operand's row or column.
+// (hi hi, hi lo, lo hi) with 32-bit sums: 2^-22 of an operand is lost.  Scales
+// are powers of two, exact: 2^10 for what is at most 1 (unit keys, queries, Y),
+// else by the largest value of the matrix or of the operand's column.
 //
 // Operand order.  A tile's accumulators hold rows 4 q + r (q = lane / 16) of
 // column lane % 16, and an operand 8 values of one row or column.  Two tiles of
@@ -50,21 +55,18 @@ __host__ __device__ constexpr int padded_dk(int dk) { return dk < 32 ? 32 : dk; 
 
 struct SlotLayout {
   int ks;        // steps of 32 key channels
-  size_t key;    // bytes of a key head: Q [ks][4 token tiles], K^T [2 ks][2 token steps]
-  size_t value;  // of a value head: W [ks][4], Y [6], scalars, U [dv / 16][4] (fp32 accumulators)
+  size_t key;    // bytes of a key head: K and Q [ks][4 token tiles], K^T [2 ks][2 token steps]
   size_t total;
   __host__ __device__ size_t q_bytes() const { return size_t(ks) * 8 * kFrag; }
-  __host__ __device__ size_t y_at() const { return q_bytes(); }
-  __host__ __device__ size_t scalars_at() const { return y_at() + 12 * kFrag; }
-  __host__ __device__ size_t u_at() const { return scalars_at() + 1024; }
 };
+constexpr size_t kYAt = 12 * kFrag, kScalarsAt = 24 * kFrag;  // of a value head: (I + A)^-1 [6], Y [6], scalars
+constexpr size_t kValue = 25 * kFrag;
 
-__host__ __device__ inline SlotLayout slot_layout(int Hk, int Hv, int dk, int dv) {
+__host__ __device__ inline SlotLayout slot_layout(int Hk, int Hv, int dk) {
   SlotLayout l;
   l.ks = padded_dk(dk) / 32;
-  l.key = 2 * l.q_bytes();
-  l.value = l.u_at() + size_t(dv / 16) * 4 * kFrag;
-  l.total = Hk * l.key + Hv * l.value;
+  l.key = 3 * l.q_bytes();
+  l.total = Hk * l.key + Hv * kValue;
   return l;
 }
 
@@ -75,14 +77,13 @@ struct Part {
 };
 
 __device__ __forceinline__ char* slot_at(const ChainArgs& a, const Part& p, int g, int m) {
-  return p.ws + (size_t(g) * p.M + m) * slot_layout(a.Hk, a.Hv, a.dk, a.dv).total;
+  return p.ws + (size_t(g) * p.M + m) * slot_layout(a.Hk, a.Hv, a.dk).total;
 }
 __device__ __forceinline__ char* key_at(const ChainArgs& a, char* slot, int hk) {
-  return slot + hk * slot_layout(a.Hk, a.Hv, a.dk, a.dv).key;
+  return slot + hk * slot_layout(a.Hk, a.Hv, a.dk).key;
 }
 __device__ __forceinline__ char* value_at(const ChainArgs& a, char* slot, int h) {
-  const SlotLayout l = slot_layout(a.Hk, a.Hv, a.dk, a.dv);
-  return slot + a.Hk * l.key + h * l.value;
+  return slot + a.Hk * slot_layout(a.Hk, a.Hv, a.dk).key + h * kValue;
 }
 
 // Step s of token tile t of a lower triangular operand (6 of them: a step holds
@@ -138,13 +139,6 @@ __device__ __forceinline__ float column_max(float x) {
   r = __builtin_amdgcn_permlane32_swap(__float_as_uint(x), __float_as_uint(x), false, false);
   return fmaxf(__uint_as_float(r[0]), __uint_as_float(r[1]));
 }
-__device__ __forceinline__ float column_sum(float x) {
-  auto r = __builtin_amdgcn_permlane16_swap(__float_as_uint(x), __float_as_uint(x), false, false);
-  x = __uint_as_float(r[0]) + __uint_as_float(r[1]);
-  r = __builtin_amdgcn_permlane32_swap(__float_as_uint(x), __float_as_uint(x), false, false);
-  return __uint_as_float(r[0]) + __uint_as_float(r[1]);
-}
-
 __device__ __forceinline__ Pair load_pair(const char* p, int tile, int lane) {
   const char* q = p + size_t(tile) * 2 * kFrag + lane * 16;
   return {*reinterpret_cast<const f16x8*>(q), *reinterpret_cast<const f16x8*>(q + kFrag)};
@@ -178,14 +172,8 @@ struct Prep {
   static constexpr int kPlane = kPacks * (kC + 1) * 16;       // bytes of hi or lo of K or Q: [pack][token]
   static constexpr int kMat = kC * kLd * int(sizeof(float));  // a chunk's matrix
   static constexpr int kRows = 4 * kPlane > kHeads * kMat ? 4 * kPlane : kHeads * kMat;
-  static constexpr int kLds = kRows + kHeads * (kC * 20 + 4);
+  static constexpr int kLds = kRows + kHeads * (kC * 12 + 4);
 };
-
-// Two channels of a row as they are, and one of them.
-__device__ __forceinline__ float2 fetch2(const float* p) { return *reinterpret_cast<const float2*>(p); }
-__device__ __forceinline__ unsigned fetch2(const BF16* p) { return *reinterpret_cast<const unsigned*>(p); }
-__device__ __forceinline__ float one_of(float2 x, int c) { return c ? x.y : x.x; }
-__device__ __forceinline__ float one_of(unsigned x, int c) { return __uint_as_float(c ? x & 0xffff0000u : x << 16); }
 
 // ---------------------------------------------------------------------------
 // What does not depend on the state.  One workgroup per (key head, chunk) with
@@ -201,10 +189,8 @@ __global__ __launch_bounds__(kPrepThreads, 2) void chunk_kernel(ChainArgs a, Par
   char* s_kq = s_raw;                            // K hi, K lo, Q hi, Q lo; then the heads' matrices
   float* s_t = reinterpret_cast<float*>(s_raw);  // [head][64][kLd]
   double* s_log = reinterpret_cast<double*>(s_raw + P::kRows);  // [head][64]
-  float* s_decay = reinterpret_cast<float*>(s_log + kHeads * kC);  // e^g
-  float* s_beta = s_decay + kHeads * kC;
-  float* s_row = s_beta + kHeads * kC;  // 1 / scale of a row of W
-  float* s_most = s_row + kHeads * kC;  // largest e^g
+  float* s_beta = reinterpret_cast<float*>(s_log + kHeads * kC);
+  float* s_scale = s_beta + kHeads * kC;  // of (I + A)^-1
   const int tid = threadIdx.x, lane = tid % kWave, w = __builtin_amdgcn_readfirstlane(tid / kWave);
   const int n16 = lane & 15, q4 = lane >> 4;
   const int hk = blockIdx.x, m = blockIdx.y, b = part.b0 + blockIdx.z;
@@ -212,7 +198,7 @@ __global__ __launch_bounds__(kPrepThreads, 2) void chunk_kernel(ChainArgs a, Par
   const int n0 = (part.c0 + m) * kC, nt = min(kC, tk.n - n0);
   if (nt <= 0) return;
   const int dk = a.dk, dv = a.dv, per = a.Hv / a.Hk, C = 2 * a.Hk * dk + a.Hv * dv;
-  const SlotLayout layout = slot_layout(a.Hk, a.Hv, dk, dv);
+  const SlotLayout layout = slot_layout(a.Hk, a.Hv, dk);
   char* slot = slot_at(a, part, blockIdx.z, m);
   const float* cs = a.conv_state + size_t(b) * 3 * C;
   const size_t row0 = size_t(tk.first) + n0;  // of the chunk's first token
@@ -299,34 +285,19 @@ __global__ __launch_bounds__(kPrepThreads, 2) void chunk_kernel(ChainArgs a, Par
       }
     }
   }
-  // K^T: rows are channels, 32 tokens; Q: rows are tokens, 32 channels; both in
-  // the order of accumulators.  A wave keeps the channels of one step of W.
+  // K and Q: rows are tokens, 32 channels; K^T: rows are channels, 32 tokens; in
+  // the order of accumulators
   char* kws = key_at(a, slot, hk);
-  const size_t kt_at = size_t(kKs) * 8 * kFrag;
-  Pair kt[4];  // [tile of 16 channels][token step]
-  if (w < kKs) {
 #pragma unroll
-    for (int u = 0; u < 4; ++u) {
-      const int c = 32 * w + u / 2 * 16 + n16, s = u % 2;
-#pragma unroll
-      for (int j = 0; j < 8; ++j) {
-        const int t = 32 * s + 16 * (j / 4) + 4 * q4 + j % 4;
-        const char* d = s_kq + (c / 8 * (kC + 1) + t) * 16 + c % 8 * 2;
-        kt[u].hi[j] = *reinterpret_cast<const _Float16*>(d);
-        kt[u].lo[j] = *reinterpret_cast<const _Float16*>(d + P::kPlane);
-      }
-      store_pair(kws + kt_at, w * 4 + u, lane, kt[u]);
-    }
-  }
-  for (int u = w; u < kKs * 4; u += kPrepWaves) {
-    const int s = u / 4, t = u % 4;
+  for (int n = 0; n < kKs * 8 / kPrepWaves; ++n) {
+    const int u = n * kPrepWaves + w, isq = u / (kKs * 4), s = u / 4 % kKs, t = u % 4;
     Pair x;
 #pragma unroll
     for (int hl = 0; hl < 2; ++hl) {
       f16x4 y[2];
 #pragma unroll
       for (int e = 0; e < 2; ++e)
-        y[e] = *reinterpret_cast<const f16x4*>(s_kq + (2 + hl) * P::kPlane +
+        y[e] = *reinterpret_cast<const f16x4*>(s_kq + (2 * isq + hl) * P::kPlane +
                                                ((4 * s + 2 * e + q4 / 2) * (kC + 1) + 16 * t + n16) * 16 + q4 % 2 * 8);
       const f16x8 z = {y[0][0], y[0][1], y[0][2], y[0][3], y[1][0], y[1][1], y[1][2], y[1][3]};
       if (hl) x.lo = z;
@@ -334,33 +305,20 @@ __global__ __launch_bounds__(kPrepThreads, 2) void chunk_kernel(ChainArgs a, Par
     }
     store_pair(kws, u, lane, x);
   }
-  __syncthreads();  // K and Q are read
-
-  // raw values of channels 32 w + 2 n16 and the next (16 channels: 0 .. 15
-  // twice) of a head, on their way while others are worked on
-  const bool own_v = 32 * w < dv;
-  const int ch = dv == 16 ? 2 * (n16 % 8) : 32 * w + 2 * n16;
-  decltype(fetch2(static_cast<const TIn*>(nullptr))) raw[2][2][7];
-  auto fetch_values = [&](int h) {
-    // rows from 3 before the chunk, by 32-bit offsets (67 rows stay below 2^32 bytes)
-    const char* x = reinterpret_cast<const char*>(reinterpret_cast<const TIn*>(a.v) + ((long long)(row0) - 3) * a.Hv * dv + h * dv);
-    const unsigned stride = unsigned(a.Hv) * dv * sizeof(TIn);
-    const unsigned t0 = opaque(4 * q4), at = ch * unsigned(sizeof(TIn));  // addresses are computed here, not held
-    auto fetch = [&](auto row) {
 #pragma unroll
-      for (int s = 0; s < 2; ++s)
+  for (int n = 0; n < kKs * 4 / kPrepWaves; ++n) {
+    const int u = n * kPrepWaves + w, c = u / 2 * 16 + n16, s = u % 2;
+    Pair x;
 #pragma unroll
-        for (int e = 0; e < 2; ++e)
-#pragma unroll
-          for (int i = 0; i < 7; ++i) raw[s][e][i] = fetch2(reinterpret_cast<const TIn*>(row(32 * s + 16 * e + i)));
-    };
-    if (n0 && nt == kC) {  // a lane's rows are a scalar apart
-      const size_t first = t0 * stride + at;
-      fetch([&](unsigned n) { return x + size_t(n) * stride + first; });
-    } else {
-      fetch([&](unsigned n) { return x + size_t(min(max(n + t0, n0 ? 0u : 3u), unsigned(nt) + 2u) * stride + at); });
+    for (int j = 0; j < 8; ++j) {
+      const int t = 32 * s + 16 * (j / 4) + 4 * q4 + j % 4;
+      const char* d = s_kq + (c / 8 * (kC + 1) + t) * 16 + c % 8 * 2;
+      x.hi[j] = *reinterpret_cast<const _Float16*>(d);
+      x.lo[j] = *reinterpret_cast<const _Float16*>(d + P::kPlane);
     }
-  };
+    store_pair(kws + 2 * layout.q_bytes(), u, lane, x);
+  }
+  __syncthreads();  // K and Q are read
 
   for (int r0 = 0; r0 < per; r0 += kHeads) {
     const int nr = min(kHeads, per - r0);
@@ -375,18 +333,21 @@ __global__ __launch_bounds__(kPrepThreads, 2) void chunk_kernel(ChainArgs a, Par
         if (lane >= d) g += x;
       }
       s_log[w * kC + lane] = g;
-      const float f = __expf(float(g));
-      s_decay[w * kC + lane] = f;
-      const float most = column_max(group_max<16>(f));
-      if (lane == 0) s_most[w] = most;
       s_beta[w * kC + lane] = be;
+      // a token a lane; its decay from the chunk's start, to the chunk's end
+      float* sc = reinterpret_cast<float*>(value_at(a, slot, hk * per + r0 + w) + kScalarsAt);
+      const float f = __expf(float(g));
+      sc[lane] = be;
+      sc[kC + lane] = f;
+      sc[2 * kC + lane] = __expf(float(__shfl(g, kC - 1) - g));
+      if (lane == kC - 1) sc[3 * kC] = f;
     }
     __syncthreads();
     // A, to be inverted, and Y
     for (int r = 0; r < nr; ++r) {
       const double* lg = s_log + r * kC;
       const int n16 = opaque(lane & 15), q4 = opaque(lane >> 4);
-      char* y_out = value_at(a, slot, hk * per + r0 + r) + layout.y_at();
+      char* y_out = value_at(a, slot, hk * per + r0 + r) + kYAt;
 #pragma unroll
       for (int n = 0; n < 2; ++n) {
         const int u = w + 4 * n, i = 16 * lower_tile(u) + n16, j0 = 32 * lower_col(u) + 4 * q4;
@@ -409,7 +370,6 @@ __global__ __launch_bounds__(kPrepThreads, 2) void chunk_kernel(ChainArgs a, Par
         store_pair(y_out, u, lane, split(y, 1.0f / kUnit));
       }
     }
-    if (own_v) fetch_values(hk * per + r0);
     __syncthreads();
     // (I + A)^-1 of a head by one wave
     if (w < nr) {
@@ -464,123 +424,32 @@ __global__ __launch_bounds__(kPrepThreads, 2) void chunk_kernel(ChainArgs a, Par
       };
       put_block(1, 0, x10), put_block(2, 1, x21), put_block(3, 2, x32);
       put_block(2, 0, x20), put_block(3, 1, x31), put_block(3, 0, x30);
+      float most = 1.0f, scale, inv;  // the diagonal
+#pragma unroll
+      for (int r = 0; r < 4; ++r) {
+        most = fmaxf(most, fmaxf(fmaxf(fabsf(x0[r]), fabsf(x1[r])), fmaxf(fabsf(x2[r]), fabsf(x[(48 + 4 * q4 + r) * kLd + 48 + n16]))));
+        most = fmaxf(most, fmaxf(fmaxf(fabsf(x10[r]), fabsf(x21[r])), fabsf(x32[r])));
+        most = fmaxf(most, fmaxf(fmaxf(fabsf(x20[r]), fabsf(x31[r])), fabsf(x30[r])));
+      }
+      f16_scale(column_max(group_max<16>(most)), scale, inv);
+      if (lane == 0) {
+        s_scale[w] = scale;
+        reinterpret_cast<float*>(value_at(a, slot, hk * per + r0 + w) + kScalarsAt)[3 * kC + 1] = inv;
+      }
     }
     __syncthreads();
 
     for (int r = 0; r < nr; ++r) {
-      const int h = hk * per + r0 + r;
-      char* vws = value_at(a, slot, h);
-      const float *t = s_t + r * kC * kLd, *beta = s_beta + r * kC, *decay = s_decay + r * kC;
-      const double* lg = s_log + r * kC;
+      char* t_out = value_at(a, slot, hk * per + r0 + r);
       const int n16 = opaque(lane & 15), q4 = opaque(lane >> 4);
-      // (I + A)^-1 diag(beta): rows n16 of tile t, columns in operand order
-      float inv[6][8], bound[4] = {}, sw[4], iw[4];
 #pragma unroll
-      for (int u = 0; u < 6; ++u) {
-        const int i = 16 * lower_tile(u) + n16, j = 32 * lower_col(u) + 4 * q4;
-#pragma unroll
-        for (int e = 0; e < 2; ++e) {
-          const float4 x = *reinterpret_cast<const float4*>(t + i * kLd + j + 16 * e);
-          const float4 y = *reinterpret_cast<const float4*>(beta + j + 16 * e);
-          inv[u][4 * e] = x.x * y.x, inv[u][4 * e + 1] = x.y * y.y, inv[u][4 * e + 2] = x.z * y.z, inv[u][4 * e + 3] = x.w * y.w;
-          const float* f = &inv[u][4 * e];
-          bound[lower_tile(u)] += (fabsf(f[0]) + fabsf(f[1])) + (fabsf(f[2]) + fabsf(f[3]));
-        }
-      }
-      // W = (I + A)^-1 diag(beta e^g) K: |W| of a row is at most the sum of the
-      // inverse's times the largest e^g
-      const float most = s_most[r];
-      float mt = 0.0f;
-#pragma unroll
-      for (int tt = 0; tt < 4; ++tt) {
-        const float x = column_sum(bound[tt]);
-        mt = fmaxf(mt, x);
-        f16_scale(x * most, sw[tt], iw[tt]);
-        if (w == 0 && q4 == 0) s_row[r * kC + 16 * tt + n16] = iw[tt];
-      }
-      if (w < kKs) {
-        float4 z[2][2];
-#pragma unroll
-        for (int s = 0; s < 2; ++s)
-#pragma unroll
-          for (int e = 0; e < 2; ++e) z[s][e] = *reinterpret_cast<const float4*>(decay + 32 * s + 4 * q4 + 16 * e);
-#pragma unroll
-        for (int tt = 0; tt < 4; ++tt) {
-          f32x4 c[2] = {};
-#pragma unroll
-          for (int s = 0; s <= tt / 2; ++s) {
-            const float* f = inv[lower_step(tt, s)];
-            const float4 z0 = z[s][0], z1 = z[s][1];
-            const float y[8] = {f[0] * z0.x, f[1] * z0.y, f[2] * z0.z, f[3] * z0.w, f[4] * z1.x, f[5] * z1.y, f[6] * z1.z, f[7] * z1.w};
-            const Pair x = split(y, sw[tt]);
-#pragma unroll
-            for (int e = 0; e < 2; ++e) c[e] = mma3(kt[2 * e + s], x, c[e]);
-          }
-          const float y[8] = {c[0][0], c[0][1], c[0][2], c[0][3], c[1][0], c[1][1], c[1][2], c[1][3]};
-          store_pair(vws, w * 4 + tt, lane, split(y, 1.0f / kUnit));
-        }
-      }
-      if (w == 3) {  // a token a lane; the decay to the chunk's end
-        float* sc = reinterpret_cast<float*>(vws + layout.scalars_at());
-        sc[kC + lane] = decay[lane];
-        sc[2 * kC + lane] = __expf(float(lg[kC - 1] - lg[lane]));
-        if (lane == 0) sc[3 * kC] = decay[kC - 1];
-      }
-      if (w == 0) reinterpret_cast<float*>(vws + layout.scalars_at())[lane] = s_row[r * kC + lane];
-      __builtin_amdgcn_sched_barrier(0);
-      if (own_v) {  // U: rows are tokens, columns this wave's channels
-        float v[2][2][8];  // [channel][step]
-        float2 old[3];     // before the chunk
-#pragma unroll
-        for (int i = 0; i < 3; ++i) old[i] = make_float2(one_of(raw[0][0][i], 0), one_of(raw[0][0][i], 1));
-        if (n0 == 0 && q4 == 0) {
-#pragma unroll
-          for (int i = 0; i < 3; ++i) old[i] = *reinterpret_cast<const float2*>(cs + 2 * a.Hk * dk + h * dv + ch + size_t(i) * C);
-        }
-#pragma unroll
-        for (int c = 0; c < 2; ++c) {
-          const float4 cw = *reinterpret_cast<const float4*>(a.conv_w + (size_t(2) * a.Hk * dk + h * dv + ch + c) * 4);
-#pragma unroll
-          for (int s = 0; s < 2; ++s)
-#pragma unroll
-            for (int e = 0; e < 2; ++e)
-#pragma unroll
-              for (int i = 0; i < 4; ++i) {
-                auto x = [&](int k) { return s + e == 0 && i + k < 3 ? one_of(old[i + k], c) : one_of(raw[s][e][i + k], c); };
-                v[c][s][4 * e + i] = silu(cw.x * x(0) + cw.y * x(1) + cw.z * x(2) + cw.w * x(3));
-              }
-        }
-        if (r + 1 < nr) fetch_values(h + 1);
-        float st, it, sv[2], iv[2];
-        f16_scale(group_max<16>(mt), st, it);
-        Pair vp[2][2];
-#pragma unroll
-        for (int c = 0; c < 2; ++c) {
-          float mv = 0.0f;
-#pragma unroll
-          for (int e = 0; e < 8; ++e) mv = fmaxf(mv, fmaxf(fabsf(v[c][0][e]), fabsf(v[c][1][e])));
-          f16_scale(column_max(mv), sv[c], iv[c]);
-#pragma unroll
-          for (int s = 0; s < 2; ++s) vp[c][s] = split(v[c][s], sv[c]);
-        }
-#pragma unroll
-        for (int tt = 0; tt < 4; ++tt) {
-          f32x4 x[2] = {};
-#pragma unroll
-          for (int s = 0; s <= tt / 2; ++s) {
-            const Pair y = split(inv[lower_step(tt, s)], st);
-#pragma unroll
-            for (int c = 0; c < 2; ++c) x[c] = mma3(y, vp[c][s], x[c]);
-          }
-#pragma unroll
-          for (int c = 0; c < 2; ++c) {
-            // the two scales apart: their product may leave the range
-            x[c] *= it;
-            x[c] *= iv[c];
-            char* d = vws + layout.u_at() + (size_t(ch / 16) * 4 + tt) * kFrag + (16 * q4 + ch % 16 + c) * 16;
-            *reinterpret_cast<f32x4*>(d) = x[c];  // of 16 channels each is written twice, the same
-          }
-        }
+      for (int n = 0; n < 2; ++n) {
+        const int u = w + 4 * n;
+        if (u >= 6) continue;
+        const float* x = s_t + (r * kC + 16 * lower_tile(u) + n16) * kLd + 32 * lower_col(u) + 4 * q4;
+        const float4 y = *reinterpret_cast<const float4*>(x), z = *reinterpret_cast<const float4*>(x + 16);
+        const float f[8] = {y.x, y.y, y.z, y.w, z.x, z.y, z.z, z.w};
+        store_pair(t_out, u, lane, split(f, s_scale[r]));
       }
     }
     __syncthreads();  // the matrices are read
@@ -592,90 +461,133 @@ __global__ __launch_bounds__(kPrepThreads, 2) void chunk_kernel(ChainArgs a, Par
 // channels; the waves of a workgroup share the chunk's operands in LDS.
 //
 // Operands come into LDS past the registers, each into the place of the last
-// chunk's as soon as that is read: W, U and Q behind the products with the
-// state, Y and K^T behind those with V'.  A wave's loads and stores complete in
-// order, so each wait names how many were issued after what it needs (or
-// fewer).  The compiler has no loads of its own in the loop: it would wait for all.
+// chunk's as soon as that is read: K, Q and (I + A)^-1 behind the products with
+// the state, Y and K^T behind those with V'; the raw values of the next chunk
+// with these.  The compiler has no loads of its own in the loop: it would wait
+// for all.
 //
 // With one wave a SIMD nothing hides an LDS read but the wave's own products:
 // operand pairs are read a group of four ahead of them, two accumulators in turn
 // (12 products of 16 clocks over about 130 of a read).
 // ---------------------------------------------------------------------------
-template <int DKP, int NW>
+template <typename TIn, int DKP, int NW>
 struct Scan {
   static constexpr int kKs = DKP / 32;
-  static constexpr int kQ = kKs * 8 * kFrag;  // bytes of Q, of K^T, of W
-  static constexpr int kY = 16 * kFrag;       // Y, and what follows, so that the waves have the same loads
-  static constexpr int kLds = 3 * kQ + kY + 2 * kFrag + NW * 4 * kFrag;
-  static constexpr int kLoadsQ = kQ / kFrag / NW, kLoadsY = kY / kFrag / NW, kLoadsU = 4 + 1;  // of a wave
+  static constexpr int kQ = kKs * 8 * kFrag;  // bytes of K, of Q, of K^T
+  static constexpr int kPieces = NW * int(sizeof(TIn));  // 16 bytes each, of a row of raw values
+  static constexpr int kRaw = ((kC + 3) * kPieces + kWave - 1) / kWave * kFrag;
+  static constexpr int kLds = 3 * kQ + 24 * kFrag + 2 * kFrag + kRaw;
 };
 
-// At most N of this wave's loads and stores are on their way, its LDS reads are
-// done; then the workgroup's.
-template <int N, int NW>
+// This wave's loads and stores are done and its LDS reads; then the workgroup's.
+template <int NW>
 __device__ __forceinline__ void arrive() {
-  asm volatile("s_waitcnt vmcnt(%0) lgkmcnt(0)" ::"i"(N < 63 ? N : 63) : "memory");
+  asm volatile("s_waitcnt vmcnt(0) lgkmcnt(0)" ::: "memory");
   if constexpr (NW > 1) __builtin_amdgcn_s_barrier();
   asm volatile("" ::: "memory");
 }
 
-__device__ __forceinline__ void to_lds(const char* src, char* dst, int lane) {
-  __builtin_amdgcn_global_load_lds((const __attribute__((address_space(1))) void*)(src + lane * 16),
+// 64 lanes of 16 bytes to consecutive places of LDS
+typedef __attribute__((address_space(3))) char* LdsPtr;
+__device__ __forceinline__ void to_lds(const char* src, LdsPtr dst) {
+  __builtin_amdgcn_global_load_lds((const __attribute__((address_space(1))) void*)(src),
                                    (__attribute__((address_space(3))) void*)(dst), 16, 0, 0);
 }
 
-template <typename TOut, int DKP, int NW>
+template <typename TIn, typename TOut, int DKP, int NW>
 __global__ __launch_bounds__(NW * kWave) void scan_kernel(ChainArgs a, Part part) {
-  typedef Scan<DKP, NW> S;
+  typedef Scan<TIn, DKP, NW> S;
   constexpr int kKs = S::kKs;
   extern __shared__ __align__(16) char s_raw[];
-  char *s_w = s_raw, *s_q = s_w + S::kQ, *s_kt = s_q + S::kQ, *s_y = s_kt + S::kQ, *s_scalars = s_y + S::kY, *s_u = s_scalars + 2 * kFrag;
+  constexpr int kAtQ = S::kQ, kAtKt = 2 * S::kQ, kAtT = 3 * S::kQ, kAtY = kAtT + 12 * kFrag, kAtScalars = kAtY + 12 * kFrag,
+                kAtV = kAtScalars + 2 * kFrag;
+  const char *s_k = s_raw, *s_q = s_raw + kAtQ, *s_kt = s_raw + kAtKt, *s_t = s_raw + kAtT, *s_y = s_raw + kAtY, *s_v = s_raw + kAtV;
+  const LdsPtr lds = (LdsPtr)s_raw;
   const int tid = threadIdx.x, lane = tid % kWave, w = __builtin_amdgcn_readfirstlane(tid / kWave);
   const int n16 = lane & 15, q4 = lane >> 4;
   // workgroups go to the 8 XCDs in turn: those of a key head to one, whose L2
-  // gives them Q and K^T
+  // gives them K, Q and K^T
   const int each = gridDim.x * gridDim.y, id = blockIdx.y * gridDim.x + blockIdx.x;
   const int place = each % 8 == 0 ? id % 8 * (each / 8) + id / 8 : id;
   const int group = place % gridDim.x * NW + w, h = place / gridDim.x, b = part.b0 + blockIdx.z, hk = h / (a.Hv / a.Hk);
   const Tokens tk = tokens_of(a, b);
   const int dk = a.dk, dv = a.dv, end = min(part.c0 + part.M, (tk.n + kC - 1) / kC);
   if (part.c0 >= end) return;
-  const SlotLayout l = slot_layout(a.Hk, a.Hv, dk, dv);
+  const SlotLayout l = slot_layout(a.Hk, a.Hv, dk);
   const int ch = group * 16 + n16;  // value channel
   const char* vws = value_at(a, slot_at(a, part, blockIdx.z, 0), h);
   const char* kws = key_at(a, slot_at(a, part, blockIdx.z, 0), hk);
-  const size_t u_at = l.u_at() + size_t(group) * 4 * kFrag;
-  char* own_u = s_u + w * 4 * kFrag;
-  auto shared = [&](const char* src, char* to, int loads) {  // of all waves
+  auto shared = [&](const char* src, int to, int frags) {  // by all waves
 #pragma unroll
-    for (int n = 0; n < loads; ++n) to_lds(src + (n * NW + w) * kFrag, to + (n * NW + w) * kFrag, lane);
+    for (int n = 0; n < (frags + NW - 1) / NW; ++n) {
+      const int u = n * NW + w;
+      if (frags % NW == 0 || u < frags) to_lds(src + u * kFrag + lane * 16, lds + to + u * kFrag);
+    }
   };
-  auto load_first = [&](int m) {  // W, U, Q, scalars
-    const char* src = vws + size_t(m) * l.total;
-    shared(src, s_w, S::kLoadsQ);
-    shared(kws + size_t(m) * l.total, s_q, S::kLoadsQ);
-    to_lds(src + l.scalars_at(), s_scalars + (m & 1) * kFrag, lane);  // by every wave, the same
-#pragma unroll
-    for (int t = 0; t < 4; ++t) to_lds(src + u_at + t * kFrag, own_u + t * kFrag, lane);
+  auto load_first = [&](int m) {  // K, Q, (I + A)^-1, scalars
+    const char *k = kws + size_t(m) * l.total, *v = vws + size_t(m) * l.total;
+    shared(k, 0, 2 * S::kQ / kFrag);
+    shared(v, kAtT, 12);
+    shared(v + kScalarsAt, kAtScalars + (m & 1) * kFrag, 1);
     asm volatile("" ::: "memory");
   };
-  auto load_second = [&](int m) {  // Y, K^T
-    shared(vws + size_t(m) * l.total + l.y_at(), s_y, S::kLoadsY);
-    shared(kws + size_t(m) * l.total + S::kQ, s_kt, S::kLoadsQ);
+  // Raw values of chunk m's tokens and the three before: row i at i kPieces,
+  // its pieces traded by the quarter of i, so that the four rows of a read lie
+  // on different banks.  Rows outside the sequence are read as its first or last.
+  constexpr int kOwn = int(sizeof(TIn));  // pieces of 16 channels
+  auto piece_of = [](int row, int piece) { return piece ^ (((row >> 2) & 3) * kOwn & (S::kPieces - 1)); };
+  const char* values = reinterpret_cast<const char*>(reinterpret_cast<const TIn*>(a.v) + size_t(tk.first) * a.Hv * dv + h * dv +
+                                                     (group - w) * 16);
+  auto load_values = [&](int m) {
+    const int n0 = (part.c0 + m) * kC - 3;
+#pragma unroll
+    for (int n = 0; n < (S::kRaw / kFrag + NW - 1) / NW; ++n) {
+      const int u = n * NW + w, slot = u * kWave + lane, row = slot / S::kPieces, piece = piece_of(row, slot % S::kPieces);
+      const int i = min(max(n0 + row, 0), tk.n - 1);
+      if (u < S::kRaw / kFrag) to_lds(values + size_t(i) * a.Hv * dv * sizeof(TIn) + piece * 16, lds + kAtV + u * kFrag);
+    }
+  };
+  auto load_second = [&](int m, int next) {  // Y, K^T, the next chunk's raw values
+    shared(vws + size_t(m) * l.total + kYAt, kAtY, 12);
+    shared(kws + size_t(m) * l.total + 2 * S::kQ, kAtKt, S::kQ / kFrag);
+    load_values(next);
     asm volatile("" ::: "memory");
   };
+  load_values(0);
   load_first(0);
 
   float* state = a.S + ((size_t(b) * a.Hv + h) * dv + ch) * dk + 4 * q4;
   f32x4 st[DKP / 16];  // key channels 16 n + 4 q4 ..
 #pragma unroll
   for (int n = 0; n < DKP / 16; ++n) st[n] = 16 * n < dk ? *reinterpret_cast<const f32x4*>(state + 16 * n) : f32x4{};
+  const size_t C = 2 * size_t(a.Hk) * dk + size_t(a.Hv) * dv, channel = 2 * size_t(a.Hk) * dk + h * dv + ch;
+  const float4 cw = *reinterpret_cast<const float4*>(a.conv_w + channel * 4);
+  float old[3];  // before the sequence's first token
+#pragma unroll
+  for (int i = 0; i < 3; ++i) old[i] = a.conv_state[(size_t(b) * 3 + i) * C + channel];
   TOut* out = reinterpret_cast<TOut*>(a.out) + (size_t(tk.first) * a.Hv + h) * dv + ch;
   float mx = 0.0f;  // the largest of this lane's values
 #pragma unroll
   for (int n = 0; n < DKP / 16; ++n)
 #pragma unroll
     for (int r = 0; r < 4; ++r) mx = fmaxf(mx, fabsf(st[n][r]));
+
+  f32x4 v[4];  // convolved values of a chunk, rows 16 t + 4 q4 ..
+  auto convolve = [&](int m, int t) {
+    float x[7];
+#pragma unroll
+    for (int i = 0; i < 7; ++i) {
+      const int row = 16 * t + 4 * q4 + i;
+      x[i] = to_f32(*reinterpret_cast<const TIn*>(s_v + (row * S::kPieces + piece_of(row, (w * 16 + n16) * kOwn / 16)) * 16 +
+                                                  n16 * kOwn % 16));
+      if (t == 0 && i < 3 && part.c0 + m == 0 && q4 == 0) x[i] = old[i];
+    }
+#pragma unroll
+    for (int r = 0; r < 4; ++r) v[t][r] = silu(cw.x * x[r] + cw.y * x[r + 1] + cw.z * x[r + 2] + cw.w * x[r + 3]);
+  };
+  arrive<NW>();
+#pragma unroll
+  for (int t = 0; t < 4; ++t) convolve(0, t);
 
   f32x4 o[4];  // outputs of a chunk
   auto store = [&](int m) {
@@ -697,8 +609,8 @@ __global__ __launch_bounds__(NW * kWave) void scan_kernel(ChainArgs a, Part part
   };
 
   for (int m = 0; m < end - part.c0; ++m) {
-    const int next = min(m + 1, end - part.c0 - 1);  // loads go on behind the last chunk, so that waits stay the same
-    const float* s_sc = reinterpret_cast<const float*>(s_scalars + (m & 1) * kFrag);
+    const int next = min(m + 1, end - part.c0 - 1);  // the last chunk's again: they are not used
+    const float* s_sc = reinterpret_cast<const float*>(s_raw + kAtScalars + (m & 1) * kFrag);
     float ss, is;  // the state as an operand
     f16_scale(column_max(mx), ss, is);
     Pair sp[kKs];
@@ -708,13 +620,12 @@ __global__ __launch_bounds__(NW * kWave) void scan_kernel(ChainArgs a, Part part
                           st[2 * s + 1][0], st[2 * s + 1][1], st[2 * s + 1][2], st[2 * s + 1][3]};
       sp[s] = split(y, ss);
     }
-    arrive<0, NW>();  // W, U, Q, scalars; the last chunk's Y and K^T are read
+    arrive<NW>();  // K, Q, (I + A)^-1, scalars; the last chunk's Y and K^T, the raw values are read
     if (m) store(m - 1);  // here: the next wait is a part away
-    load_second(m);
+    load_second(m, next);
 
-    // V' = U - W S^T, and Q S^T.  Group n: token tiles 2 (n / (kKs / 2)) and the
-    // next, steps 2 (n % (kKs / 2)) and the next (one step of two groups' tiles
-    // where there is one step only).
+    // K S^T and Q S^T.  Group n: token tiles 2 (n / kPer) and the next, kSteps
+    // steps from n % kPer kSteps on.
     constexpr int kPer = kKs > 1 ? kKs / 2 : 1, kGroups = 2 * kPer, kSteps = kKs > 1 ? 2 : 1;
     Pair f[2][2 * kSteps];
     auto read = [&](Pair (&f)[2 * kSteps], const char* from, int n) {
@@ -735,39 +646,88 @@ __global__ __launch_bounds__(NW * kWave) void scan_kernel(ChainArgs a, Part part
         c[t + 1] = mma(f[2 * k + 1].hi, y.hi, c[t + 1]);
       }
     };
-    f32x4 p[4] = {};
+    // A lower triangular operand: tiles 0, 1 and the first step of 2, 3; then their second.
+    Pair g[2][4];
+    auto read_lower = [&](Pair (&f)[4], const char* from, int n) {
+#pragma unroll
+      for (int k = 0; k < 4 - 2 * n; ++k) f[k] = load_pair(from, n ? lower_step(2 + k, 1) : lower_step(k, 0), lane);
+    };
+    auto times_lower = [&](const Pair (&f)[4], const Pair& y, f32x4 (&c)[4], int n) {
+#pragma unroll
+      for (int k = 0; k < 4 - 2 * n; ++k) c[2 * n + k] = mma(f[k].lo, y.hi, c[2 * n + k]);
+#pragma unroll
+      for (int k = 0; k < 4 - 2 * n; ++k) c[2 * n + k] = mma(f[k].hi, y.lo, c[2 * n + k]);
+#pragma unroll
+      for (int k = 0; k < 4 - 2 * n; ++k) c[2 * n + k] = mma(f[k].hi, y.hi, c[2 * n + k]);
+    };
+    f32x4 x[4] = {};
 #pragma unroll
     for (int t = 0; t < 4; ++t) o[t] = f32x4{};
-    float mv = 0.0f, md = 0.0f, sv, iv, sd, id;
-    f32x4 x[4], xd[4];  // xd: decayed to the chunk's end
-    auto value = [&](int t) {
-      const f32x4 rs = *reinterpret_cast<const f32x4*>(s_sc + 16 * t + 4 * q4);
-      const f32x4 dec = *reinterpret_cast<const f32x4*>(s_sc + 2 * kC + 16 * t + 4 * q4);
-      const f32x4 u = *reinterpret_cast<const f32x4*>(own_u + t * kFrag + lane * 16);
-#pragma unroll
-      for (int r = 0; r < 4; ++r) {
-        x[t][r] = u[r] - p[t][r] * rs[r] * is;
-        xd[t][r] = x[t][r] * dec[r];
-        mv = fmaxf(mv, fabsf(x[t][r]));
-        md = fmaxf(md, fabsf(xd[t][r]));
-      }
-    };
-    read(f[0], s_w, 0);
+    read(f[0], s_k, 0);
 #pragma unroll
     for (int n = 0; n < kGroups; ++n) {
-      if (n + 1 < kGroups) read(f[(n + 1) & 1], s_w, n + 1);
+      if (n + 1 < kGroups) read(f[(n + 1) & 1], s_k, n + 1);
       else read(f[kGroups & 1], s_q, 0);
       __builtin_amdgcn_sched_barrier(0);
-      times(f[n & 1], p, n);
+      times(f[n & 1], x, n);
       __builtin_amdgcn_sched_barrier(0);
     }
+    // beta (V - e^g K S^T), beside half of the queries' products
+    float mr = 0.0f, sr, ir;
+    const float ik = is * (1.0f / kUnit);
 #pragma unroll
-    for (int n = 0; n < kGroups; ++n) {
+    for (int n = 0; n < kGroups / 2; ++n) {
+      read(f[(kGroups + n + 1) & 1], s_q, n + 1);
+      __builtin_amdgcn_sched_barrier(0);
+      times(f[(kGroups + n) & 1], o, n);
+#pragma unroll
+      for (int t = n * 8 / kGroups; t < (n + 1) * 8 / kGroups; ++t) {
+        const f32x4 be = *reinterpret_cast<const f32x4*>(s_sc + 16 * t + 4 * q4);
+        const f32x4 dec = *reinterpret_cast<const f32x4*>(s_sc + kC + 16 * t + 4 * q4);
+#pragma unroll
+        for (int r = 0; r < 4; ++r) {
+          x[t][r] = be[r] * (v[t][r] - dec[r] * (x[t][r] * ik));
+          mr = fmaxf(mr, fabsf(x[t][r]));
+        }
+      }
+      __builtin_amdgcn_sched_barrier(0);
+    }
+    f16_scale(column_max(mr), sr, ir);
+    Pair rp[2];
+#pragma unroll
+    for (int s = 0; s < 2; ++s) {
+      const float y[8] = {x[2 * s][0], x[2 * s][1], x[2 * s][2], x[2 * s][3],
+                          x[2 * s + 1][0], x[2 * s + 1][1], x[2 * s + 1][2], x[2 * s + 1][3]};
+      rp[s] = split(y, sr);
+    }
+    read_lower(g[0], s_t, 0);
+    read_lower(g[1], s_t, 1);
+    __builtin_amdgcn_sched_barrier(0);
+#pragma unroll
+    for (int t = 0; t < 4; ++t) x[t] = f32x4{};
+    times_lower(g[0], rp[0], x, 0);
+    times_lower(g[1], rp[1], x, 1);
+    __builtin_amdgcn_sched_barrier(0);
+    // V', and decayed to the chunk's end, beside the others
+    float mv = 0.0f, md = 0.0f, sv, iv, sd, id;
+    const float it = s_sc[3 * kC + 1] * ir, last = s_sc[3 * kC];
+    f32x4 xd[4];
+#pragma unroll
+    for (int n = kGroups / 2; n < kGroups; ++n) {
       if (n + 1 < kGroups) read(f[(kGroups + n + 1) & 1], s_q, n + 1);
       __builtin_amdgcn_sched_barrier(0);
       times(f[(kGroups + n) & 1], o, n);
 #pragma unroll
-      for (int t = n * 4 / kGroups; t < (n + 1) * 4 / kGroups; ++t) value(t);
+      for (int t = n * 8 / kGroups - 4; t < (n + 1) * 8 / kGroups - 4; ++t) {
+        const f32x4 dec = *reinterpret_cast<const f32x4*>(s_sc + 2 * kC + 16 * t + 4 * q4);
+#pragma unroll
+        for (int r = 0; r < 4; ++r) {
+          x[t][r] *= it;
+          xd[t][r] = x[t][r] * dec[r];
+          mv = fmaxf(mv, fabsf(x[t][r]));
+          md = fmaxf(md, fabsf(xd[t][r]));
+        }
+      }
       __builtin_amdgcn_sched_barrier(0);
     }
     f16_scale(column_max(mv), sv, iv);
@@ -782,40 +742,25 @@ __global__ __launch_bounds__(NW * kWave) void scan_kernel(ChainArgs a, Part part
       vp[s] = split(y, sv);
       vd[s] = split(z, sd);
     }
-    const float last = s_sc[3 * kC];
-    arrive<0, NW>();  // Y, K^T; W, U and Q are read
+    arrive<NW>();  // Y, K^T, raw values; K, Q and (I + A)^-1 are read
     load_first(next);
 
-    // outputs: rows of Y V' beside those of Q S^T; then the state behind the chunk
+    // outputs: Y V' beside Q S^T; then the state behind the chunk, and the next
+    // chunk's values
     f32x4 y[4] = {};
-    Pair g[2][4];
-    auto read_y = [&](Pair (&f)[4], int n) {  // tiles 0, 1 and the first step of 2, 3; their second
-#pragma unroll
-      for (int k = 0; k < 4 - 2 * n; ++k) f[k] = load_pair(s_y, n ? lower_step(2 + k, 1) : lower_step(k, 0), lane);
-    };
     auto read_k = [&](Pair (&f)[4], int n) {
 #pragma unroll
       for (int k = 0; k < 4; ++k) f[k] = load_pair(s_kt, 4 * n + k, lane);
     };
-    read_y(g[0], 0);
-    read_y(g[1], 1);
+    read_lower(g[0], s_y, 0);
+    read_lower(g[1], s_y, 1);
     __builtin_amdgcn_sched_barrier(0);
-#pragma unroll
-    for (int k = 0; k < 4; ++k) y[k] = mma(g[0][k].lo, vp[0].hi, y[k]);
-#pragma unroll
-    for (int k = 0; k < 4; ++k) y[k] = mma(g[0][k].hi, vp[0].lo, y[k]);
-#pragma unroll
-    for (int k = 0; k < 4; ++k) y[k] = mma(g[0][k].hi, vp[0].hi, y[k]);
+    times_lower(g[0], vp[0], y, 0);
     read_k(g[0], 0);
     __builtin_amdgcn_sched_barrier(0);
-#pragma unroll
-    for (int k = 0; k < 2; ++k) y[2 + k] = mma(g[1][k].lo, vp[1].hi, y[2 + k]);
-#pragma unroll
-    for (int k = 0; k < 2; ++k) y[2 + k] = mma(g[1][k].hi, vp[1].lo, y[2 + k]);
-#pragma unroll
-    for (int k = 0; k < 2; ++k) y[2 + k] = mma(g[1][k].hi, vp[1].hi, y[2 + k]);
+    times_lower(g[1], vp[1], y, 1);
     iv *= a.scale * (1.0f / kUnit);
-    const float io = is * (a.scale * (1.0f / kUnit));
+    const float io = ik * a.scale;
     id *= 1.0f / kUnit;
     mx = 0.0f;
 #pragma unroll
@@ -833,12 +778,13 @@ __global__ __launch_bounds__(NW * kWave) void scan_kernel(ChainArgs a, Part part
         c[0] = mma(f[s].hi, vd[s].hi, c[0]);
         c[1] = mma(f[2 + s].hi, vd[s].hi, c[1]);
       }
-      // outputs of a share of the tiles beside these products
+      // a share of the outputs and of the next values beside these products
 #pragma unroll
       for (int t = n * 4 / (DKP / 32); t < (n + 1) * 4 / (DKP / 32); ++t) {
         const f32x4 dec = *reinterpret_cast<const f32x4*>(s_sc + kC + 16 * t + 4 * q4);
 #pragma unroll
         for (int r = 0; r < 4; ++r) o[t][r] = o[t][r] * dec[r] * io + y[t][r] * iv;
+        convolve(next, t);
       }
 #pragma unroll
       for (int e = 0; e < 2; ++e)
@@ -892,39 +838,45 @@ int launch_prep(const ChainArgs& a, const Part& p, hipStream_t stream) {
   return after_launch();
 }
 
-template <typename TOut, int DKP, int NW>
+template <typename TIn, typename TOut, int DKP, int NW>
 int launch_waves(const ChainArgs& a, const Part& p, hipStream_t stream) {
-  constexpr int lds = Scan<DKP, NW>::kLds;
-  const int rc = ensure_dynamic_lds(reinterpret_cast<const void*>(scan_kernel<TOut, DKP, NW>), lds, "chain");
+  constexpr int lds = Scan<TIn, DKP, NW>::kLds;
+  const int rc = ensure_dynamic_lds(reinterpret_cast<const void*>(scan_kernel<TIn, TOut, DKP, NW>), lds, "chain");
   if (rc != GDN_OK) return rc;
-  scan_kernel<TOut, DKP, NW><<<dim3(a.dv / 16 / NW, a.Hv, p.G), NW * kWave, lds, stream>>>(a, p);
+  scan_kernel<TIn, TOut, DKP, NW><<<dim3(a.dv / 16 / NW, a.Hv, p.G), NW * kWave, lds, stream>>>(a, p);
   return after_launch();
 }
 
-template <typename TOut, int DKP>
+template <typename TIn, typename TOut, int DKP>
 int launch_scan(const ChainArgs& a, const Part& p, hipStream_t stream) {
   // waves of a workgroup: as many as share a head, but a workgroup a CU
   const int groups = a.dv / 16;
   int nw = groups;
   while (nw > 1 && (long long)(p.G) * a.Hv * (groups / nw) < 192) nw /= 2;
-  if (nw >= 8) return launch_waves<TOut, DKP, 8>(a, p, stream);
-  if (nw == 4) return launch_waves<TOut, DKP, 4>(a, p, stream);
-  if (nw == 2) return launch_waves<TOut, DKP, 2>(a, p, stream);
-  return launch_waves<TOut, DKP, 1>(a, p, stream);
+  if (nw >= 8) return launch_waves<TIn, TOut, DKP, 8>(a, p, stream);
+  if (nw == 4) return launch_waves<TIn, TOut, DKP, 4>(a, p, stream);
+  if (nw == 2) return launch_waves<TIn, TOut, DKP, 2>(a, p, stream);
+  return launch_waves<TIn, TOut, DKP, 1>(a, p, stream);
 }
 
-template <int DKP>
+template <typename TIn, int DKP>
 int launch_part(const ChainArgs& a, const Part& p, hipStream_t stream) {
-  int rc = a.in_dtype == GDN_BF16 ? launch_prep<BF16, DKP>(a, p, stream) : launch_prep<float, DKP>(a, p, stream);
+  const int rc = launch_prep<TIn, DKP>(a, p, stream);
   if (rc != GDN_OK) return rc;
-  return a.out_dtype == GDN_BF16 ? launch_scan<BF16, DKP>(a, p, stream) : launch_scan<float, DKP>(a, p, stream);
+  return a.out_dtype == GDN_BF16 ? launch_scan<TIn, BF16, DKP>(a, p, stream) : launch_scan<TIn, float, DKP>(a, p, stream);
+}
+
+template <typename TIn>
+int launch_type(const ChainArgs& a, const Part& p, hipStream_t stream) {
+  if (padded_dk(a.dk) == 32) return launch_part<TIn, 32>(a, p, stream);
+  return a.dk == 64 ? launch_part<TIn, 64>(a, p, stream) : launch_part<TIn, 128>(a, p, stream);
 }
 
 }  // namespace
 
 int launch_chain_chunks(const ChainArgs& a, hipStream_t stream) {
   const StreamOrder order(stream);
-  const size_t slot = slot_layout(a.Hk, a.Hv, a.dk, a.dv).total;
+  const size_t slot = slot_layout(a.Hk, a.Hv, a.dk).total;
   const int chunks = (a.T + kC - 1) / kC;
   const long long slots = std::max<long long>(1, (long long)(GDN_CHAIN_WORKSPACE / slot));
   Part p;
@@ -941,9 +893,7 @@ int launch_chain_chunks(const ChainArgs& a, hipStream_t stream) {
   for (p.b0 = 0; p.b0 < a.B; p.b0 += G) {
     p.G = std::min(G, a.B - p.b0);
     for (p.c0 = 0; p.c0 < chunks; p.c0 += p.M) {
-      rc = padded_dk(a.dk) == 32 ? launch_part<32>(a, p, stream)
-           : a.dk == 64          ? launch_part<64>(a, p, stream)
-                                 : launch_part<128>(a, p, stream);
+      rc = a.in_dtype == GDN_BF16 ? launch_type<BF16>(a, p, stream) : launch_type<float>(a, p, stream);
       if (rc != GDN_OK) return rc;
     }
   }
