@@ -457,8 +457,155 @@ __global__ __launch_bounds__(kPrepThreads, 2) void chunk_kernel(ChainArgs a, Par
 }
 
 // ---------------------------------------------------------------------------
-// The chunks of a sequence in turn.  A wave holds the state of 16 value
-// channels; the waves of a workgroup share the chunk's operands in LDS.
+// The chunks of a sequence in turn: parts of both forms of the scan.
+// ---------------------------------------------------------------------------
+// Two tiles of accumulators as an operand.
+__device__ __forceinline__ Pair operand(const f32x4& x, const f32x4& y, float scale) {
+  const float z[8] = {x[0], x[1], x[2], x[3], y[0], y[1], y[2], y[3]};
+  return split(z, scale);
+}
+
+// Products of K or Q (rows: tokens, kKs steps of channels) with the state.
+// Group n: token tiles 2 (n / kPer) and the next, kSteps steps from
+// n % kPer kSteps on; two accumulators in turn.
+template <int kKs>
+struct Rows {
+  static constexpr int kPer = kKs > 1 ? kKs / 2 : 1, kGroups = 2 * kPer, kSteps = kKs > 1 ? 2 : 1;
+  typedef Pair Group[2 * kSteps];
+  static __device__ __forceinline__ void read(Group& f, const char* from, int n, int lane) {
+#pragma unroll
+    for (int k = 0; k < 2 * kSteps; ++k) f[k] = load_pair(from, (n % kPer * kSteps + k / 2) * 4 + n / kPer * 2 + k % 2, lane);
+  }
+  static __device__ __forceinline__ void times(const Group& f, const Pair (&sp)[kKs], f32x4 (&c)[4], int n) {
+    const int t = n / kPer * 2, s = n % kPer * kSteps;
+#pragma unroll
+    for (int k = 0; k < kSteps; ++k) {
+      const Pair& y = sp[s + k];
+      c[t] = mma(f[2 * k].lo, y.hi, c[t]);
+      c[t + 1] = mma(f[2 * k + 1].lo, y.hi, c[t + 1]);
+      c[t] = mma(f[2 * k].hi, y.lo, c[t]);
+      c[t + 1] = mma(f[2 * k + 1].hi, y.lo, c[t + 1]);
+      c[t] = mma(f[2 * k].hi, y.hi, c[t]);
+      c[t + 1] = mma(f[2 * k + 1].hi, y.hi, c[t + 1]);
+    }
+  }
+};
+
+// Products of a lower triangular operand: n = 0: tiles 0, 1 and the first step
+// of 2, 3; n = 1: their second.
+__device__ __forceinline__ void read_lower(Pair (&f)[4], const char* from, int n, int lane) {
+#pragma unroll
+  for (int k = 0; k < 4 - 2 * n; ++k) f[k] = load_pair(from, n ? lower_step(2 + k, 1) : lower_step(k, 0), lane);
+}
+__device__ __forceinline__ void times_lower(const Pair (&f)[4], const Pair& y, f32x4 (&c)[4], int n) {
+#pragma unroll
+  for (int k = 0; k < 4 - 2 * n; ++k) c[2 * n + k] = mma(f[k].lo, y.hi, c[2 * n + k]);
+#pragma unroll
+  for (int k = 0; k < 4 - 2 * n; ++k) c[2 * n + k] = mma(f[k].hi, y.lo, c[2 * n + k]);
+#pragma unroll
+  for (int k = 0; k < 4 - 2 * n; ++k) c[2 * n + k] = mma(f[k].hi, y.hi, c[2 * n + k]);
+}
+
+// Products of K^T: group n: tiles 2 n and 2 n + 1 of 16 key channels.
+__device__ __forceinline__ void read_kt(Pair (&f)[4], const char* from, int n, int lane) {
+#pragma unroll
+  for (int k = 0; k < 4; ++k) f[k] = load_pair(from, 4 * n + k, lane);
+}
+__device__ __forceinline__ void times_kt(const Pair (&f)[4], const Pair (&vd)[2], f32x4 (&c)[2]) {
+#pragma unroll
+  for (int s = 0; s < 2; ++s) {
+    c[0] = mma(f[s].lo, vd[s].hi, c[0]);
+    c[1] = mma(f[2 + s].lo, vd[s].hi, c[1]);
+    c[0] = mma(f[s].hi, vd[s].lo, c[0]);
+    c[1] = mma(f[2 + s].hi, vd[s].lo, c[1]);
+    c[0] = mma(f[s].hi, vd[s].hi, c[0]);
+    c[1] = mma(f[2 + s].hi, vd[s].hi, c[1]);
+  }
+}
+
+// This wave's loads and stores are done and its LDS reads; then the workgroup's.
+template <int NW>
+__device__ __forceinline__ void arrive() {
+  asm volatile("s_waitcnt vmcnt(0) lgkmcnt(0)" ::: "memory");
+  if constexpr (NW > 1) __builtin_amdgcn_s_barrier();
+  asm volatile("" ::: "memory");
+}
+
+// 64 lanes of 16 bytes to consecutive places of LDS: from base + at
+typedef __attribute__((address_space(3))) char* LdsPtr;
+__device__ __forceinline__ void to_lds(const char* base, unsigned at, LdsPtr dst) {
+  __builtin_amdgcn_global_load_lds((const __attribute__((address_space(1))) void*)(base + at),
+                                   (__attribute__((address_space(3))) void*)(dst), 16, 0, 0);
+}
+
+// Raw values of a chunk's tokens and the three before, of NG groups of 16
+// channels: row i at i kPieces, its pieces of 16 bytes traded by the quarter of
+// i, so that the four rows of a read lie on different banks.  Rows outside the
+// sequence are read as its first or last.
+template <typename TIn, int NG>
+struct RawRows {
+  static constexpr int kOwn = int(sizeof(TIn)), kPieces = NG * kOwn;  // of a group, of a row
+  static constexpr int kFrags = ((kC + 3) * kPieces + kWave - 1) / kWave;
+  static __device__ __forceinline__ int place(int row, int piece) { return piece ^ (((row >> 2) & 3) * kOwn & (kPieces - 1)); }
+  // load u of chunk c; values: the sequence's first row
+  static __device__ __forceinline__ void load(const char* values, size_t stride, int n, int c, int u, int lane, LdsPtr to) {
+    const int slot = u * kWave + lane, row = slot / kPieces, piece = place(row, slot % kPieces);
+    const int i = min(max(c * kC - 3 + row, 0), n - 1);
+    to_lds(values + size_t(i) * stride + piece * 16, 0, to + u * kFrag);
+  }
+  static __device__ __forceinline__ float get(const char* s_v, int row, int group, int n16) {
+    return to_f32(*reinterpret_cast<const TIn*>(s_v + (row * kPieces + place(row, (group * 16 + n16) * kOwn / 16)) * 16 +
+                                                n16 * kOwn % 16));
+  }
+};
+
+// Convolved values of token tile t, rows 16 t + 4 q4 .. of channel n16; old:
+// those before the sequence, first: whether the chunk is its first.
+template <typename TIn, int NG>
+__device__ __forceinline__ f32x4 convolve(const char* s_v, int t, int group, int n16, int q4, float4 cw, const float (&old)[3],
+                                          bool first) {
+  float x[7];
+#pragma unroll
+  for (int i = 0; i < 7; ++i) {
+    x[i] = RawRows<TIn, NG>::get(s_v, 16 * t + 4 * q4 + i, group, n16);
+    if (t == 0 && i < 3) x[i] = first && q4 == 0 ? old[i] : x[i];
+  }
+  f32x4 v;
+#pragma unroll
+  for (int r = 0; r < 4; ++r) v[r] = silu(cw.x * x[r] + cw.y * x[r + 1] + cw.z * x[r + 2] + cw.w * x[r + 3]);
+  return v;
+}
+
+// Outputs of a chunk whose first row is `to` and that has n tokens left.
+template <typename TOut>
+__device__ __forceinline__ void store_chunk(TOut* to, size_t stride, int n, int q4, const f32x4 (&o)[4]) {
+  to += 4 * q4 * stride;
+  if (n >= kC) {
+#pragma unroll
+    for (int t = 0; t < 4; ++t)
+#pragma unroll
+      for (int r = 0; r < 4; ++r) put(to + (16 * t + r) * stride, o[t][r]);
+  } else {
+#pragma unroll
+    for (int t = 0; t < 4; ++t)
+#pragma unroll
+      for (int r = 0; r < 4; ++r)
+        if (16 * t + 4 * q4 + r < n) put(to + (16 * t + r) * stride, o[t][r]);
+  }
+  asm volatile("" ::: "memory");
+}
+
+// Head and slice of a workgroup.  Workgroups go to the 8 XCDs in turn: those of
+// a key head to one, whose L2 gives them K, Q and K^T.
+__device__ __forceinline__ int2 head_of() {
+  const int each = gridDim.x * gridDim.y, id = blockIdx.y * gridDim.x + blockIdx.x;
+  const int place = each % 8 == 0 ? id % 8 * (each / 8) + id / 8 : id;
+  return make_int2(place / gridDim.x, place % gridDim.x);
+}
+
+// ---------------------------------------------------------------------------
+// Many heads.  A wave holds the state of 16 value channels and does all with it;
+// the waves of a workgroup share the chunk's operands in LDS.
 //
 // Operands come into LDS past the registers, each into the place of the last
 // chunk's as soon as that is read: K, Q and (I + A)^-1 behind the products with
@@ -474,42 +621,25 @@ template <typename TIn, int DKP, int NW>
 struct Scan {
   static constexpr int kKs = DKP / 32;
   static constexpr int kQ = kKs * 8 * kFrag;  // bytes of K, of Q, of K^T
-  static constexpr int kPieces = NW * int(sizeof(TIn));  // 16 bytes each, of a row of raw values
-  static constexpr int kRaw = ((kC + 3) * kPieces + kWave - 1) / kWave * kFrag;
-  static constexpr int kLds = 3 * kQ + 24 * kFrag + 2 * kFrag + kRaw;
+  static constexpr int kAtQ = kQ, kAtKt = 2 * kQ, kAtT = 3 * kQ, kAtY = kAtT + 12 * kFrag, kAtScalars = kAtY + 12 * kFrag,
+                       kAtV = kAtScalars + 2 * kFrag;
+  static constexpr int kLds = kAtV + RawRows<TIn, NW>::kFrags * kFrag;
 };
-
-// This wave's loads and stores are done and its LDS reads; then the workgroup's.
-template <int NW>
-__device__ __forceinline__ void arrive() {
-  asm volatile("s_waitcnt vmcnt(0) lgkmcnt(0)" ::: "memory");
-  if constexpr (NW > 1) __builtin_amdgcn_s_barrier();
-  asm volatile("" ::: "memory");
-}
-
-// 64 lanes of 16 bytes to consecutive places of LDS
-typedef __attribute__((address_space(3))) char* LdsPtr;
-__device__ __forceinline__ void to_lds(const char* src, LdsPtr dst) {
-  __builtin_amdgcn_global_load_lds((const __attribute__((address_space(1))) void*)(src),
-                                   (__attribute__((address_space(3))) void*)(dst), 16, 0, 0);
-}
 
 template <typename TIn, typename TOut, int DKP, int NW>
 __global__ __launch_bounds__(NW * kWave) void scan_kernel(ChainArgs a, Part part) {
   typedef Scan<TIn, DKP, NW> S;
-  constexpr int kKs = S::kKs;
+  typedef Rows<S::kKs> R;
+  typedef RawRows<TIn, NW> Raw;
+  constexpr int kKs = S::kKs, kGroups = R::kGroups, kQFrags = S::kQ / kFrag;
   extern __shared__ __align__(16) char s_raw[];
-  constexpr int kAtQ = S::kQ, kAtKt = 2 * S::kQ, kAtT = 3 * S::kQ, kAtY = kAtT + 12 * kFrag, kAtScalars = kAtY + 12 * kFrag,
-                kAtV = kAtScalars + 2 * kFrag;
-  const char *s_k = s_raw, *s_q = s_raw + kAtQ, *s_kt = s_raw + kAtKt, *s_t = s_raw + kAtT, *s_y = s_raw + kAtY, *s_v = s_raw + kAtV;
+  const char *s_k = s_raw, *s_q = s_raw + S::kAtQ, *s_kt = s_raw + S::kAtKt, *s_t = s_raw + S::kAtT, *s_y = s_raw + S::kAtY,
+             *s_v = s_raw + S::kAtV;
   const LdsPtr lds = (LdsPtr)s_raw;
   const int tid = threadIdx.x, lane = tid % kWave, w = __builtin_amdgcn_readfirstlane(tid / kWave);
   const int n16 = lane & 15, q4 = lane >> 4;
-  // workgroups go to the 8 XCDs in turn: those of a key head to one, whose L2
-  // gives them K, Q and K^T
-  const int each = gridDim.x * gridDim.y, id = blockIdx.y * gridDim.x + blockIdx.x;
-  const int place = each % 8 == 0 ? id % 8 * (each / 8) + id / 8 : id;
-  const int group = place % gridDim.x * NW + w, h = place / gridDim.x, b = part.b0 + blockIdx.z, hk = h / (a.Hv / a.Hk);
+  const int2 hs = head_of();
+  const int group = hs.y * NW + w, h = hs.x, b = part.b0 + blockIdx.z, hk = h / (a.Hv / a.Hk);
   const Tokens tk = tokens_of(a, b);
   const int dk = a.dk, dv = a.dv, end = min(part.c0 + part.M, (tk.n + kC - 1) / kC);
   if (part.c0 >= end) return;
@@ -517,39 +647,31 @@ __global__ __launch_bounds__(NW * kWave) void scan_kernel(ChainArgs a, Part part
   const int ch = group * 16 + n16;  // value channel
   const char* vws = value_at(a, slot_at(a, part, blockIdx.z, 0), h);
   const char* kws = key_at(a, slot_at(a, part, blockIdx.z, 0), hk);
+  const unsigned at = lane * 16;
   auto shared = [&](const char* src, int to, int frags) {  // by all waves
 #pragma unroll
     for (int n = 0; n < (frags + NW - 1) / NW; ++n) {
       const int u = n * NW + w;
-      if (frags % NW == 0 || u < frags) to_lds(src + u * kFrag + lane * 16, lds + to + u * kFrag);
+      if (frags % NW == 0 || u < frags) to_lds(src + u * kFrag, at, lds + to + u * kFrag);
     }
+  };
+  const size_t vstride = size_t(a.Hv) * dv;
+  const char* values = reinterpret_cast<const char*>(reinterpret_cast<const TIn*>(a.v) + size_t(tk.first) * vstride + h * dv + hs.y * NW * 16);
+  auto load_values = [&](int m) {
+#pragma unroll
+    for (int n = 0; n < (Raw::kFrags + NW - 1) / NW; ++n)
+      if (n * NW + w < Raw::kFrags) Raw::load(values, vstride * sizeof(TIn), tk.n, part.c0 + m, n * NW + w, lane, lds + S::kAtV);
   };
   auto load_first = [&](int m) {  // K, Q, (I + A)^-1, scalars
     const char *k = kws + size_t(m) * l.total, *v = vws + size_t(m) * l.total;
-    shared(k, 0, 2 * S::kQ / kFrag);
-    shared(v, kAtT, 12);
-    shared(v + kScalarsAt, kAtScalars + (m & 1) * kFrag, 1);
+    shared(k, 0, 2 * kQFrags);
+    shared(v, S::kAtT, 12);
+    shared(v + kScalarsAt, S::kAtScalars + (m & 1) * kFrag, 1);
     asm volatile("" ::: "memory");
   };
-  // Raw values of chunk m's tokens and the three before: row i at i kPieces,
-  // its pieces traded by the quarter of i, so that the four rows of a read lie
-  // on different banks.  Rows outside the sequence are read as its first or last.
-  constexpr int kOwn = int(sizeof(TIn));  // pieces of 16 channels
-  auto piece_of = [](int row, int piece) { return piece ^ (((row >> 2) & 3) * kOwn & (S::kPieces - 1)); };
-  const char* values = reinterpret_cast<const char*>(reinterpret_cast<const TIn*>(a.v) + size_t(tk.first) * a.Hv * dv + h * dv +
-                                                     (group - w) * 16);
-  auto load_values = [&](int m) {
-    const int n0 = (part.c0 + m) * kC - 3;
-#pragma unroll
-    for (int n = 0; n < (S::kRaw / kFrag + NW - 1) / NW; ++n) {
-      const int u = n * NW + w, slot = u * kWave + lane, row = slot / S::kPieces, piece = piece_of(row, slot % S::kPieces);
-      const int i = min(max(n0 + row, 0), tk.n - 1);
-      if (u < S::kRaw / kFrag) to_lds(values + size_t(i) * a.Hv * dv * sizeof(TIn) + piece * 16, lds + kAtV + u * kFrag);
-    }
-  };
   auto load_second = [&](int m, int next) {  // Y, K^T, the next chunk's raw values
-    shared(vws + size_t(m) * l.total + kYAt, kAtY, 12);
-    shared(kws + size_t(m) * l.total + 2 * S::kQ, kAtKt, S::kQ / kFrag);
+    shared(vws + size_t(m) * l.total + kYAt, S::kAtY, 12);
+    shared(kws + size_t(m) * l.total + 2 * S::kQ, S::kAtKt, kQFrags);
     load_values(next);
     asm volatile("" ::: "memory");
   };
@@ -560,116 +682,54 @@ __global__ __launch_bounds__(NW * kWave) void scan_kernel(ChainArgs a, Part part
   f32x4 st[DKP / 16];  // key channels 16 n + 4 q4 ..
 #pragma unroll
   for (int n = 0; n < DKP / 16; ++n) st[n] = 16 * n < dk ? *reinterpret_cast<const f32x4*>(state + 16 * n) : f32x4{};
-  const size_t C = 2 * size_t(a.Hk) * dk + size_t(a.Hv) * dv, channel = 2 * size_t(a.Hk) * dk + h * dv + ch;
+  const size_t C = 2 * size_t(a.Hk) * dk + vstride, channel = 2 * size_t(a.Hk) * dk + h * dv + ch;
   const float4 cw = *reinterpret_cast<const float4*>(a.conv_w + channel * 4);
   float old[3];  // before the sequence's first token
 #pragma unroll
   for (int i = 0; i < 3; ++i) old[i] = a.conv_state[(size_t(b) * 3 + i) * C + channel];
-  TOut* out = reinterpret_cast<TOut*>(a.out) + (size_t(tk.first) * a.Hv + h) * dv + ch;
+  TOut* out = reinterpret_cast<TOut*>(a.out) + size_t(tk.first) * vstride + h * dv + ch;
+  auto store = [&](int m, const f32x4 (&o)[4]) {
+    const int n0 = (part.c0 + m) * kC;
+    store_chunk(out + size_t(n0) * vstride, vstride, tk.n - n0, q4, o);
+  };
   float mx = 0.0f;  // the largest of this lane's values
 #pragma unroll
   for (int n = 0; n < DKP / 16; ++n)
 #pragma unroll
     for (int r = 0; r < 4; ++r) mx = fmaxf(mx, fabsf(st[n][r]));
-
-  f32x4 v[4];  // convolved values of a chunk, rows 16 t + 4 q4 ..
-  auto convolve = [&](int m, int t) {
-    float x[7];
-#pragma unroll
-    for (int i = 0; i < 7; ++i) {
-      const int row = 16 * t + 4 * q4 + i;
-      x[i] = to_f32(*reinterpret_cast<const TIn*>(s_v + (row * S::kPieces + piece_of(row, (w * 16 + n16) * kOwn / 16)) * 16 +
-                                                  n16 * kOwn % 16));
-      if (t == 0 && i < 3 && part.c0 + m == 0 && q4 == 0) x[i] = old[i];
-    }
-#pragma unroll
-    for (int r = 0; r < 4; ++r) v[t][r] = silu(cw.x * x[r] + cw.y * x[r + 1] + cw.z * x[r + 2] + cw.w * x[r + 3]);
+  f32x4 v[4];  // convolved values of a chunk
+  auto values_of = [&](int m, int t) {
+    v[t] = convolve<TIn, NW>(s_v, t, w, n16, q4, cw, old, part.c0 + m == 0);
+    asm volatile("" : "+v"(v[t]));  // here, not at its use a chunk later
   };
   arrive<NW>();
 #pragma unroll
-  for (int t = 0; t < 4; ++t) convolve(0, t);
+  for (int t = 0; t < 4; ++t) values_of(0, t);
 
   f32x4 o[4];  // outputs of a chunk
-  auto store = [&](int m) {
-    const int n0 = (part.c0 + m) * kC;
-    TOut* to = out + size_t(n0 + 4 * q4) * a.Hv * dv;
-    if (n0 + kC <= tk.n) {
-#pragma unroll
-      for (int t = 0; t < 4; ++t)
-#pragma unroll
-        for (int r = 0; r < 4; ++r) put(to + size_t(16 * t + r) * a.Hv * dv, o[t][r]);
-    } else {
-#pragma unroll
-      for (int t = 0; t < 4; ++t)
-#pragma unroll
-        for (int r = 0; r < 4; ++r)
-          if (n0 + 16 * t + 4 * q4 + r < tk.n) put(to + size_t(16 * t + r) * a.Hv * dv, o[t][r]);
-    }
-    asm volatile("" ::: "memory");
-  };
-
   for (int m = 0; m < end - part.c0; ++m) {
     const int next = min(m + 1, end - part.c0 - 1);  // the last chunk's again: they are not used
-    const float* s_sc = reinterpret_cast<const float*>(s_raw + kAtScalars + (m & 1) * kFrag);
+    const float* s_sc = reinterpret_cast<const float*>(s_raw + S::kAtScalars + (m & 1) * kFrag);
     float ss, is;  // the state as an operand
     f16_scale(column_max(mx), ss, is);
     Pair sp[kKs];
 #pragma unroll
-    for (int s = 0; s < kKs; ++s) {
-      const float y[8] = {st[2 * s][0], st[2 * s][1], st[2 * s][2], st[2 * s][3],
-                          st[2 * s + 1][0], st[2 * s + 1][1], st[2 * s + 1][2], st[2 * s + 1][3]};
-      sp[s] = split(y, ss);
-    }
+    for (int s = 0; s < kKs; ++s) sp[s] = operand(st[2 * s], st[2 * s + 1], ss);
     arrive<NW>();  // K, Q, (I + A)^-1, scalars; the last chunk's Y and K^T, the raw values are read
-    if (m) store(m - 1);  // here: the next wait is a part away
+    if (m) store(m - 1, o);  // here: the next wait is a part away
     load_second(m, next);
 
-    // K S^T and Q S^T.  Group n: token tiles 2 (n / kPer) and the next, kSteps
-    // steps from n % kPer kSteps on.
-    constexpr int kPer = kKs > 1 ? kKs / 2 : 1, kGroups = 2 * kPer, kSteps = kKs > 1 ? 2 : 1;
-    Pair f[2][2 * kSteps];
-    auto read = [&](Pair (&f)[2 * kSteps], const char* from, int n) {
-#pragma unroll
-      for (int k = 0; k < 2 * kSteps; ++k)
-        f[k] = load_pair(from, (n % kPer * kSteps + k / 2) * 4 + n / kPer * 2 + k % 2, lane);
-    };
-    auto times = [&](const Pair (&f)[2 * kSteps], f32x4 (&c)[4], int n) {
-      const int t = n / kPer * 2, s = n % kPer * kSteps;
-#pragma unroll
-      for (int k = 0; k < kSteps; ++k) {
-        const Pair& y = sp[s + k];
-        c[t] = mma(f[2 * k].lo, y.hi, c[t]);
-        c[t + 1] = mma(f[2 * k + 1].lo, y.hi, c[t + 1]);
-        c[t] = mma(f[2 * k].hi, y.lo, c[t]);
-        c[t + 1] = mma(f[2 * k + 1].hi, y.lo, c[t + 1]);
-        c[t] = mma(f[2 * k].hi, y.hi, c[t]);
-        c[t + 1] = mma(f[2 * k + 1].hi, y.hi, c[t + 1]);
-      }
-    };
-    // A lower triangular operand: tiles 0, 1 and the first step of 2, 3; then their second.
-    Pair g[2][4];
-    auto read_lower = [&](Pair (&f)[4], const char* from, int n) {
-#pragma unroll
-      for (int k = 0; k < 4 - 2 * n; ++k) f[k] = load_pair(from, n ? lower_step(2 + k, 1) : lower_step(k, 0), lane);
-    };
-    auto times_lower = [&](const Pair (&f)[4], const Pair& y, f32x4 (&c)[4], int n) {
-#pragma unroll
-      for (int k = 0; k < 4 - 2 * n; ++k) c[2 * n + k] = mma(f[k].lo, y.hi, c[2 * n + k]);
-#pragma unroll
-      for (int k = 0; k < 4 - 2 * n; ++k) c[2 * n + k] = mma(f[k].hi, y.lo, c[2 * n + k]);
-#pragma unroll
-      for (int k = 0; k < 4 - 2 * n; ++k) c[2 * n + k] = mma(f[k].hi, y.hi, c[2 * n + k]);
-    };
+    typename R::Group f[2];
     f32x4 x[4] = {};
 #pragma unroll
     for (int t = 0; t < 4; ++t) o[t] = f32x4{};
-    read(f[0], s_k, 0);
+    R::read(f[0], s_k, 0, lane);
 #pragma unroll
     for (int n = 0; n < kGroups; ++n) {
-      if (n + 1 < kGroups) read(f[(n + 1) & 1], s_k, n + 1);
-      else read(f[kGroups & 1], s_q, 0);
+      if (n + 1 < kGroups) R::read(f[(n + 1) & 1], s_k, n + 1, lane);
+      else R::read(f[kGroups & 1], s_q, 0, lane);
       __builtin_amdgcn_sched_barrier(0);
-      times(f[n & 1], x, n);
+      R::times(f[n & 1], sp, x, n);
       __builtin_amdgcn_sched_barrier(0);
     }
     // beta (V - e^g K S^T), beside half of the queries' products
@@ -677,9 +737,9 @@ __global__ __launch_bounds__(NW * kWave) void scan_kernel(ChainArgs a, Part part
     const float ik = is * (1.0f / kUnit);
 #pragma unroll
     for (int n = 0; n < kGroups / 2; ++n) {
-      read(f[(kGroups + n + 1) & 1], s_q, n + 1);
+      R::read(f[(kGroups + n + 1) & 1], s_q, n + 1, lane);
       __builtin_amdgcn_sched_barrier(0);
-      times(f[(kGroups + n) & 1], o, n);
+      R::times(f[(kGroups + n) & 1], sp, o, n);
 #pragma unroll
       for (int t = n * 8 / kGroups; t < (n + 1) * 8 / kGroups; ++t) {
         const f32x4 be = *reinterpret_cast<const f32x4*>(s_sc + 16 * t + 4 * q4);
@@ -693,20 +753,15 @@ __global__ __launch_bounds__(NW * kWave) void scan_kernel(ChainArgs a, Part part
       __builtin_amdgcn_sched_barrier(0);
     }
     f16_scale(column_max(mr), sr, ir);
-    Pair rp[2];
-#pragma unroll
-    for (int s = 0; s < 2; ++s) {
-      const float y[8] = {x[2 * s][0], x[2 * s][1], x[2 * s][2], x[2 * s][3],
-                          x[2 * s + 1][0], x[2 * s + 1][1], x[2 * s + 1][2], x[2 * s + 1][3]};
-      rp[s] = split(y, sr);
-    }
-    read_lower(g[0], s_t, 0);
-    read_lower(g[1], s_t, 1);
+    const Pair r0 = operand(x[0], x[1], sr), r1 = operand(x[2], x[3], sr);
+    Pair g[2][4];
+    read_lower(g[0], s_t, 0, lane);
+    read_lower(g[1], s_t, 1, lane);
     __builtin_amdgcn_sched_barrier(0);
 #pragma unroll
     for (int t = 0; t < 4; ++t) x[t] = f32x4{};
-    times_lower(g[0], rp[0], x, 0);
-    times_lower(g[1], rp[1], x, 1);
+    times_lower(g[0], r0, x, 0);
+    times_lower(g[1], r1, x, 1);
     __builtin_amdgcn_sched_barrier(0);
     // V', and decayed to the chunk's end, beside the others
     float mv = 0.0f, md = 0.0f, sv, iv, sd, id;
@@ -714,9 +769,9 @@ __global__ __launch_bounds__(NW * kWave) void scan_kernel(ChainArgs a, Part part
     f32x4 xd[4];
 #pragma unroll
     for (int n = kGroups / 2; n < kGroups; ++n) {
-      if (n + 1 < kGroups) read(f[(kGroups + n + 1) & 1], s_q, n + 1);
+      if (n + 1 < kGroups) R::read(f[(kGroups + n + 1) & 1], s_q, n + 1, lane);
       __builtin_amdgcn_sched_barrier(0);
-      times(f[(kGroups + n) & 1], o, n);
+      R::times(f[(kGroups + n) & 1], sp, o, n);
 #pragma unroll
       for (int t = n * 8 / kGroups - 4; t < (n + 1) * 8 / kGroups - 4; ++t) {
         const f32x4 dec = *reinterpret_cast<const f32x4*>(s_sc + 2 * kC + 16 * t + 4 * q4);
@@ -732,31 +787,19 @@ __global__ __launch_bounds__(NW * kWave) void scan_kernel(ChainArgs a, Part part
     }
     f16_scale(column_max(mv), sv, iv);
     f16_scale(column_max(md), sd, id);
-    Pair vp[2], vd[2];
-#pragma unroll
-    for (int s = 0; s < 2; ++s) {
-      const float y[8] = {x[2 * s][0], x[2 * s][1], x[2 * s][2], x[2 * s][3],
-                          x[2 * s + 1][0], x[2 * s + 1][1], x[2 * s + 1][2], x[2 * s + 1][3]};
-      const float z[8] = {xd[2 * s][0], xd[2 * s][1], xd[2 * s][2], xd[2 * s][3],
-                          xd[2 * s + 1][0], xd[2 * s + 1][1], xd[2 * s + 1][2], xd[2 * s + 1][3]};
-      vp[s] = split(y, sv);
-      vd[s] = split(z, sd);
-    }
+    const Pair vp[2] = {operand(x[0], x[1], sv), operand(x[2], x[3], sv)};
+    const Pair vd[2] = {operand(xd[0], xd[1], sd), operand(xd[2], xd[3], sd)};
     arrive<NW>();  // Y, K^T, raw values; K, Q and (I + A)^-1 are read
     load_first(next);
 
     // outputs: Y V' beside Q S^T; then the state behind the chunk, and the next
     // chunk's values
     f32x4 y[4] = {};
-    auto read_k = [&](Pair (&f)[4], int n) {
-#pragma unroll
-      for (int k = 0; k < 4; ++k) f[k] = load_pair(s_kt, 4 * n + k, lane);
-    };
-    read_lower(g[0], s_y, 0);
-    read_lower(g[1], s_y, 1);
+    read_lower(g[0], s_y, 0, lane);
+    read_lower(g[1], s_y, 1, lane);
     __builtin_amdgcn_sched_barrier(0);
     times_lower(g[0], vp[0], y, 0);
-    read_k(g[0], 0);
+    read_kt(g[0], s_kt, 0, lane);
     __builtin_amdgcn_sched_barrier(0);
     times_lower(g[1], vp[1], y, 1);
     iv *= a.scale * (1.0f / kUnit);
@@ -765,26 +808,17 @@ __global__ __launch_bounds__(NW * kWave) void scan_kernel(ChainArgs a, Part part
     mx = 0.0f;
 #pragma unroll
     for (int n = 0; n < DKP / 32; ++n) {
-      if (n + 1 < DKP / 32) read_k(g[(n + 1) & 1], n + 1);
+      if (n + 1 < DKP / 32) read_kt(g[(n + 1) & 1], s_kt, n + 1, lane);
       __builtin_amdgcn_sched_barrier(0);
       f32x4 c[2] = {};
-      const Pair(&f)[4] = g[n & 1];
-#pragma unroll
-      for (int s = 0; s < 2; ++s) {
-        c[0] = mma(f[s].lo, vd[s].hi, c[0]);
-        c[1] = mma(f[2 + s].lo, vd[s].hi, c[1]);
-        c[0] = mma(f[s].hi, vd[s].lo, c[0]);
-        c[1] = mma(f[2 + s].hi, vd[s].lo, c[1]);
-        c[0] = mma(f[s].hi, vd[s].hi, c[0]);
-        c[1] = mma(f[2 + s].hi, vd[s].hi, c[1]);
-      }
+      times_kt(g[n & 1], vd, c);
       // a share of the outputs and of the next values beside these products
 #pragma unroll
       for (int t = n * 4 / (DKP / 32); t < (n + 1) * 4 / (DKP / 32); ++t) {
         const f32x4 dec = *reinterpret_cast<const f32x4*>(s_sc + kC + 16 * t + 4 * q4);
 #pragma unroll
         for (int r = 0; r < 4; ++r) o[t][r] = o[t][r] * dec[r] * io + y[t][r] * iv;
-        convolve(next, t);
+        values_of(next, t);
       }
 #pragma unroll
       for (int e = 0; e < 2; ++e)
@@ -796,11 +830,246 @@ __global__ __launch_bounds__(NW * kWave) void scan_kernel(ChainArgs a, Part part
       __builtin_amdgcn_sched_barrier(0);
     }
   }
-  store(end - part.c0 - 1);
+  store(end - part.c0 - 1, o);
   asm volatile("s_waitcnt vmcnt(0)" ::: "memory");  // nothing arrives in LDS after the end
 #pragma unroll
   for (int n = 0; n < DKP / 16; ++n)
     if (16 * n < dk) *reinterpret_cast<f32x4*>(state + 16 * n) = st[n];
+}
+
+// ---------------------------------------------------------------------------
+// Few heads: the recurrence is what takes time, a chunk behind the other, and
+// half of the SIMDs have nothing.  The work of 16 value channels goes to two
+// waves: one takes the state from chunk to chunk (K S^T, V', the new state), the
+// other, a part behind, makes the outputs and convolves the next chunk's values.
+// They pass the state, V' and the values as operands through LDS.  One more wave
+// does all loads.
+// ---------------------------------------------------------------------------
+template <typename TIn, int DKP, int NG>
+struct ScanPair {
+  typedef Scan<TIn, DKP, NG> Base;
+  static constexpr int kKs = DKP / 32, kThreads = (2 * NG + 1) * kWave;
+  static constexpr int kAtS = Base::kLds;                       // of a group: the state's operands [ks]
+  static constexpr int kAtX = kAtS + NG * kKs * 2 * kFrag;      // of a group: the values, then V' [2 steps]
+  static constexpr int kAtScale = kAtX + NG * 4 * kFrag;        // of a group: 1 / scale of the state, of V' [2][16]
+  static constexpr int kLds = kAtScale + NG * 128;
+};
+
+template <typename TIn, typename TOut, int DKP, int NG>
+__global__ __launch_bounds__((2 * NG + 1) * kWave) void scan_pair_kernel(ChainArgs a, Part part) {
+  typedef ScanPair<TIn, DKP, NG> S;
+  typedef typename S::Base B;
+  typedef Rows<S::kKs> R;
+  typedef RawRows<TIn, NG> Raw;
+  constexpr int kKs = S::kKs, kGroups = R::kGroups, kQFrags = B::kQ / kFrag, kWaves = 2 * NG + 1;
+  extern __shared__ __align__(16) char s_raw[];
+  const char *s_k = s_raw, *s_q = s_raw + B::kAtQ, *s_kt = s_raw + B::kAtKt, *s_t = s_raw + B::kAtT, *s_y = s_raw + B::kAtY,
+             *s_v = s_raw + B::kAtV;
+  const int tid = threadIdx.x, lane = tid % kWave, w = __builtin_amdgcn_readfirstlane(tid / kWave);
+  const int n16 = lane & 15, q4 = lane >> 4;
+  const int2 hs = head_of();
+  const int mine = w % NG, h = hs.x, b = part.b0 + blockIdx.z, hk = h / (a.Hv / a.Hk);
+  const Tokens tk = tokens_of(a, b);
+  const int dk = a.dk, dv = a.dv, end = min(part.c0 + part.M, (tk.n + kC - 1) / kC), count = end - part.c0;
+  if (count <= 0) return;
+  const size_t vstride = size_t(a.Hv) * dv;
+
+  if (w == 2 * NG) {  // loads
+    const LdsPtr lds = (LdsPtr)s_raw;
+    const SlotLayout l = slot_layout(a.Hk, a.Hv, dk);
+    const char* vws = value_at(a, slot_at(a, part, blockIdx.z, 0), h);
+    const char* kws = key_at(a, slot_at(a, part, blockIdx.z, 0), hk);
+    const char* values = reinterpret_cast<const char*>(reinterpret_cast<const TIn*>(a.v) + size_t(tk.first) * vstride + h * dv + hs.y * NG * 16);
+    const unsigned at = lane * 16;
+    auto copy = [&](const char* src, int to, int frags) {
+#pragma unroll 4
+      for (int u = 0; u < frags; ++u) to_lds(src + u * kFrag, at, lds + to + u * kFrag);
+    };
+    auto load_values = [&](int m) {
+#pragma unroll
+      for (int u = 0; u < Raw::kFrags; ++u) Raw::load(values, vstride * sizeof(TIn), tk.n, part.c0 + m, u, lane, lds + B::kAtV);
+    };
+    auto load_first = [&](int m) {  // K, (I + A)^-1, scalars, Q
+      const char *k = kws + size_t(m) * l.total, *v = vws + size_t(m) * l.total;
+      copy(k, 0, kQFrags);
+      to_lds(v + kScalarsAt, at, lds + B::kAtScalars + (m & 1) * kFrag);
+      copy(v, B::kAtT, 12);
+      copy(k + B::kQ, B::kAtQ, kQFrags);
+    };
+    load_values(0);
+    load_first(0);
+    arrive<kWaves>();
+    for (int m = 0; m < count; ++m) {
+      arrive<kWaves>();
+      copy(kws + size_t(m) * l.total + 2 * B::kQ, B::kAtKt, kQFrags);
+      copy(vws + size_t(m) * l.total + kYAt, B::kAtY, 12);
+      if (m + 1 < count) load_values(m + 1);
+      arrive<kWaves>();
+      if (m + 1 < count) load_first(m + 1);
+    }
+    return;
+  }
+
+  const int ch = (hs.y * NG + mine) * 16 + n16;  // value channel
+  char* s_s = s_raw + S::kAtS + mine * kKs * 2 * kFrag;
+  char* s_x = s_raw + S::kAtX + mine * 4 * kFrag;
+  float* s_scale = reinterpret_cast<float*>(s_raw + S::kAtScale + mine * 128) + n16;
+  if (w < NG) {  // the state
+    float* state = a.S + ((size_t(b) * a.Hv + h) * dv + ch) * dk + 4 * q4;
+    f32x4 st[DKP / 16];
+    float mx = 0.0f;
+#pragma unroll
+    for (int n = 0; n < DKP / 16; ++n) {
+      st[n] = 16 * n < dk ? *reinterpret_cast<const f32x4*>(state + 16 * n) : f32x4{};
+#pragma unroll
+      for (int r = 0; r < 4; ++r) mx = fmaxf(mx, fabsf(st[n][r]));
+    }
+    arrive<kWaves>();
+    for (int m = 0; m < count; ++m) {
+      const float* s_sc = reinterpret_cast<const float*>(s_raw + B::kAtScalars + (m & 1) * kFrag);
+      float ss, is;
+      f16_scale(column_max(mx), ss, is);
+      Pair sp[kKs];
+#pragma unroll
+      for (int s = 0; s < kKs; ++s) {
+        sp[s] = operand(st[2 * s], st[2 * s + 1], ss);
+        store_pair(s_s, s, lane, sp[s]);
+      }
+      s_scale[0] = is;
+      arrive<kWaves>();  // K, (I + A)^-1, scalars; values, the state
+      typename R::Group f[2];
+      f32x4 x[4] = {};
+      R::read(f[0], s_k, 0, lane);
+      Pair g[2][4];
+#pragma unroll
+      for (int n = 0; n < kGroups; ++n) {
+        if (n + 1 < kGroups) R::read(f[(n + 1) & 1], s_k, n + 1, lane);
+        __builtin_amdgcn_sched_barrier(0);
+        R::times(f[n & 1], sp, x, n);
+        __builtin_amdgcn_sched_barrier(0);
+      }
+      read_lower(g[0], s_t, 0, lane);
+      read_lower(g[1], s_t, 1, lane);
+      float mr = 0.0f, sr, ir;
+      const float ik = is * (1.0f / kUnit);
+#pragma unroll
+      for (int t = 0; t < 4; ++t) {  // beta (V - e^g K S^T)
+        const f32x4 be = *reinterpret_cast<const f32x4*>(s_sc + 16 * t + 4 * q4);
+        const f32x4 dec = *reinterpret_cast<const f32x4*>(s_sc + kC + 16 * t + 4 * q4);
+        const f32x4 v = *reinterpret_cast<const f32x4*>(s_x + t * kFrag + lane * 16);
+#pragma unroll
+        for (int r = 0; r < 4; ++r) {
+          x[t][r] = be[r] * (v[r] - dec[r] * (x[t][r] * ik));
+          mr = fmaxf(mr, fabsf(x[t][r]));
+        }
+      }
+      f16_scale(column_max(mr), sr, ir);
+      const Pair r0 = operand(x[0], x[1], sr), r1 = operand(x[2], x[3], sr);
+#pragma unroll
+      for (int t = 0; t < 4; ++t) x[t] = f32x4{};
+      times_lower(g[0], r0, x, 0);
+      times_lower(g[1], r1, x, 1);
+      float mv = 0.0f, md = 0.0f, sv, iv, sd, id;
+      const float it = s_sc[3 * kC + 1] * ir, last = s_sc[3 * kC];
+      f32x4 xd[4];
+#pragma unroll
+      for (int t = 0; t < 4; ++t) {
+        const f32x4 dec = *reinterpret_cast<const f32x4*>(s_sc + 2 * kC + 16 * t + 4 * q4);
+#pragma unroll
+        for (int r = 0; r < 4; ++r) {
+          x[t][r] *= it;
+          xd[t][r] = x[t][r] * dec[r];
+          mv = fmaxf(mv, fabsf(x[t][r]));
+          md = fmaxf(md, fabsf(xd[t][r]));
+        }
+      }
+      f16_scale(column_max(mv), sv, iv);
+      store_pair(s_x, 0, lane, operand(x[0], x[1], sv));  // in place of the values, which this wave has read
+      store_pair(s_x, 1, lane, operand(x[2], x[3], sv));
+      s_scale[16] = iv;
+      f16_scale(column_max(md), sd, id);
+      const Pair vd[2] = {operand(xd[0], xd[1], sd), operand(xd[2], xd[3], sd)};
+      id *= 1.0f / kUnit;
+      arrive<kWaves>();  // K^T; V'
+      read_kt(g[0], s_kt, 0, lane);
+      mx = 0.0f;
+#pragma unroll
+      for (int n = 0; n < DKP / 32; ++n) {
+        if (n + 1 < DKP / 32) read_kt(g[(n + 1) & 1], s_kt, n + 1, lane);
+        __builtin_amdgcn_sched_barrier(0);
+        f32x4 c[2] = {};
+        times_kt(g[n & 1], vd, c);
+#pragma unroll
+        for (int e = 0; e < 2; ++e)
+#pragma unroll
+          for (int r = 0; r < 4; ++r) {
+            st[2 * n + e][r] = last * st[2 * n + e][r] + c[e][r] * id;
+            mx = fmaxf(mx, fabsf(st[2 * n + e][r]));
+          }
+      }
+    }
+#pragma unroll
+    for (int n = 0; n < DKP / 16; ++n)
+      if (16 * n < dk) *reinterpret_cast<f32x4*>(state + 16 * n) = st[n];
+    return;
+  }
+
+  // the outputs
+  const size_t C = 2 * size_t(a.Hk) * dk + vstride, channel = 2 * size_t(a.Hk) * dk + h * dv + ch;
+  const float4 cw = *reinterpret_cast<const float4*>(a.conv_w + channel * 4);
+  float old[3];  // before the sequence's first token
+#pragma unroll
+  for (int i = 0; i < 3; ++i) old[i] = a.conv_state[(size_t(b) * 3 + i) * C + channel];
+  TOut* out = reinterpret_cast<TOut*>(a.out) + size_t(tk.first) * vstride + h * dv + ch;
+  auto values_of = [&](int m) {
+#pragma unroll
+    for (int t = 0; t < 4; ++t)
+      *reinterpret_cast<f32x4*>(s_x + t * kFrag + lane * 16) = convolve<TIn, NG>(s_v, t, mine, n16, q4, cw, old, part.c0 + m == 0);
+  };
+  arrive<kWaves>();
+  values_of(0);
+  f32x4 o[4];
+  for (int m = 0; m < count; ++m) {
+    const float* s_sc = reinterpret_cast<const float*>(s_raw + B::kAtScalars + (m & 1) * kFrag);
+    arrive<kWaves>();  // Q, scalars; the state
+    if (m) {
+      const int n0 = (part.c0 + m - 1) * kC;
+      store_chunk(out + size_t(n0) * vstride, vstride, tk.n - n0, q4, o);
+    }
+    Pair sp[kKs];
+#pragma unroll
+    for (int s = 0; s < kKs; ++s) sp[s] = load_pair(s_s, s, lane);
+    typename R::Group f[2];
+#pragma unroll
+    for (int t = 0; t < 4; ++t) o[t] = f32x4{};
+    R::read(f[0], s_q, 0, lane);
+#pragma unroll
+    for (int n = 0; n < kGroups; ++n) {
+      if (n + 1 < kGroups) R::read(f[(n + 1) & 1], s_q, n + 1, lane);
+      __builtin_amdgcn_sched_barrier(0);
+      R::times(f[n & 1], sp, o, n);
+      __builtin_amdgcn_sched_barrier(0);
+    }
+    const float io = s_scale[0] * (a.scale * (1.0f / kUnit));
+    arrive<kWaves>();  // Y, raw values; V'
+    const Pair v0 = load_pair(s_x, 0, lane), v1 = load_pair(s_x, 1, lane);
+    const float iv = s_scale[16] * (a.scale * (1.0f / kUnit));
+    Pair g[2][4];
+    read_lower(g[0], s_y, 0, lane);
+    read_lower(g[1], s_y, 1, lane);
+    f32x4 y[4] = {};
+    times_lower(g[0], v0, y, 0);
+    times_lower(g[1], v1, y, 1);
+#pragma unroll
+    for (int t = 0; t < 4; ++t) {
+      const f32x4 dec = *reinterpret_cast<const f32x4*>(s_sc + kC + 16 * t + 4 * q4);
+#pragma unroll
+      for (int r = 0; r < 4; ++r) o[t][r] = o[t][r] * dec[r] * io + y[t][r] * iv;
+    }
+    if (m + 1 < count) values_of(m + 1);  // V' is read
+  }
+  const int n0 = (end - 1) * kC;
+  store_chunk(out + size_t(n0) * vstride, vstride, tk.n - n0, q4, o);
 }
 
 // The conv state behind the last token, and the statuses.
@@ -847,16 +1116,27 @@ int launch_waves(const ChainArgs& a, const Part& p, hipStream_t stream) {
   return after_launch();
 }
 
+template <typename TIn, typename TOut, int DKP, int NG>
+int launch_pairs(const ChainArgs& a, const Part& p, hipStream_t stream) {
+  typedef ScanPair<TIn, DKP, NG> S;
+  const int rc = ensure_dynamic_lds(reinterpret_cast<const void*>(scan_pair_kernel<TIn, TOut, DKP, NG>), S::kLds, "chain");
+  if (rc != GDN_OK) return rc;
+  scan_pair_kernel<TIn, TOut, DKP, NG><<<dim3(a.dv / 16 / NG, a.Hv, p.G), S::kThreads, S::kLds, stream>>>(a, p);
+  return after_launch();
+}
+
 template <typename TIn, typename TOut, int DKP>
 int launch_scan(const ChainArgs& a, const Part& p, hipStream_t stream) {
-  // waves of a workgroup: as many as share a head, but a workgroup a CU
   const int groups = a.dv / 16;
+  const long long heads = (long long)(p.G) * a.Hv;
+  if (groups == 1 || heads * groups <= 256) return launch_pairs<TIn, TOut, DKP, 1>(a, p, stream);
+  if (heads * groups <= 512) return launch_pairs<TIn, TOut, DKP, 2>(a, p, stream);
+  // waves of a workgroup: as many as share a head, but a workgroup a CU
   int nw = groups;
-  while (nw > 1 && (long long)(p.G) * a.Hv * (groups / nw) < 192) nw /= 2;
+  while (nw > 2 && heads * (groups / nw) < 192) nw /= 2;
   if (nw >= 8) return launch_waves<TIn, TOut, DKP, 8>(a, p, stream);
   if (nw == 4) return launch_waves<TIn, TOut, DKP, 4>(a, p, stream);
-  if (nw == 2) return launch_waves<TIn, TOut, DKP, 2>(a, p, stream);
-  return launch_waves<TIn, TOut, DKP, 1>(a, p, stream);
+  return launch_waves<TIn, TOut, DKP, 2>(a, p, stream);
 }
 
 template <typename TIn, int DKP>
