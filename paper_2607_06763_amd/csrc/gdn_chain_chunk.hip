@@ -339,8 +339,13 @@ __global__ __launch_bounds__(kPrepThreads, 2) void chunk_kernel(ChainArgs a, Par
       const float f = __expf(float(g));
       sc[lane] = be;
       sc[kC + lane] = f;
-      sc[2 * kC + lane] = __expf(float(__shfl(g, kC - 1) - g));
-      if (lane == kC - 1) sc[3 * kC] = f;
+      const float to_end = __expf(float(__shfl(g, kC - 1) - g));
+      sc[2 * kC + lane] = to_end;
+      const float most = column_max(group_max<16>(to_end));
+      if (lane == kC - 1) {
+        sc[3 * kC] = f;
+        sc[3 * kC + 3] = most;
+      }
     }
     __syncthreads();
     // A, to be inverted, and Y
@@ -431,10 +436,13 @@ __global__ __launch_bounds__(kPrepThreads, 2) void chunk_kernel(ChainArgs a, Par
         most = fmaxf(most, fmaxf(fmaxf(fabsf(x10[r]), fabsf(x21[r])), fabsf(x32[r])));
         most = fmaxf(most, fmaxf(fmaxf(fabsf(x20[r]), fabsf(x31[r])), fabsf(x30[r])));
       }
-      f16_scale(column_max(group_max<16>(most)), scale, inv);
+      most = column_max(group_max<16>(most));
+      f16_scale(most, scale, inv);
       if (lane == 0) {
         s_scale[w] = scale;
-        reinterpret_cast<float*>(value_at(a, slot, hk * per + r0 + w) + kScalarsAt)[3 * kC + 1] = inv;
+        float* sc = reinterpret_cast<float*>(value_at(a, slot, hk * per + r0 + w) + kScalarsAt) + 3 * kC;
+        sc[1] = inv;
+        sc[2] = kC * most;  // at least the largest sum of a row
       }
     }
     __syncthreads();
@@ -523,6 +531,47 @@ __device__ __forceinline__ void times_kt(const Pair (&f)[4], const Pair (&vd)[2]
   }
 }
 
+// What a chunk's scalars give: the decay over it, 1 / scale of (I + A)^-1, a
+// bound of the sums of its rows, the largest decay to the chunk's end.
+struct ChunkScalars {
+  float last, inv, rows, most;
+};
+__device__ __forceinline__ ChunkScalars scalars_of(const float* s_sc) {
+  const float4 x = *reinterpret_cast<const float4*>(s_sc + 3 * kC);
+  return {x.x, x.y, x.z, x.w};
+}
+
+// V' as operands, plain and decayed to the chunk's end, and the scale of the
+// state behind the chunk.  Scales come from bounds, so that no value waits for
+// the largest of all: |V'| is at most a row's sum of (I + A)^-1 times mr, the
+// largest value of its operand (in a column), and the state at most `last` times
+// what it was plus 64 times that.  They are up to 2^6 and 2^12 too small, and
+// leave the pairs their 22 bits: hi is normal down to 2^-28 of the bound, lo
+// counts in steps of 2^-38 of it.
+struct Scales {
+  float v, iv, d, id, s, is;  // of V', of V' decayed, of the state; their inverses
+};
+__device__ __forceinline__ Scales scales_of(const ChunkScalars& c, float mr, float mx) {
+  Scales k;
+  const float v = c.rows * mr, d = v * c.most;
+  f16_scale(v, k.v, k.iv);
+  f16_scale(d, k.d, k.id);
+  f16_scale(fabsf(c.last) * mx + kC * d, k.s, k.is);
+  return k;
+}
+// x: accumulators of (I + A)^-1 times its operand, which has the scale 1 / ir
+__device__ __forceinline__ void value_operands(const f32x4 (&x)[4], const float* s_sc, int q4, const ChunkScalars& c, float ir,
+                                               const Scales& k, Pair (&vp)[2], Pair (&vd)[2]) {
+  const float fv = ir * k.v * c.inv, fd = ir * k.d * c.inv;
+#pragma unroll
+  for (int s = 0; s < 2; ++s) {
+    const f32x4 d0 = *reinterpret_cast<const f32x4*>(s_sc + 2 * kC + 32 * s + 4 * q4);
+    const f32x4 d1 = *reinterpret_cast<const f32x4*>(s_sc + 2 * kC + 32 * s + 16 + 4 * q4);
+    vp[s] = operand(x[2 * s], x[2 * s + 1], fv);
+    vd[s] = operand(x[2 * s] * d0, x[2 * s + 1] * d1, fd);
+  }
+}
+
 // This wave's loads and stores are done and its LDS reads; then the workgroup's.
 template <int NW>
 __device__ __forceinline__ void arrive() {
@@ -559,17 +608,17 @@ struct RawRows {
   }
 };
 
-// Convolved values of token tile t, rows 16 t + 4 q4 .. of channel n16; old:
-// those before the sequence, first: whether the chunk is its first.
+// Raw values that token tile t of channel n16 needs, rows 16 t + 4 q4 - 3 ..;
+// old: those before the sequence, first: whether the chunk is its first.
 template <typename TIn, int NG>
-__device__ __forceinline__ f32x4 convolve(const char* s_v, int t, int group, int n16, int q4, float4 cw, const float (&old)[3],
-                                          bool first) {
-  float x[7];
+__device__ __forceinline__ void window(float (&x)[7], const char* s_v, int t, int group, int n16, int q4, const float (&old)[3], bool first) {
 #pragma unroll
   for (int i = 0; i < 7; ++i) {
     x[i] = RawRows<TIn, NG>::get(s_v, 16 * t + 4 * q4 + i, group, n16);
     if (t == 0 && i < 3) x[i] = first && q4 == 0 ? old[i] : x[i];
   }
+}
+__device__ __forceinline__ f32x4 convolved(const float (&x)[7], float4 cw) {
   f32x4 v;
 #pragma unroll
   for (int r = 0; r < 4; ++r) v[r] = silu(cw.x * x[r] + cw.y * x[r + 1] + cw.z * x[r + 2] + cw.w * x[r + 3]);
@@ -699,7 +748,9 @@ __global__ __launch_bounds__(NW * kWave) void scan_kernel(ChainArgs a, Part part
     for (int r = 0; r < 4; ++r) mx = fmaxf(mx, fabsf(st[n][r]));
   f32x4 v[4];  // convolved values of a chunk
   auto values_of = [&](int m, int t) {
-    v[t] = convolve<TIn, NW>(s_v, t, w, n16, q4, cw, old, part.c0 + m == 0);
+    float x[7];
+    window<TIn, NW>(x, s_v, t, w, n16, q4, old, part.c0 + m == 0);
+    v[t] = convolved(x, cw);
     asm volatile("" : "+v"(v[t]));  // here, not at its use a chunk later
   };
   arrive<NW>();
@@ -707,14 +758,17 @@ __global__ __launch_bounds__(NW * kWave) void scan_kernel(ChainArgs a, Part part
   for (int t = 0; t < 4; ++t) values_of(0, t);
 
   f32x4 o[4];  // outputs of a chunk
+  float is;    // the state as operands
+  Pair sp[kKs];
+  {
+    float ss;
+    f16_scale(column_max(mx), ss, is);
+#pragma unroll
+    for (int s = 0; s < kKs; ++s) sp[s] = operand(st[2 * s], st[2 * s + 1], ss);
+  }
   for (int m = 0; m < end - part.c0; ++m) {
     const int next = min(m + 1, end - part.c0 - 1);  // the last chunk's again: they are not used
     const float* s_sc = reinterpret_cast<const float*>(s_raw + S::kAtScalars + (m & 1) * kFrag);
-    float ss, is;  // the state as an operand
-    f16_scale(column_max(mx), ss, is);
-    Pair sp[kKs];
-#pragma unroll
-    for (int s = 0; s < kKs; ++s) sp[s] = operand(st[2 * s], st[2 * s + 1], ss);
     arrive<NW>();  // K, Q, (I + A)^-1, scalars; the last chunk's Y and K^T, the raw values are read
     if (m) store(m - 1, o);  // here: the next wait is a part away
     load_second(m, next);
@@ -752,7 +806,8 @@ __global__ __launch_bounds__(NW * kWave) void scan_kernel(ChainArgs a, Part part
       }
       __builtin_amdgcn_sched_barrier(0);
     }
-    f16_scale(column_max(mr), sr, ir);
+    mr = column_max(mr);
+    f16_scale(mr, sr, ir);
     const Pair r0 = operand(x[0], x[1], sr), r1 = operand(x[2], x[3], sr);
     Pair g[2][4];
     read_lower(g[0], s_t, 0, lane);
@@ -763,32 +818,17 @@ __global__ __launch_bounds__(NW * kWave) void scan_kernel(ChainArgs a, Part part
     times_lower(g[0], r0, x, 0);
     times_lower(g[1], r1, x, 1);
     __builtin_amdgcn_sched_barrier(0);
-    // V', and decayed to the chunk's end, beside the others
-    float mv = 0.0f, md = 0.0f, sv, iv, sd, id;
-    const float it = s_sc[3 * kC + 1] * ir, last = s_sc[3 * kC];
-    f32x4 xd[4];
+    const ChunkScalars cs = scalars_of(s_sc);
+    const Scales sc = scales_of(cs, mr, column_max(mx));
+    Pair vp[2], vd[2];
 #pragma unroll
     for (int n = kGroups / 2; n < kGroups; ++n) {
       if (n + 1 < kGroups) R::read(f[(kGroups + n + 1) & 1], s_q, n + 1, lane);
       __builtin_amdgcn_sched_barrier(0);
       R::times(f[(kGroups + n) & 1], sp, o, n);
-#pragma unroll
-      for (int t = n * 8 / kGroups - 4; t < (n + 1) * 8 / kGroups - 4; ++t) {
-        const f32x4 dec = *reinterpret_cast<const f32x4*>(s_sc + 2 * kC + 16 * t + 4 * q4);
-#pragma unroll
-        for (int r = 0; r < 4; ++r) {
-          x[t][r] *= it;
-          xd[t][r] = x[t][r] * dec[r];
-          mv = fmaxf(mv, fabsf(x[t][r]));
-          md = fmaxf(md, fabsf(xd[t][r]));
-        }
-      }
+      if (n == kGroups / 2) value_operands(x, s_sc, q4, cs, ir, sc, vp, vd);  // V', beside the others
       __builtin_amdgcn_sched_barrier(0);
     }
-    f16_scale(column_max(mv), sv, iv);
-    f16_scale(column_max(md), sd, id);
-    const Pair vp[2] = {operand(x[0], x[1], sv), operand(x[2], x[3], sv)};
-    const Pair vd[2] = {operand(xd[0], xd[1], sd), operand(xd[2], xd[3], sd)};
     arrive<NW>();  // Y, K^T, raw values; K, Q and (I + A)^-1 are read
     load_first(next);
 
@@ -802,33 +842,38 @@ __global__ __launch_bounds__(NW * kWave) void scan_kernel(ChainArgs a, Part part
     read_kt(g[0], s_kt, 0, lane);
     __builtin_amdgcn_sched_barrier(0);
     times_lower(g[1], vp[1], y, 1);
-    iv *= a.scale * (1.0f / kUnit);
-    const float io = ik * a.scale;
-    id *= 1.0f / kUnit;
+    const float iv = sc.iv * (a.scale * (1.0f / kUnit)), io = ik * a.scale, id = sc.id * (1.0f / kUnit);
     mx = 0.0f;
+    f32x4 c[2][2];
+    auto state_of = [&](int n) {
 #pragma unroll
-    for (int n = 0; n < DKP / 32; ++n) {
-      if (n + 1 < DKP / 32) read_kt(g[(n + 1) & 1], s_kt, n + 1, lane);
+      for (int e = 0; e < 2; ++e)
+#pragma unroll
+        for (int r = 0; r < 4; ++r) {
+          st[2 * n + e][r] = cs.last * st[2 * n + e][r] + c[n & 1][e][r] * id;
+          mx = fmaxf(mx, fabsf(st[2 * n + e][r]));
+        }
+      sp[n] = operand(st[2 * n], st[2 * n + 1], sc.s);
+    };
+#pragma unroll
+    for (int n = 0; n < kKs; ++n) {
+      if (n + 1 < kKs) read_kt(g[(n + 1) & 1], s_kt, n + 1, lane);
       __builtin_amdgcn_sched_barrier(0);
-      f32x4 c[2] = {};
-      times_kt(g[n & 1], vd, c);
+      c[n & 1][0] = c[n & 1][1] = f32x4{};
+      times_kt(g[n & 1], vd, c[n & 1]);
+      if (n) state_of(n - 1);
       // a share of the outputs and of the next values beside these products
 #pragma unroll
-      for (int t = n * 4 / (DKP / 32); t < (n + 1) * 4 / (DKP / 32); ++t) {
+      for (int t = n * 4 / kKs; t < (n + 1) * 4 / kKs; ++t) {
         const f32x4 dec = *reinterpret_cast<const f32x4*>(s_sc + kC + 16 * t + 4 * q4);
 #pragma unroll
         for (int r = 0; r < 4; ++r) o[t][r] = o[t][r] * dec[r] * io + y[t][r] * iv;
         values_of(next, t);
       }
-#pragma unroll
-      for (int e = 0; e < 2; ++e)
-#pragma unroll
-        for (int r = 0; r < 4; ++r) {
-          st[2 * n + e][r] = last * st[2 * n + e][r] + c[e][r] * id;
-          mx = fmaxf(mx, fabsf(st[2 * n + e][r]));
-        }
       __builtin_amdgcn_sched_barrier(0);
     }
+    state_of(kKs - 1);
+    is = sc.is;
   }
   store(end - part.c0 - 1, o);
   asm volatile("s_waitcnt vmcnt(0)" ::: "memory");  // nothing arrives in LDS after the end
@@ -842,13 +887,15 @@ __global__ __launch_bounds__(NW * kWave) void scan_kernel(ChainArgs a, Part part
 // half of the SIMDs have nothing.  The work of 16 value channels goes to two
 // waves: one takes the state from chunk to chunk (K S^T, V', the new state), the
 // other, a part behind, makes the outputs and convolves the next chunk's values.
-// They pass the state, V' and the values as operands through LDS.  One more wave
-// does all loads.
+// They pass the state, V' and the values as operands through LDS.  Two more waves
+// do all loads (a wave has at most 64 on their way).
 // ---------------------------------------------------------------------------
+constexpr int kLoaders = 2;
+
 template <typename TIn, int DKP, int NG>
 struct ScanPair {
   typedef Scan<TIn, DKP, NG> Base;
-  static constexpr int kKs = DKP / 32, kThreads = (2 * NG + 1) * kWave;
+  static constexpr int kKs = DKP / 32, kThreads = (2 * NG + kLoaders) * kWave;
   static constexpr int kAtS = Base::kLds;                       // of a group: the state's operands [ks]
   static constexpr int kAtX = kAtS + NG * kKs * 2 * kFrag;      // of a group: the values, then V' [2 steps]
   static constexpr int kAtScale = kAtX + NG * 4 * kFrag;        // of a group: 1 / scale of the state, of V' [2][16]
@@ -856,12 +903,12 @@ struct ScanPair {
 };
 
 template <typename TIn, typename TOut, int DKP, int NG>
-__global__ __launch_bounds__((2 * NG + 1) * kWave) void scan_pair_kernel(ChainArgs a, Part part) {
+__global__ __launch_bounds__((2 * NG + kLoaders) * kWave) void scan_pair_kernel(ChainArgs a, Part part) {
   typedef ScanPair<TIn, DKP, NG> S;
   typedef typename S::Base B;
   typedef Rows<S::kKs> R;
   typedef RawRows<TIn, NG> Raw;
-  constexpr int kKs = S::kKs, kGroups = R::kGroups, kQFrags = B::kQ / kFrag, kWaves = 2 * NG + 1;
+  constexpr int kKs = S::kKs, kGroups = R::kGroups, kQFrags = B::kQ / kFrag, kWaves = 2 * NG + kLoaders;
   extern __shared__ __align__(16) char s_raw[];
   const char *s_k = s_raw, *s_q = s_raw + B::kAtQ, *s_kt = s_raw + B::kAtKt, *s_t = s_raw + B::kAtT, *s_y = s_raw + B::kAtY,
              *s_v = s_raw + B::kAtV;
@@ -874,7 +921,7 @@ __global__ __launch_bounds__((2 * NG + 1) * kWave) void scan_pair_kernel(ChainAr
   if (count <= 0) return;
   const size_t vstride = size_t(a.Hv) * dv;
 
-  if (w == 2 * NG) {  // loads
+  if (w >= 2 * NG) {  // loads, every other one of a list by each of the two waves
     const LdsPtr lds = (LdsPtr)s_raw;
     const SlotLayout l = slot_layout(a.Hk, a.Hv, dk);
     const char* vws = value_at(a, slot_at(a, part, blockIdx.z, 0), h);
@@ -883,16 +930,16 @@ __global__ __launch_bounds__((2 * NG + 1) * kWave) void scan_pair_kernel(ChainAr
     const unsigned at = lane * 16;
     auto copy = [&](const char* src, int to, int frags) {
 #pragma unroll 4
-      for (int u = 0; u < frags; ++u) to_lds(src + u * kFrag, at, lds + to + u * kFrag);
+      for (int u = w - 2 * NG; u < frags; u += kLoaders) to_lds(src + u * kFrag, at, lds + to + u * kFrag);
     };
     auto load_values = [&](int m) {
-#pragma unroll
-      for (int u = 0; u < Raw::kFrags; ++u) Raw::load(values, vstride * sizeof(TIn), tk.n, part.c0 + m, u, lane, lds + B::kAtV);
+      for (int u = w - 2 * NG; u < Raw::kFrags; u += kLoaders)
+        Raw::load(values, vstride * sizeof(TIn), tk.n, part.c0 + m, u, lane, lds + B::kAtV);
     };
     auto load_first = [&](int m) {  // K, (I + A)^-1, scalars, Q
       const char *k = kws + size_t(m) * l.total, *v = vws + size_t(m) * l.total;
       copy(k, 0, kQFrags);
-      to_lds(v + kScalarsAt, at, lds + B::kAtScalars + (m & 1) * kFrag);
+      copy(v + kScalarsAt, B::kAtScalars + (m & 1) * kFrag, 1);
       copy(v, B::kAtT, 12);
       copy(k + B::kQ, B::kAtQ, kQFrags);
     };
@@ -924,17 +971,20 @@ __global__ __launch_bounds__((2 * NG + 1) * kWave) void scan_pair_kernel(ChainAr
 #pragma unroll
       for (int r = 0; r < 4; ++r) mx = fmaxf(mx, fabsf(st[n][r]));
     }
-    arrive<kWaves>();
-    for (int m = 0; m < count; ++m) {
-      const float* s_sc = reinterpret_cast<const float*>(s_raw + B::kAtScalars + (m & 1) * kFrag);
-      float ss, is;
+    float is;
+    Pair sp[kKs];
+    {
+      float ss;
       f16_scale(column_max(mx), ss, is);
-      Pair sp[kKs];
 #pragma unroll
       for (int s = 0; s < kKs; ++s) {
         sp[s] = operand(st[2 * s], st[2 * s + 1], ss);
         store_pair(s_s, s, lane, sp[s]);
       }
+    }
+    arrive<kWaves>();
+    for (int m = 0; m < count; ++m) {
+      const float* s_sc = reinterpret_cast<const float*>(s_raw + B::kAtScalars + (m & 1) * kFrag);
       s_scale[0] = is;
       arrive<kWaves>();  // K, (I + A)^-1, scalars; values, the state
       typename R::Group f[2];
@@ -963,50 +1013,47 @@ __global__ __launch_bounds__((2 * NG + 1) * kWave) void scan_pair_kernel(ChainAr
           mr = fmaxf(mr, fabsf(x[t][r]));
         }
       }
-      f16_scale(column_max(mr), sr, ir);
+      mr = column_max(mr);
+      f16_scale(mr, sr, ir);
       const Pair r0 = operand(x[0], x[1], sr), r1 = operand(x[2], x[3], sr);
 #pragma unroll
       for (int t = 0; t < 4; ++t) x[t] = f32x4{};
       times_lower(g[0], r0, x, 0);
       times_lower(g[1], r1, x, 1);
-      float mv = 0.0f, md = 0.0f, sv, iv, sd, id;
-      const float it = s_sc[3 * kC + 1] * ir, last = s_sc[3 * kC];
-      f32x4 xd[4];
-#pragma unroll
-      for (int t = 0; t < 4; ++t) {
-        const f32x4 dec = *reinterpret_cast<const f32x4*>(s_sc + 2 * kC + 16 * t + 4 * q4);
-#pragma unroll
-        for (int r = 0; r < 4; ++r) {
-          x[t][r] *= it;
-          xd[t][r] = x[t][r] * dec[r];
-          mv = fmaxf(mv, fabsf(x[t][r]));
-          md = fmaxf(md, fabsf(xd[t][r]));
-        }
-      }
-      f16_scale(column_max(mv), sv, iv);
-      store_pair(s_x, 0, lane, operand(x[0], x[1], sv));  // in place of the values, which this wave has read
-      store_pair(s_x, 1, lane, operand(x[2], x[3], sv));
-      s_scale[16] = iv;
-      f16_scale(column_max(md), sd, id);
-      const Pair vd[2] = {operand(xd[0], xd[1], sd), operand(xd[2], xd[3], sd)};
-      id *= 1.0f / kUnit;
+      const ChunkScalars cs = scalars_of(s_sc);
+      const Scales sc = scales_of(cs, mr, column_max(mx));
+      Pair vp[2], vd[2];
+      value_operands(x, s_sc, q4, cs, ir, sc, vp, vd);
+      store_pair(s_x, 0, lane, vp[0]);  // in place of the values, which this wave has read
+      store_pair(s_x, 1, lane, vp[1]);
+      s_scale[16] = sc.iv;
+      const float id = sc.id * (1.0f / kUnit);
       arrive<kWaves>();  // K^T; V'
       read_kt(g[0], s_kt, 0, lane);
       mx = 0.0f;
-#pragma unroll
-      for (int n = 0; n < DKP / 32; ++n) {
-        if (n + 1 < DKP / 32) read_kt(g[(n + 1) & 1], s_kt, n + 1, lane);
-        __builtin_amdgcn_sched_barrier(0);
-        f32x4 c[2] = {};
-        times_kt(g[n & 1], vd, c);
+      f32x4 c[2][2];
+      auto state_of = [&](int n) {
 #pragma unroll
         for (int e = 0; e < 2; ++e)
 #pragma unroll
           for (int r = 0; r < 4; ++r) {
-            st[2 * n + e][r] = last * st[2 * n + e][r] + c[e][r] * id;
+            st[2 * n + e][r] = cs.last * st[2 * n + e][r] + c[n & 1][e][r] * id;
             mx = fmaxf(mx, fabsf(st[2 * n + e][r]));
           }
+        sp[n] = operand(st[2 * n], st[2 * n + 1], sc.s);
+        store_pair(s_s, n, lane, sp[n]);
+      };
+#pragma unroll
+      for (int n = 0; n < kKs; ++n) {
+        if (n + 1 < kKs) read_kt(g[(n + 1) & 1], s_kt, n + 1, lane);
+        __builtin_amdgcn_sched_barrier(0);
+        c[n & 1][0] = c[n & 1][1] = f32x4{};
+        times_kt(g[n & 1], vd, c[n & 1]);
+        if (n) state_of(n - 1);
+        __builtin_amdgcn_sched_barrier(0);
       }
+      state_of(kKs - 1);
+      is = sc.is;
     }
 #pragma unroll
     for (int n = 0; n < DKP / 16; ++n)
@@ -1021,13 +1068,18 @@ __global__ __launch_bounds__((2 * NG + 1) * kWave) void scan_pair_kernel(ChainAr
 #pragma unroll
   for (int i = 0; i < 3; ++i) old[i] = a.conv_state[(size_t(b) * 3 + i) * C + channel];
   TOut* out = reinterpret_cast<TOut*>(a.out) + size_t(tk.first) * vstride + h * dv + ch;
-  auto values_of = [&](int m) {
+  float x[4][7];
+  auto windows = [&](int m) {
 #pragma unroll
-    for (int t = 0; t < 4; ++t)
-      *reinterpret_cast<f32x4*>(s_x + t * kFrag + lane * 16) = convolve<TIn, NG>(s_v, t, mine, n16, q4, cw, old, part.c0 + m == 0);
+    for (int t = 0; t < 4; ++t) window<TIn, NG>(x[t], s_v, t, mine, n16, q4, old, part.c0 + m == 0);
+  };
+  auto pass_values = [&]() {
+#pragma unroll
+    for (int t = 0; t < 4; ++t) *reinterpret_cast<f32x4*>(s_x + t * kFrag + lane * 16) = convolved(x[t], cw);
   };
   arrive<kWaves>();
-  values_of(0);
+  windows(0);
+  pass_values();
   f32x4 o[4];
   for (int m = 0; m < count; ++m) {
     const float* s_sc = reinterpret_cast<const float*>(s_raw + B::kAtScalars + (m & 1) * kFrag);
@@ -1057,6 +1109,7 @@ __global__ __launch_bounds__((2 * NG + 1) * kWave) void scan_pair_kernel(ChainAr
     Pair g[2][4];
     read_lower(g[0], s_y, 0, lane);
     read_lower(g[1], s_y, 1, lane);
+    windows(m + 1);  // behind the last chunk: not used
     f32x4 y[4] = {};
     times_lower(g[0], v0, y, 0);
     times_lower(g[1], v1, y, 1);
@@ -1066,7 +1119,7 @@ __global__ __launch_bounds__((2 * NG + 1) * kWave) void scan_pair_kernel(ChainAr
 #pragma unroll
       for (int r = 0; r < 4; ++r) o[t][r] = o[t][r] * dec[r] * io + y[t][r] * iv;
     }
-    if (m + 1 < count) values_of(m + 1);  // V' is read
+    pass_values();  // V' is read
   }
   const int n0 = (end - 1) * kC;
   store_chunk(out + size_t(n0) * vstride, vstride, tk.n - n0, q4, o);
