@@ -899,7 +899,8 @@ struct ScanPair {
   static constexpr int kAtS = Base::kLds;                       // of a group: the state's operands [ks]
   static constexpr int kAtX = kAtS + NG * kKs * 2 * kFrag;      // of a group: the values, then V' [2 steps]
   static constexpr int kAtScale = kAtX + NG * 4 * kFrag;        // of a group: 1 / scale of the state, of V' [2][16]
-  static constexpr int kLds = kAtScale + NG * 128;
+  static constexpr int kAtScrap = kAtScale + NG * 128;
+  static constexpr int kLds = kAtScrap + 256;
 };
 
 template <typename TIn, typename TOut, int DKP, int NG>
@@ -936,22 +937,38 @@ __global__ __launch_bounds__((2 * NG + kLoaders) * kWave) void scan_pair_kernel(
       for (int u = w - 2 * NG; u < Raw::kFrags; u += kLoaders)
         Raw::load(values, vstride * sizeof(TIn), tk.n, part.c0 + m, u, lane, lds + B::kAtV);
     };
-    auto load_first = [&](int m) {  // K, (I + A)^-1, scalars, Q
-      const char *k = kws + size_t(m) * l.total, *v = vws + size_t(m) * l.total;
-      copy(k, 0, kQFrags);
+    auto load_first = [&](int m) {  // K, (I + A)^-1, scalars
+      const char* v = vws + size_t(m) * l.total;
+      copy(kws + size_t(m) * l.total, 0, kQFrags);
       copy(v + kScalarsAt, B::kAtScalars + (m & 1) * kFrag, 1);
       copy(v, B::kAtT, 12);
-      copy(k + B::kQ, B::kAtQ, kQFrags);
+    };
+    // Lines of a chunk into L2, a chunk ahead of the loads, a lane a line: those of
+    // a key head by its workgroups in turn
+    const int per = a.Hv / a.Hk, turns = per * gridDim.x, turn = h % per * gridDim.x + hs.y;
+    auto touch = [&](const char* p) {
+      __builtin_amdgcn_global_load_lds((const __attribute__((address_space(1))) void*)(p),
+                                       (__attribute__((address_space(3))) void*)(lds + S::kAtScrap), 4, 0, 0);
+    };
+    auto ahead = [&](int m) {
+      if (w != 2 * NG || m >= count) return;
+      for (int u = turn; u < 3 * B::kQ / 8192; u += turns) touch(kws + size_t(m) * l.total + u * 8192 + lane * 128);
+      for (int u = hs.y; u < 4; u += gridDim.x) touch(vws + size_t(m) * l.total + min(u * 8192 + lane * 128, int(kValue) - 128));
+      const int i = min((part.c0 + m + 1) * kC + lane, tk.n - 1);
+      touch(values + size_t(i) * vstride * sizeof(TIn));
     };
     load_values(0);
+    arrive<kWaves>();
     load_first(0);
     arrive<kWaves>();
+    load_values(min(1, count - 1));
     for (int m = 0; m < count; ++m) {
       arrive<kWaves>();
-      copy(kws + size_t(m) * l.total + 2 * B::kQ, B::kAtKt, kQFrags);
+      ahead(m + 1);
+      copy(kws + size_t(m) * l.total + B::kQ, B::kAtQ, 2 * kQFrags);  // and K^T
       copy(vws + size_t(m) * l.total + kYAt, B::kAtY, 12);
-      if (m + 1 < count) load_values(m + 1);
       arrive<kWaves>();
+      if (m + 2 < count) load_values(m + 2);
       if (m + 1 < count) load_first(m + 1);
     }
     return;
@@ -982,6 +999,7 @@ __global__ __launch_bounds__((2 * NG + kLoaders) * kWave) void scan_pair_kernel(
         store_pair(s_s, s, lane, sp[s]);
       }
     }
+    arrive<kWaves>();
     arrive<kWaves>();
     for (int m = 0; m < count; ++m) {
       const float* s_sc = reinterpret_cast<const float*>(s_raw + B::kAtScalars + (m & 1) * kFrag);
@@ -1068,22 +1086,29 @@ __global__ __launch_bounds__((2 * NG + kLoaders) * kWave) void scan_pair_kernel(
 #pragma unroll
   for (int i = 0; i < 3; ++i) old[i] = a.conv_state[(size_t(b) * 3 + i) * C + channel];
   TOut* out = reinterpret_cast<TOut*>(a.out) + size_t(tk.first) * vstride + h * dv + ch;
-  float x[4][7];
-  auto windows = [&](int m) {
+  f32x4 v[4];
+  auto values_of = [&](int m) {
+    float x[4][7];
 #pragma unroll
     for (int t = 0; t < 4; ++t) window<TIn, NG>(x[t], s_v, t, mine, n16, q4, old, part.c0 + m == 0);
+#pragma unroll
+    for (int t = 0; t < 4; ++t) {
+      v[t] = convolved(x[t], cw);
+      asm volatile("" : "+v"(v[t]));  // here, not at its use a part later
+    }
   };
   auto pass_values = [&]() {
 #pragma unroll
-    for (int t = 0; t < 4; ++t) *reinterpret_cast<f32x4*>(s_x + t * kFrag + lane * 16) = convolved(x[t], cw);
+    for (int t = 0; t < 4; ++t) *reinterpret_cast<f32x4*>(s_x + t * kFrag + lane * 16) = v[t];
   };
-  arrive<kWaves>();
-  windows(0);
+  arrive<kWaves>();  // raw values
+  values_of(0);
   pass_values();
+  arrive<kWaves>();
   f32x4 o[4];
   for (int m = 0; m < count; ++m) {
     const float* s_sc = reinterpret_cast<const float*>(s_raw + B::kAtScalars + (m & 1) * kFrag);
-    arrive<kWaves>();  // Q, scalars; the state
+    arrive<kWaves>();  // raw values of the next chunk; the state
     if (m) {
       const int n0 = (part.c0 + m - 1) * kC;
       store_chunk(out + size_t(n0) * vstride, vstride, tk.n - n0, q4, o);
@@ -1091,25 +1116,26 @@ __global__ __launch_bounds__((2 * NG + kLoaders) * kWave) void scan_pair_kernel(
     Pair sp[kKs];
 #pragma unroll
     for (int s = 0; s < kKs; ++s) sp[s] = load_pair(s_s, s, lane);
+    const float io = s_scale[0] * (a.scale * (1.0f / kUnit));
+    values_of(m + 1);  // behind the last chunk: not used
+    arrive<kWaves>();  // Q, Y; V'
+    const Pair v0 = load_pair(s_x, 0, lane), v1 = load_pair(s_x, 1, lane);
+    const float iv = s_scale[16] * (a.scale * (1.0f / kUnit));
     typename R::Group f[2];
+    Pair g[2][4];
 #pragma unroll
     for (int t = 0; t < 4; ++t) o[t] = f32x4{};
     R::read(f[0], s_q, 0, lane);
 #pragma unroll
     for (int n = 0; n < kGroups; ++n) {
       if (n + 1 < kGroups) R::read(f[(n + 1) & 1], s_q, n + 1, lane);
+      else read_lower(g[0], s_y, 0, lane);
       __builtin_amdgcn_sched_barrier(0);
       R::times(f[n & 1], sp, o, n);
+      if (n == 0) pass_values();  // V' is read
       __builtin_amdgcn_sched_barrier(0);
     }
-    const float io = s_scale[0] * (a.scale * (1.0f / kUnit));
-    arrive<kWaves>();  // Y, raw values; V'
-    const Pair v0 = load_pair(s_x, 0, lane), v1 = load_pair(s_x, 1, lane);
-    const float iv = s_scale[16] * (a.scale * (1.0f / kUnit));
-    Pair g[2][4];
-    read_lower(g[0], s_y, 0, lane);
     read_lower(g[1], s_y, 1, lane);
-    windows(m + 1);  // behind the last chunk: not used
     f32x4 y[4] = {};
     times_lower(g[0], v0, y, 0);
     times_lower(g[1], v1, y, 1);
@@ -1119,7 +1145,6 @@ __global__ __launch_bounds__((2 * NG + kLoaders) * kWave) void scan_pair_kernel(
 #pragma unroll
       for (int r = 0; r < 4; ++r) o[t][r] = o[t][r] * dec[r] * io + y[t][r] * iv;
     }
-    pass_values();  // V' is read
   }
   const int n0 = (end - 1) * kC;
   store_chunk(out + size_t(n0) * vstride, vstride, tk.n - n0, q4, o);
