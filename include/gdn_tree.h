@@ -466,15 +466,17 @@ typedef struct {
  *              length is negative or above T, or whose rows are outside
  *              [0, rows); 0 otherwise
  * A sequence without tokens, or with a non-zero status, keeps S and gets
- * conv_state_out = conv_state.  A decay below the smallest normal float counts
- * as that in the chunked form.
+ * conv_state_out = conv_state.  No tensor may overlap S or conv_state_out.  A
+ * decay below the smallest normal float counts as that in the chunked form.
+ * Inputs have to be finite: an infinity or NaN may reach every token of its
+ * chunk, those before it too.
  * Short sequences (T <= GDN_CHAIN_STEP_T) go token by token with the state in
  * registers and need no workspace.  Longer ones go in chunks of 64 tokens, all
  * products in 32 bits (fp16 pairs, three products, fp32 sums), through a
  * workspace that the library keeps (see Workspaces above), at most
  * GDN_CHAIN_WORKSPACE bytes or what one chunk of one sequence needs:
  * a chunk takes 768 Hk dk + 25600 Hv bytes (dk of 16 as 32). */
-#define GDN_CHAIN_STEP_T 16
+#define GDN_CHAIN_STEP_T 20
 #define GDN_CHAIN_WORKSPACE (1u << 28)
 int gdn_chain(const gdn_chain_dims* dims, const int32_t* start, const int32_t* n_new, const void* q,
               const void* k, const void* v, const void* alpha, const void* beta,

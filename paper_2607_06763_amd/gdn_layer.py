@@ -7,7 +7,7 @@ A GDN layer over prompts or single tokens, and the residual stream around it::
     L.gate_norm(o, gate, y, weight=w)                    # then the output projection
     L.add_norm(p, residual, residual, x, weight=w2)      # the next block's input
 
-``chain`` of more than 16 tokens a sequence works in a buffer that the library
+``chain`` of more than 20 tokens a sequence works in a buffer that the library
 keeps per stream (the header's "Workspaces"): before a capture the same sizes
 run once uncaptured on the capture stream, and a graph must not run at the same
 time as other such calls of that stream, or as another graph captured there.
@@ -20,7 +20,7 @@ from .gdn_tree import GDN_BF16, GDN_F32, _check, _ptrs, _stream, lib
 
 ACTS = {"silu": 0, "sigmoid": 1}
 MAX_CHAIN_T = 1 << 24  # GDN_MAX_CHAIN_T of gdn_tree.h
-STEP_T = 16  # GDN_CHAIN_STEP_T
+STEP_T = 20  # GDN_CHAIN_STEP_T
 MAX_NORM_D = 16384  # GDN_MAX_NORM_D
 
 

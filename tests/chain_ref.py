@@ -71,7 +71,7 @@ class Chain:
         Hk, Hv, dk, dv = self.Hk, self.Hv, self.dk, self.dv
         scale = dk ** -0.5 if scale is None else scale
         f = lambda t: t.double().numpy()
-        raw = np.concatenate([f(x).reshape(self.rows, -1) for x in (self.q, self.k, self.v)], 1)
+        raw = np.concatenate([f(x).reshape(self.rows, x.shape[1] * x.shape[2]) for x in (self.q, self.k, self.v)], 1)
         al, be = f(self.alpha), f(self.beta)
         cw = self.conv_w.astype(np.float64)
         out = np.zeros((self.rows, Hv, dv))
