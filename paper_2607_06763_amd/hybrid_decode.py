@@ -12,16 +12,21 @@ an output projection; the projections are plain matrix products.  A step of
     sample, accept                              a token per node, the walk along them
     per attention layer:  kv_commit             the accepted path's rows to the front
 
-``Decoder.prompt`` takes the prompts as chunks of a chain: verify and commit
-of the GDN layers, append and attend (without metadata, a length a sequence)
-of the attention layers.
+``Decoder.prompt`` takes the prompts in pieces: verify and commit of the GDN
+layers, or with ``prompt_form="chain"`` one call of the chain form, which has no
+tree to prepare; append and attend (without metadata, a length a sequence) of
+the attention layers.
+
+A ``HybridModel`` with ``gated`` has a weighted norm and a gate on every GDN
+head's output, and weighted norms before and after every block: ``gate_norm``,
+and ``add_norm`` from one block to the next.
 
 The random number of a position is fixed beforehand (``u`` [B][positions]),
 so the tokens do not depend on the draft trees: a node's token is the sample
 of the model given its context, and the tree only decides how many of them a
 step emits.
 
-    python -m paper_2607_06763_amd.hybrid_decode [--batch 4] [--slots 32] [--tokens 64]
+    python -m paper_2607_06763_amd.hybrid_decode [--batch 4] [--slots 32] [--tokens 64] [--gated] [--prompt-form chain]
 """
 from __future__ import annotations
 
@@ -42,7 +47,7 @@ class HybridModel:
 
     def __init__(self, vocab: int = 64, width: int = 64, layers: Sequence[str] = ("gdn", "attn", "gdn", "attn"),
                  Hk: int = 2, Hv: int = 4, dk: int = 64, dv: int = 64, Hq: int = 4, Hkv: int = 2, d: int = 64,
-                 rot: int = 32, positions: int = 1024, sharpness: float = 3.0, seed: int = 0):
+                 rot: int = 32, positions: int = 1024, sharpness: float = 3.0, seed: int = 0, gated: bool = False):
         rng = np.random.default_rng([seed, 15485863])
         self.V, self.width, self.positions = vocab, width, positions
         self.Hk, self.Hv, self.dk, self.dv = Hk, Hv, dk, dv
@@ -68,6 +73,14 @@ class HybridModel:
                 raise ValueError(f"layer kind {kind!r}, expected 'gdn' or 'attn'")
         angle = np.arange(positions)[:, None] * 10000.0 ** (-np.arange(rot // 2) / max(1, rot // 2))
         self.rope = np.stack([np.cos(angle), np.sin(angle)], axis=-1).astype(np.float32)
+        self.gated = gated
+        if gated:  # behind all others, so that these are the same with and without
+            near_one = lambda n: (1.0 + 0.2 * rng.standard_normal(n)).astype(np.float32)
+            for kind, l in zip(layers, self.layers):
+                l.update(norm=near_one(width), post=near_one(width), scale=(0.5 * near_one(width)).astype(np.float32))
+                if kind == "gdn":
+                    l.update(z=mat(Hv * dv, width), head=near_one(dv))
+            self.final = near_one(width)
 
         # the drafter: the next token from the last one's embedding alone
         z = self.embed / np.sqrt(np.mean(self.embed ** 2, axis=1, keepdims=True) + EPS) @ self.unembed.T
@@ -85,17 +98,22 @@ class Decoder:
     number of each position, for sequences of up to n tokens."""
 
     def __init__(self, model: HybridModel, B: int, T: int, u: np.ndarray, max_pages: int = 32, page: int = 16,
-                 dtype: str = "f32", temperature=None, top_k=None, top_p=None, min_p=None, device="cuda"):
+                 dtype: str = "f32", temperature=None, top_k=None, top_p=None, min_p=None, device="cuda",
+                 prompt_form: str = "tree"):
         import torch
         from . import gdn_attn as A
+        from . import gdn_layer as L
         from . import gdn_tree as G
-        self.A, self.G, self.torch = A, G, torch
+        if prompt_form not in ("tree", "chain"):
+            raise ValueError(f"prompt_form: {prompt_form!r}, expected 'tree' or 'chain'")
+        self.A, self.G, self.L, self.torch, self.prompt_form = A, G, L, torch, prompt_form
         self.m, self.B, self.T, self.dtype, self.device = model, B, T, dtype, device
         self.max_pages, self.page = max_pages, page
         self.dt = torch.bfloat16 if dtype == "bf16" else torch.float32
         up = lambda a, t=None: torch.as_tensor(np.ascontiguousarray(a), dtype=t).to(device)
         self.embed, self.unembed, self.rope = up(model.embed), up(model.unembed).t().contiguous(), up(model.rope)
-        self.w = [{n: up(a) if n == "conv_w" else up(a).t().contiguous() for n, a in l.items()} for l in model.layers]
+        self.w = [{n: up(a) if n == "conv_w" or a.ndim == 1 else up(a).t().contiguous() for n, a in l.items()} for l in model.layers]
+        self.final = up(model.final) if model.gated else None
         row = lambda x, t: None if x is None else up(np.broadcast_to(x, (B,)), t)
         self.sampling = dict(temperature=row(temperature, torch.float32), top_k=row(top_k, torch.int32),
                              top_p=row(top_p, torch.float32), min_p=row(min_p, torch.float32))
@@ -126,25 +144,35 @@ class Decoder:
     def _norm(self, x):
         return x * self.torch.rsqrt((x * x).mean(-1, keepdim=True) + EPS)
 
+    def _next(self, i):
+        """The weight of the norm before layer i (the last norm's behind the layers)."""
+        return self.w[i]["norm"] if i < len(self.w) else self.final
+
     def _unit(self, x):
         return x / x.norm(dim=-1, keepdim=True).clamp_min(EPS)
 
     def _layers(self, tok, meta, n_new, gdn):
-        """Hidden vectors after the layers; gdn(i, inputs) gives the output of GDN layer i, n_new the lengths of chains
-        (None: trees).  Returns them and the inputs of the GDN layers."""
+        """Normed hidden vectors after the layers; gdn(i, inputs) gives the output of GDN layer i, n_new the lengths of
+        chains (None: trees).  Returns them and the inputs of the GDN layers."""
         torch, m, (B, T) = self.torch, self.m, tok.shape
-        x = self.embed[tok.long()]
+        x = self.embed[tok.long()].reshape(B * T, -1)
         F = torch.nn.functional
         inputs, status = {}, []
         da = self._attn(T)
+        if m.gated:
+            h = torch.empty_like(x)
+            self.L.add_norm(x, None, None, h, weight=self._next(0), eps=EPS)
         for i, (kind, w) in enumerate(zip(m.kinds, self.w)):
-            y = self._norm(x)
+            y = (h if m.gated else self._norm(x)).view(B, T, -1)
             if kind == "gdn":
                 a = dict(q=self._unit((y @ w["q"]).view(B, T, m.Hk, m.dk)), k=self._unit((y @ w["k"]).view(B, T, m.Hk, m.dk)),
                          v=(y @ w["v"]).view(B, T, m.Hv, m.dv), alpha=torch.exp(-F.softplus(y @ w["alpha"])),
                          beta=torch.sigmoid(y @ w["beta"]))
                 inputs[i] = {n: t.to(self.dt).contiguous() for n, t in a.items()}
                 out = gdn(i, inputs[i])
+                if m.gated:
+                    heads = out.view(B * T, m.Hv, m.dv)
+                    self.L.gate_norm(heads, (y @ w["z"]).view(B * T, m.Hv, m.dv), heads, weight=w["head"], eps=EPS)
             else:
                 s = self.state[i]
                 q, k, v = ((y @ w[n]).view(B, T, -1, m.d).to(self.dt) for n in "qkv")
@@ -155,8 +183,12 @@ class Decoder:
                 out = torch.empty_like(q)
                 self.A.attend(da, q, s["k"], s["v"], self.table, self.ctx_len, out, **tree)
                 status.append(st)
-            x = x + out.float().reshape(B, T, -1) @ w["o"]
-        return x, inputs, status
+            block = out.float().reshape(B * T, -1) @ w["o"]
+            if m.gated:
+                self.L.add_norm(block, x, x, h, weight=self._next(i + 1), post_weight=w["post"], scale=w["scale"], post=True, eps=EPS)
+            else:
+                x = x + block
+        return (h if m.gated else self._norm(x)).view(B, T, -1), inputs, status
 
     def _check(self, statuses, what):
         worst = self.torch.stack(statuses).amax(0).tolist() if statuses else []
@@ -178,12 +210,23 @@ class Decoder:
                 tok[b, :n[b]] = p[at:at + n[b]]
                 parent[b, :n[b]] = np.arange(n[b]) - 1
             d = self._gdn(T)
-            meta = torch.empty(G.meta_bytes(B, T), dtype=torch.uint8, device=self.device)
             lengths, accepted = torch.from_numpy(n).to(self.device), torch.from_numpy(n - 1).to(self.device)
-            G.prepare(d, torch.from_numpy(parent).to(self.device), meta)
+            if self.prompt_form == "tree":
+                meta = torch.empty(G.meta_bytes(B, T), dtype=torch.uint8, device=self.device)
+                G.prepare(d, torch.from_numpy(parent).to(self.device), meta)
+            else:
+                meta, dc = None, self.L.make_chain_dims(B, T, m.Hk, m.Hv, m.dk, m.dv, in_dtype=self.dtype)
 
             def gdn(i, a):
                 s = self.state[i]
+                if meta is None:
+                    out = torch.zeros(B, T, m.Hv, m.dv, device=self.device)  # rows without a token are not written
+                    conv, st = torch.empty_like(s["conv"]), torch.empty(B, dtype=torch.int32, device=self.device)
+                    self.L.chain(dc, **a, conv_w=self.w[i]["conv_w"], conv_state=s["conv"], conv_state_out=conv, S=s["S"], out=out,
+                                 n_new=lengths, status=st)
+                    s["conv"] = conv
+                    statuses.append(st)
+                    return out
                 out = torch.empty(B, T, m.Hv, m.dv, device=self.device)
                 G.verify(d, meta, **a, conv_w=self.w[i]["conv_w"], conv_state=s["conv"], S0=s["S"], out=out)
                 st = torch.empty(B, dtype=torch.int32, device=self.device)
@@ -229,7 +272,7 @@ class Decoder:
             return out
 
         x, inputs, st = self._layers(draft, meta, None, gdn)
-        logits = self._norm(x) @ self.unembed
+        logits = x @ self.unembed
         # the number of the position after a node's (that of an absent slot is not used)
         u = torch.gather(self.u, 1, (self.ctx_len.long()[:, None] + dev(depth) + 1).clamp_max(self.u.shape[1] - 1))
         token, accepted, n_emitted, emitted = new(B, T), new(B), new(B), new(B, T)
@@ -279,14 +322,17 @@ def main(argv=None) -> None:
     ap.add_argument("--top-p", type=float, default=1.0)
     ap.add_argument("--min-p", type=float, default=0.0)
     ap.add_argument("--seed", type=int, default=0)
+    ap.add_argument("--gated", action="store_true", help="norms and gates around the blocks")
+    ap.add_argument("--prompt-form", choices=("tree", "chain"), default="tree", help="GDN layers over the prompts")
     a = ap.parse_args(argv)
     rng = np.random.default_rng(a.seed)
     # the whole batch goes on until its last sequence is done: up to `slots` tokens a step
     longest = 16 + a.tokens * a.slots + 2 * a.slots
-    model = HybridModel(seed=a.seed, positions=longest)
+    model = HybridModel(seed=a.seed, positions=longest, gated=a.gated)
     prompts = [[int(t) for t in rng.integers(0, model.V, rng.integers(1, 17))] for _ in range(a.batch)]
     dec = Decoder(model, a.batch, a.slots, rng.random((a.batch, longest), dtype=np.float32), max_pages=-(-longest // 16),
-                  dtype=a.dtype, temperature=a.temperature, top_k=a.top_k, top_p=a.top_p, min_p=a.min_p)
+                  dtype=a.dtype, temperature=a.temperature, top_k=a.top_k, top_p=a.top_p, min_p=a.min_p,
+                  prompt_form=a.prompt_form)
     seqs, steps = decode(dec, prompts, a.tokens)
     made = sum(len(s) - len(p) for s, p in zip(seqs, prompts))
     print(f"{made} tokens of {a.batch} sequences in {steps} steps: {made / (steps * a.batch):.2f} a step and sequence")
