@@ -506,8 +506,7 @@ typedef struct {
  *   weight  fp32 [d], or NULL: 1
  *   out     out_dtype [N][H d]  written; may be x itself where types and rows
  *           are the same (any other overlap is not allowed)
- * These pointers need the alignment of their elements only; rows that all
- * begin at multiples of 16 bytes, d a multiple of 8, are read in whole packs.
+ * These pointers need the alignment of their elements only.
  * In 32 bits: the squares of a head have to sum to less than 2^128. */
 int gdn_gate_norm(const gdn_gate_norm_dims* dims, const void* x, const void* gate,
                   const float* weight, void* out, hipStream_t stream);

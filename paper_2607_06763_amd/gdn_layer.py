@@ -15,6 +15,7 @@ time as other such calls of that stream, or as another graph captured there.
 from __future__ import annotations
 
 import ctypes
+import functools
 
 from .gdn_tree import GDN_BF16, GDN_F32, _check, _ptrs, _stream, lib
 
@@ -85,16 +86,27 @@ def chain(d: ChainDims, q, k, v, alpha, beta, conv_w, conv_state, conv_state_out
         (out, vs, ot, "out"), (status, ls, i32, "status", None))), _stream(stream)))
 
 
+_codes = {}  # type codes of the norms' tensors
+
+
+def _code(dtype):
+    if not _codes:
+        import torch
+        _codes.update({torch.bfloat16: GDN_BF16, torch.float32: GDN_F32})
+    return _codes.get(dtype)
+
+
 def _rows(t, shape, name, device, ld=False):
-    """Pointer, type code and row stride of a bf16 or fp32 device tensor of this shape; ld: rows may be further apart."""
-    import torch
-    if not isinstance(t, torch.Tensor):
-        raise TypeError(f"{name}: expected a torch.Tensor")
-    if t.dtype is torch.bfloat16:
-        code = GDN_BF16
-    elif t.dtype is torch.float32:
-        code = GDN_F32
-    else:
+    """Pointer, type code and row stride of a bf16 or fp32 device tensor of this shape; ld: rows may be further apart
+    (stride 0: they are not).  A tensor that is right takes the first lines; a call of few rows is bound by them."""
+    try:
+        code = _codes.get(t.dtype)
+        if code is not None and t.shape == shape and t.is_contiguous() and t.get_device() == device:
+            return t.data_ptr(), code, 0
+    except AttributeError:
+        raise TypeError(f"{name}: expected a torch.Tensor") from None
+    code = _code(t.dtype)
+    if code is None:
         raise ValueError(f"{name}: dtype {t.dtype}, expected bfloat16 or float32")
     if t.shape != shape:
         raise ValueError(f"{name}: shape {tuple(t.shape)}, expected {tuple(shape)}")
@@ -111,16 +123,31 @@ def _rows(t, shape, name, device, ld=False):
 
 
 def _param(t, n, name, device):
-    import torch
     if t is None:
         return None
-    if not isinstance(t, torch.Tensor):
-        raise TypeError(f"{name}: expected a torch.Tensor")
-    if t.dtype is not torch.float32 or t.shape != (n,) or not t.is_contiguous():
+    try:
+        if _codes.get(t.dtype) == GDN_F32 and t.shape == (n,) and t.is_contiguous() and t.get_device() == device:
+            return t.data_ptr()
+    except AttributeError:
+        raise TypeError(f"{name}: expected a torch.Tensor") from None
+    if _code(t.dtype) != GDN_F32 or t.shape != (n,) or not t.is_contiguous():
         raise ValueError(f"{name}: {t.dtype} {tuple(t.shape)}, expected contiguous float32 ({n},)")
     if not t.is_cuda or t.get_device() != device:
         raise ValueError(f"{name}: on {t.device}, expected the current device {device}")
     return t.data_ptr()
+
+
+# dims of the norms by their sizes: making one takes as long as the checks
+@functools.lru_cache(maxsize=256, typed=True)
+def _gate_dims(*sizes):
+    d = GateNormDims(*sizes)
+    return d, ctypes.byref(d)
+
+
+@functools.lru_cache(maxsize=256, typed=True)
+def _add_dims(*sizes):
+    d = AddNormDims(*sizes)
+    return d, ctypes.byref(d)
 
 
 def gate_norm(x, gate, out, weight=None, eps=1e-6, act="silu", stream=None) -> None:
@@ -134,13 +161,13 @@ def gate_norm(x, gate, out, weight=None, eps=1e-6, act="silu", stream=None) -> N
         raise ValueError(f"x: shape {tuple(x.shape)}, expected [N][H][d]")
     if act not in ACTS:
         raise ValueError(f"act: {act!r}, expected 'silu' or 'sigmoid'")
-    dev, shape = torch.cuda.current_device(), x.shape
+    dev, shape = torch._C._cuda_getDevice(), x.shape
     px, tx, ldx = _rows(x, shape, "x", dev, ld=True)
     pg, tg, ldg = (None, GDN_F32, 0) if gate is None else _rows(gate, shape, "gate", dev, ld=True)
     po, to, _ = _rows(out, shape, "out", dev)
     N, H, d = shape
-    dims = GateNormDims(N, H, d, tx, tg, to, ACTS[act], ldx, ldg, eps)
-    _check(lib().gdn_gate_norm(ctypes.byref(dims), px, pg, _param(weight, d, "weight", dev), po, _stream(stream)))
+    dims = _gate_dims(N, H, d, tx, tg, to, ACTS[act], ldx, ldg, eps)
+    _check(lib().gdn_gate_norm(dims[1], px, pg, _param(weight, d, "weight", dev), po, _stream(stream)))
 
 
 def add_norm(x, residual, res_out, out, weight=None, post_weight=None, scale=None, post=False, eps=1e-6, stream=None) -> None:
@@ -153,7 +180,7 @@ def add_norm(x, residual, res_out, out, weight=None, post_weight=None, scale=Non
         raise TypeError("x: expected a torch.Tensor")
     if x.dim() != 2:
         raise ValueError(f"x: shape {tuple(x.shape)}, expected [N][D]")
-    dev, shape = torch.cuda.current_device(), x.shape
+    dev, shape = torch._C._cuda_getDevice(), x.shape
     px, tx, _ = _rows(x, shape, "x", dev)
     pr, tr, _ = (None, None, 0) if residual is None else _rows(residual, shape, "residual", dev)
     pro, tro, _ = (None, tr, 0) if res_out is None else _rows(res_out, shape, "res_out", dev)
@@ -162,6 +189,6 @@ def add_norm(x, residual, res_out, out, weight=None, post_weight=None, scale=Non
     po, to, _ = (None, GDN_F32, 0) if out is None else _rows(out, shape, "out", dev)
     N, D = shape
     t = tro if tr is None else tr
-    dims = AddNormDims(N, D, tx, GDN_F32 if t is None else t, to, 1 if post else 0, eps)
+    dims = _add_dims(N, D, tx, GDN_F32 if t is None else t, to, 1 if post else 0, eps)
     w, pw, sc = _param(weight, D, "weight", dev), _param(post_weight, D, "post_weight", dev), _param(scale, D, "scale", dev)
-    _check(lib().gdn_add_norm(ctypes.byref(dims), px, pr, w, pw, sc, pro, po, _stream(stream)))
+    _check(lib().gdn_add_norm(dims[1], px, pr, w, pw, sc, pro, po, _stream(stream)))
