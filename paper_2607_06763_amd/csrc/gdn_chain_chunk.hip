@@ -652,6 +652,34 @@ __device__ __forceinline__ int2 head_of() {
   return make_int2(place / gridDim.x, place % gridDim.x);
 }
 
+// What a workgroup of the scan writes beside outputs and state: the status (one of
+// a sequence, with its first part), and behind the last token the conv state of
+// its `many` value channels from v0 on (of a head) and, one of a key head, of
+// that head's queries and keys.  By `threads` threads; true where there are no
+// chunks to take.
+template <typename TIn>
+__device__ __forceinline__ bool tail(const ChainArgs& a, const Part& part, const Tokens& tk, int b, int h, int v0, int many, int tid,
+                                     int threads) {
+  const int chunks = (tk.n + kC - 1) / kC, per = a.Hv / a.Hk, hk = h / per, nq = a.Hk * a.dk, nv = a.Hv * a.dv;
+  const bool one = v0 == 0 && h % per == 0;
+  if (part.c0 == 0 && one && hk == 0 && tid == 0 && a.status) a.status[b] = tk.status;
+  const bool last = part.c0 + part.M >= chunks && (part.c0 < chunks || part.c0 == 0);
+  if (last) {
+    const int all = many + (one ? 2 * a.dk : 0);
+    for (int i = tid; i < 3 * all; i += threads) {
+      const int s = i / all, c = i % all, t = tk.n - 3 + s;
+      const int which = c < many ? 2 : c < many + a.dk ? 0 : 1;  // values, queries, keys
+      const int at = which == 2 ? h * a.dv + v0 + c : hk * a.dk + (c - many) % a.dk, width = which == 2 ? nv : nq;
+      const size_t row = size_t(b) * 3 * (2 * nq + nv) + which * size_t(nq) + at;
+      float x;
+      if (t < 0) x = a.conv_state[row + size_t(t + 3) * (2 * nq + nv)];
+      else x = to_f32(static_cast<const TIn*>(which == 2 ? a.v : which == 0 ? a.q : a.k)[size_t(tk.first + t) * width + at]);
+      a.conv_state_out[row + size_t(s) * (2 * nq + nv)] = x;
+    }
+  }
+  return part.c0 >= chunks;
+}
+
 // ---------------------------------------------------------------------------
 // Many heads.  A wave holds the state of 16 value channels and does all with it;
 // the waves of a workgroup share the chunk's operands in LDS.
@@ -691,7 +719,7 @@ __global__ __launch_bounds__(NW * kWave) void scan_kernel(ChainArgs a, Part part
   const int group = hs.y * NW + w, h = hs.x, b = part.b0 + blockIdx.z, hk = h / (a.Hv / a.Hk);
   const Tokens tk = tokens_of(a, b);
   const int dk = a.dk, dv = a.dv, end = min(part.c0 + part.M, (tk.n + kC - 1) / kC);
-  if (part.c0 >= end) return;
+  if (tail<TIn>(a, part, tk, b, h, hs.y * NW * 16, NW * 16, tid, NW * kWave)) return;
   const SlotLayout l = slot_layout(a.Hk, a.Hv, dk);
   const int ch = group * 16 + n16;  // value channel
   const char* vws = value_at(a, slot_at(a, part, blockIdx.z, 0), h);
@@ -919,7 +947,10 @@ __global__ __launch_bounds__((2 * NG + kLoaders) * kWave) void scan_pair_kernel(
   const int mine = w % NG, h = hs.x, b = part.b0 + blockIdx.z, hk = h / (a.Hv / a.Hk);
   const Tokens tk = tokens_of(a, b);
   const int dk = a.dk, dv = a.dv, end = min(part.c0 + part.M, (tk.n + kC - 1) / kC), count = end - part.c0;
-  if (count <= 0) return;
+  if (count <= 0) {
+    tail<TIn>(a, part, tk, b, h, hs.y * NG * 16, NG * 16, tid, kWaves * kWave);
+    return;
+  }
   const size_t vstride = size_t(a.Hv) * dv;
 
   if (w >= 2 * NG) {  // loads, every other one of a list by each of the two waves
@@ -971,6 +1002,7 @@ __global__ __launch_bounds__((2 * NG + kLoaders) * kWave) void scan_pair_kernel(
       if (m + 2 < count) load_values(m + 2);
       if (m + 1 < count) load_first(m + 1);
     }
+    tail<TIn>(a, part, tk, b, h, hs.y * NG * 16, NG * 16, tid - 2 * NG * kWave, kLoaders * kWave);
     return;
   }
 
@@ -1150,27 +1182,6 @@ __global__ __launch_bounds__((2 * NG + kLoaders) * kWave) void scan_pair_kernel(
   store_chunk(out + size_t(n0) * vstride, vstride, tk.n - n0, q4, o);
 }
 
-// The conv state behind the last token, and the statuses.
-template <typename TIn>
-__global__ __launch_bounds__(256) void tail_kernel(ChainArgs a) {
-  const int b = blockIdx.y, nq = a.Hk * a.dk, nv = a.Hv * a.dv, C = 2 * nq + nv;
-  const Tokens tk = tokens_of(a, b);
-  if (a.status && blockIdx.x == 0 && threadIdx.x == 0) a.status[b] = tk.status;
-  const int c = blockIdx.x * 256 + threadIdx.x;
-  if (c >= C) return;
-  const size_t at = size_t(b) * 3 * C + c;
-#pragma unroll
-  for (int s = 0; s < 3; ++s) {
-    const int t = tk.n - 3 + s;
-    float x;
-    if (t < 0) x = a.conv_state[at + size_t(t + 3) * C];
-    else if (c < nq) x = to_f32(reinterpret_cast<const TIn*>(a.q)[size_t(tk.first + t) * nq + c]);
-    else if (c < 2 * nq) x = to_f32(reinterpret_cast<const TIn*>(a.k)[size_t(tk.first + t) * nq + c - nq]);
-    else x = to_f32(reinterpret_cast<const TIn*>(a.v)[size_t(tk.first + t) * nv + c - 2 * nq]);
-    a.conv_state_out[at + size_t(s) * C] = x;
-  }
-}
-
 int after_launch() {
   const hipError_t e = hipGetLastError();
   return e == hipSuccess ? GDN_OK : set_error(GDN_EHIP, "chain: launch: %s", hipGetErrorString(e));
@@ -1244,10 +1255,7 @@ int launch_chain_chunks(const ChainArgs& a, hipStream_t stream) {
   int rc = GDN_OK;
   p.ws = static_cast<char*>(stream_workspace(slot * p.G * p.M, stream, &rc));
   if (!p.ws) return rc;
-  const int C = 2 * a.Hk * a.dk + a.Hv * a.dv, G = p.G;
-  if (a.in_dtype == GDN_BF16) tail_kernel<BF16><<<dim3((C + 255) / 256, a.B), 256, 0, stream>>>(a);
-  else tail_kernel<float><<<dim3((C + 255) / 256, a.B), 256, 0, stream>>>(a);
-  if ((rc = after_launch()) != GDN_OK) return rc;
+  const int G = p.G;
   for (p.b0 = 0; p.b0 < a.B; p.b0 += G) {
     p.G = std::min(G, a.B - p.b0);
     for (p.c0 = 0; p.c0 < chunks; p.c0 += p.M) {
