@@ -40,7 +40,7 @@ typedef _Float16 f16x2 __attribute__((ext_vector_type(2)));
 typedef _Float16 f16x4 __attribute__((ext_vector_type(4)));
 
 constexpr int kC = 64;          // tokens of a chunk
-constexpr int kPrepThreads = 256;
+constexpr int kPrepThreads = 512;
 constexpr int kPrepWaves = kPrepThreads / kWave;
 constexpr int kHeads = 3;       // value heads that are inverted at once
 constexpr int kLd = kC + 4;     // floats of a row of a chunk's matrix in LDS
@@ -99,18 +99,23 @@ struct Pair {
   f16x8 hi, lo;
 };
 
+// hi of two values times a scale; lo
+__device__ __forceinline__ unsigned split2(float x, float y, float scale, unsigned& lo) {
+  f16x2 h = {(_Float16)(x * scale), (_Float16)(y * scale)};
+  // a value of its own: were it computed again for the difference, with another
+  // rounding of the product, hi + lo would miss x by a step of hi
+  asm("" : "+v"(h));
+  const f16x2 l = {(_Float16)__builtin_fmaf(x, scale, -(float)h[0]), (_Float16)__builtin_fmaf(y, scale, -(float)h[1])};
+  lo = __builtin_bit_cast(unsigned, l);
+  return __builtin_bit_cast(unsigned, h);
+}
 __device__ __forceinline__ Pair split(const float (&x)[8], float scale) {
   u32x4 hi, lo;
 #pragma unroll
   for (int e = 0; e < 4; ++e) {
-    f16x2 h = {(_Float16)(x[2 * e] * scale), (_Float16)(x[2 * e + 1] * scale)};
-    // a value of its own: were it computed again for the difference, with another
-    // rounding of the product, hi + lo would miss x by a step of hi
-    asm("" : "+v"(h));
-    const f16x2 l = {(_Float16)__builtin_fmaf(x[2 * e], scale, -(float)h[0]),
-                     (_Float16)__builtin_fmaf(x[2 * e + 1], scale, -(float)h[1])};
-    hi[e] = __builtin_bit_cast(unsigned, h);
-    lo[e] = __builtin_bit_cast(unsigned, l);
+    unsigned l;
+    hi[e] = split2(x[2 * e], x[2 * e + 1], scale, l);
+    lo[e] = l;
   }
   return {__builtin_bit_cast(f16x8, hi), __builtin_bit_cast(f16x8, lo)};
 }
@@ -149,23 +154,6 @@ __device__ __forceinline__ void store_pair(char* p, int tile, int lane, const Pa
   *reinterpret_cast<f16x8*>(q + kFrag) = x.lo;
 }
 
-// ---------------------------------------------------------------------------
-// Raw inputs
-// ---------------------------------------------------------------------------
-// 8 channels of a row.
-__device__ __forceinline__ void fetch8(const float* p, float (&x)[8]) {
-  const float4 y = ld4(p), z = ld4(p + 4);
-  x[0] = y.x, x[1] = y.y, x[2] = y.z, x[3] = y.w, x[4] = z.x, x[5] = z.y, x[6] = z.z, x[7] = z.w;
-}
-__device__ __forceinline__ void fetch8(const BF16* p, float (&x)[8]) {
-  const u32x4 u = *reinterpret_cast<const u32x4*>(p);
-#pragma unroll
-  for (int e = 0; e < 4; ++e) {
-    x[2 * e] = __uint_as_float(u[e] << 16);
-    x[2 * e + 1] = __uint_as_float(u[e] & 0xffff0000u);
-  }
-}
-
 template <int DKP>
 struct Prep {
   static constexpr int kPacks = DKP / 8, kKs = DKP / 32;
@@ -182,7 +170,7 @@ struct Prep {
 // them wait for one another.
 // ---------------------------------------------------------------------------
 template <typename TIn, int DKP>
-__global__ __launch_bounds__(kPrepThreads, 2) void chunk_kernel(ChainArgs a, Part part) {
+__global__ __launch_bounds__(kPrepThreads, 4) void chunk_kernel(ChainArgs a, Part part) {
   typedef Prep<DKP> P;
   constexpr int kKs = P::kKs, kPacks = P::kPacks;
   extern __shared__ __align__(16) char s_raw[];
@@ -213,49 +201,53 @@ __global__ __launch_bounds__(kPrepThreads, 2) void chunk_kernel(ChainArgs a, Par
   };
   fetch_gates(0, min(kHeads, per));
 
-  // keys and queries: 8 channels a thread, kLpt threads a token
+  // keys and queries: 4 channels a thread, kLpt threads a token
   {
-    constexpr int kLpt = kPacks, kGroups = kPrepThreads / kLpt, kTok = kC / kGroups;
-    static_assert(kTok * kGroups == kC, "every thread has tokens");
-    const int p = tid % kLpt, t0 = tid / kLpt * kTok, c8 = min(p * 8, dk - 8);
-    const bool in = p * 8 < dk;
-    float win[2][kTok + 3][8];
+    constexpr int kLpt = DKP / 4, kTok = kC * kLpt / kPrepThreads;
+    static_assert(kTok >= 1, "every thread has a token");
+    const int p = tid % kLpt, t0 = tid / kLpt * kTok, c4 = min(p * 4, dk - 4);
+    const bool in = p * 4 < dk;
+    float4 win[2][kTok + 3], cw[2][4];  // all loads before the first is waited for
 #pragma unroll
     for (int isq = 0; isq < 2; ++isq) {
-      const TIn* x = reinterpret_cast<const TIn*>(isq ? a.q : a.k) + hk * dk + c8;
+      const TIn* x = reinterpret_cast<const TIn*>(isq ? a.q : a.k) + hk * dk + c4;
 #pragma unroll
       for (int i = 0; i < kTok + 3; ++i) {
         const int t = min(max(t0 - 3 + i, n0 ? -3 : 0), nt - 1);
-        fetch8(x + (long long)(row0 + t) * a.Hk * dk, win[isq][i]);
+        win[isq][i] = ld4(x + (long long)(row0 + t) * a.Hk * dk);
       }
+#pragma unroll
+      for (int e = 0; e < 4; ++e)
+        cw[isq][e] = *reinterpret_cast<const float4*>(a.conv_w + size_t((isq ? hk : a.Hk + hk) * dk + c4 + e) * 4);
     }
     if (n0 == 0 && t0 < 3) {  // before the sequence's first token
 #pragma unroll
       for (int isq = 0; isq < 2; ++isq)
 #pragma unroll
         for (int i = 0; i < 3; ++i)
-          if (t0 + i < 3) fetch8(cs + size_t(t0 + i) * C + (isq ? hk : a.Hk + hk) * dk + c8, win[isq][i]);
+          if (t0 + i < 3) win[isq][i] = ld4(cs + size_t(t0 + i) * C + (isq ? hk : a.Hk + hk) * dk + c4);
     }
 #pragma unroll
     for (int isq = 0; isq < 2; ++isq) {
-      float4 cw[8];
-#pragma unroll
-      for (int e = 0; e < 8; ++e)
-        cw[e] = *reinterpret_cast<const float4*>(a.conv_w + size_t((isq ? hk : a.Hk + hk) * dk + c8 + e) * 4);
 #pragma unroll
       for (int i = 0; i < kTok; ++i) {
-        float y[8], sum = 0.0f;
+        const float4 *x = &win[isq][i], *f = cw[isq];
+        float y[4] = {silu(f[0].x * x[0].x + f[0].y * x[1].x + f[0].z * x[2].x + f[0].w * x[3].x),
+                      silu(f[1].x * x[0].y + f[1].y * x[1].y + f[1].z * x[2].y + f[1].w * x[3].y),
+                      silu(f[2].x * x[0].z + f[2].y * x[1].z + f[2].z * x[2].z + f[2].w * x[3].z),
+                      silu(f[3].x * x[0].w + f[3].y * x[1].w + f[3].z * x[2].w + f[3].w * x[3].w)};
+        float sum = 0.0f;
 #pragma unroll
-        for (int e = 0; e < 8; ++e) {
-          const auto& x = win[isq];
-          y[e] = silu(cw[e].x * x[i][e] + cw[e].y * x[i + 1][e] + cw[e].z * x[i + 2][e] + cw[e].w * x[i + 3][e]);
+        for (int e = 0; e < 4; ++e) {
           if (!in || t0 + i >= nt) y[e] = 0.0f;
           sum += y[e] * y[e];
         }
-        const Pair x8 = split(y, rsqrt_hw(group_sum<kLpt>(sum) + 1e-6f) * kUnit);
-        char* d = s_kq + isq * 2 * P::kPlane + (p * (kC + 1) + t0 + i) * 16;
-        *reinterpret_cast<f16x8*>(d) = x8.hi;
-        *reinterpret_cast<f16x8*>(d + P::kPlane) = x8.lo;
+        const float scale = rsqrt_hw(group_sum<kLpt>(sum) + 1e-6f) * kUnit;
+        unsigned lo0, lo1;
+        const unsigned hi0 = split2(y[0], y[1], scale, lo0), hi1 = split2(y[2], y[3], scale, lo1);
+        char* d = s_kq + isq * 2 * P::kPlane + (p / 2 * (kC + 1) + t0 + i) * 16 + p % 2 * 8;
+        *reinterpret_cast<uint2*>(d) = make_uint2(hi0, hi1);
+        *reinterpret_cast<uint2*>(d + P::kPlane) = make_uint2(lo0, lo1);
       }
     }
   }
@@ -266,22 +258,19 @@ __global__ __launch_bounds__(kPrepThreads, 2) void chunk_kernel(ChainArgs a, Par
     return Pair{*reinterpret_cast<const f16x8*>(d), *reinterpret_cast<const f16x8*>(d + P::kPlane)};
   };
   // k_j.k_i and k_j.q_i, rows j, columns i, in the units of a lower triangular
-  // operand: w and w + 4 (what is above the diagonal stays 0)
-  f32x4 kk[2][2] = {}, kq[2][2] = {};
-#pragma unroll
-  for (int n = 0; n < 2; ++n) {
-    const int u = w + 4 * n, t = lower_tile(u);
-    if (u >= 6) continue;
+  // operand, one a wave (what is above the diagonal stays 0)
+  const int unit = min(w, 5), tile = lower_tile(unit), step = lower_col(unit);
+  f32x4 kk[2] = {}, kq[2] = {};
+  if (w < 6) {
 #pragma unroll
     for (int s = 0; s < kKs; ++s) {
-      const Pair k = rows_of(0, t, s), q = rows_of(1, t, s);
+      const Pair k = rows_of(0, tile, s), q = rows_of(1, tile, s);
 #pragma unroll
       for (int e = 0; e < 2; ++e) {
-        const int j = 2 * lower_col(u) + e;
-        if (j > t) continue;
-        const Pair x = rows_of(0, j, s);
-        kk[n][e] = mma3(x, k, kk[n][e]);
-        kq[n][e] = mma3(x, q, kq[n][e]);
+        if (2 * step + e > tile) continue;
+        const Pair x = rows_of(0, 2 * step + e, s);
+        kk[e] = mma3(x, k, kk[e]);
+        kq[e] = mma3(x, q, kq[e]);
       }
     }
   }
@@ -306,8 +295,9 @@ __global__ __launch_bounds__(kPrepThreads, 2) void chunk_kernel(ChainArgs a, Par
     store_pair(kws, u, lane, x);
   }
 #pragma unroll
-  for (int n = 0; n < kKs * 4 / kPrepWaves; ++n) {
+  for (int n = 0; n < (kKs * 4 + kPrepWaves - 1) / kPrepWaves; ++n) {
     const int u = n * kPrepWaves + w, c = u / 2 * 16 + n16, s = u % 2;
+    if (u >= kKs * 4) continue;
     Pair x;
 #pragma unroll
     for (int j = 0; j < 8; ++j) {
@@ -349,15 +339,11 @@ __global__ __launch_bounds__(kPrepThreads, 2) void chunk_kernel(ChainArgs a, Par
     }
     __syncthreads();
     // A, to be inverted, and Y
-    for (int r = 0; r < nr; ++r) {
-      const double* lg = s_log + r * kC;
-      const int n16 = opaque(lane & 15), q4 = opaque(lane >> 4);
-      char* y_out = value_at(a, slot, hk * per + r0 + r) + kYAt;
-#pragma unroll
-      for (int n = 0; n < 2; ++n) {
-        const int u = w + 4 * n, i = 16 * lower_tile(u) + n16, j0 = 32 * lower_col(u) + 4 * q4;
-        if (u >= 6) continue;
-        const double li = lg[i];
+    if (w < 6) {
+      for (int r = 0; r < nr; ++r) {
+        const int n16 = opaque(lane & 15), q4 = opaque(lane >> 4);  // addresses are computed here, not held
+        const int i = 16 * tile + n16, j0 = 32 * step + 4 * q4;
+        const double *lg = s_log + r * kC, li = lg[i];
         const float bi = s_beta[r * kC + i] * (1.0f / (kUnit * kUnit));
         float y[8];
 #pragma unroll
@@ -367,12 +353,12 @@ __global__ __launch_bounds__(kPrepThreads, 2) void chunk_kernel(ChainArgs a, Par
           for (int k = 0; k < 4; ++k) {
             const int j = j0 + 16 * e + k;
             const float f = j <= i ? __expf(float(li - lg[j])) : 0.0f;
-            x[k] = j < i ? bi * kk[n][e][k] * f : 0.0f;
-            y[4 * e + k] = kq[n][e][k] * f;
+            x[k] = j < i ? bi * kk[e][k] * f : 0.0f;
+            y[4 * e + k] = kq[e][k] * f;
           }
           *reinterpret_cast<f32x4*>(s_t + (r * kC + i) * kLd + j0 + 16 * e) = x;
         }
-        store_pair(y_out, u, lane, split(y, 1.0f / kUnit));
+        store_pair(value_at(a, slot, hk * per + r0 + r) + kYAt, unit, lane, split(y, 1.0f / kUnit));
       }
     }
     __syncthreads();
@@ -447,17 +433,12 @@ __global__ __launch_bounds__(kPrepThreads, 2) void chunk_kernel(ChainArgs a, Par
     }
     __syncthreads();
 
-    for (int r = 0; r < nr; ++r) {
-      char* t_out = value_at(a, slot, hk * per + r0 + r);
-      const int n16 = opaque(lane & 15), q4 = opaque(lane >> 4);
-#pragma unroll
-      for (int n = 0; n < 2; ++n) {
-        const int u = w + 4 * n;
-        if (u >= 6) continue;
-        const float* x = s_t + (r * kC + 16 * lower_tile(u) + n16) * kLd + 32 * lower_col(u) + 4 * q4;
+    if (w < 6) {
+      for (int r = 0; r < nr; ++r) {
+        const float* x = s_t + (r * kC + 16 * tile + n16) * kLd + 32 * step + 4 * q4;
         const float4 y = *reinterpret_cast<const float4*>(x), z = *reinterpret_cast<const float4*>(x + 16);
         const float f[8] = {y.x, y.y, y.z, y.w, z.x, z.y, z.z, z.w};
-        store_pair(t_out, u, lane, split(f, s_scale[r]));
+        store_pair(value_at(a, slot, hk * per + r0 + r), unit, lane, split(f, s_scale[r]));
       }
     }
     __syncthreads();  // the matrices are read
