@@ -16,6 +16,13 @@ constexpr int kOwn = 2;  // channels that a thread convolves
 // workgroup per (slice of rows, value head, sequence); every workgroup
 // convolves the key head's channels and its own value channels, and keeps the
 // last three raw inputs of each in registers.
+//
+// Bound by the state, read and written once a call: one token of 32 sequences of
+// 16 / 48 heads of 128, 210 MB, in 33 us called again and again (part of it stays
+// in the caches), 45 us in turn with other work; a copy of as much takes 41.  A
+// token of one sequence takes 5 us, the latency of a launch, of the loads, which go
+// out together, and of the stores; each further one 0.9 us, for a barrier and the
+// sums over a row's lanes.
 template <typename TIn, typename TOut, int DK, int RP>
 __global__ __launch_bounds__(kThreads) void chain_step_kernel(ChainArgs a) {
   constexpr int kLanes = DK >= 32 ? 8 : 4, kCols = DK / kLanes, kRows = kThreads / kLanes * RP;

@@ -168,6 +168,12 @@ struct Prep {
 // all of its value heads: keys and queries are convolved once.  Loads have no
 // branch around them (rows are clamped and values selected): a branch each made
 // them wait for one another.
+//
+// Bound by its own chain of steps, convolution, products, inversion, stores, each
+// behind a barrier: 14 us for a single chunk.  1365 workgroups, a third of 4
+// sequences of 4096 tokens of 16 / 48 heads of 128, take 73 us and write 233 MB,
+// 3.2 TB/s; a workgroup has 69 KB of LDS, two are on a CU, and half of the wave
+// cycles are spent waiting.
 // ---------------------------------------------------------------------------
 template <typename TIn, int DKP>
 __global__ __launch_bounds__(kPrepThreads, 4) void chunk_kernel(ChainArgs a, Part part) {
@@ -674,6 +680,11 @@ __device__ __forceinline__ bool tail(const ChainArgs& a, const Part& part, const
 // With one wave a SIMD nothing hides an LDS read but the wave's own products:
 // operand pairs are read a group of four ahead of them, two accumulators in turn
 // (12 products of 16 clocks over about 130 of a read).
+//
+// Bound by the vector and matrix instructions of a wave, which do not overlap
+// enough: 4 sequences of 4096 tokens of 48 value heads of 128, 192 workgroups of
+// eight waves, 590 us, 15000 to 17000 clocks a chunk; the matrix units are busy for
+// 34 % of them, the vector units for 48 % (operands made of values and of V', scales).
 // ---------------------------------------------------------------------------
 template <typename TIn, int DKP, int NW>
 struct Scan {
@@ -898,6 +909,11 @@ __global__ __launch_bounds__(NW * kWave) void scan_kernel(ChainArgs a, Part part
 // other, a part behind, makes the outputs and convolves the next chunk's values.
 // They pass the state, V' and the values as operands through LDS.  Two more waves
 // do all loads (a wave has at most 64 on their way).
+//
+// Bound by the state's wave, whose steps wait for one another (8192 tokens of one
+// sequence of 48 heads of 128: 409 us, 6500 to 7000 clocks a chunk, matrix units 22 %
+// busy), and behind it by the loads, 170 KB a chunk and CU at about 30 bytes a clock.
+// With one wave for both 1024 tokens of 32 such heads take 109 us, with two 70.
 // ---------------------------------------------------------------------------
 constexpr int kLoaders = 2;
 
@@ -1195,18 +1211,25 @@ int launch_pairs(const ChainArgs& a, const Part& p, hipStream_t stream) {
   return after_launch();
 }
 
+// The fewest of a head's channels a workgroup that leave at most one for each of the
+// 256 CUs, else all of them.  us for 1024 tokens and heads of 128, one key head a value
+// head (pairs of waves: 1 and 2 of them; waves: 2, 4 and 8):
+//   32 heads    70  71   109 109 130
+//   48         116  82   117 116 139
+//   64         124  90   122 121 143
+//   80         173 142   213 134 156
+//   128        282 207   260 187 207
+//   144          - 298   389 303 244
+//   256        583 429   545 382 324
 template <typename TIn, typename TOut, int DKP>
 int launch_scan(const ChainArgs& a, const Part& p, hipStream_t stream) {
-  const int groups = a.dv / 16;
-  const long long heads = (long long)(p.G) * a.Hv;
-  if (groups == 1 || heads * groups <= 256) return launch_pairs<TIn, TOut, DKP, 1>(a, p, stream);
-  if (heads * groups <= 512) return launch_pairs<TIn, TOut, DKP, 2>(a, p, stream);
-  // waves of a workgroup: as many as share a head, but a workgroup a CU
-  int nw = groups;
-  while (nw > 2 && heads * (groups / nw) < 192) nw /= 2;
-  if (nw >= 8) return launch_waves<TIn, TOut, DKP, 8>(a, p, stream);
-  if (nw == 4) return launch_waves<TIn, TOut, DKP, 4>(a, p, stream);
-  return launch_waves<TIn, TOut, DKP, 2>(a, p, stream);
+  const int groups = a.dv / 16;  // of 16 value channels
+  const long long all = (long long)(p.G) * a.Hv * groups;
+  if (groups == 1 || all <= 256) return launch_pairs<TIn, TOut, DKP, 1>(a, p, stream);
+  if (all <= 512) return launch_pairs<TIn, TOut, DKP, 2>(a, p, stream);
+  if (groups == 2) return launch_waves<TIn, TOut, DKP, 2>(a, p, stream);
+  if (groups == 4 || all <= 1024) return launch_waves<TIn, TOut, DKP, 4>(a, p, stream);
+  return launch_waves<TIn, TOut, DKP, 8>(a, p, stream);
 }
 
 template <typename TIn, int DKP>

@@ -92,9 +92,9 @@ int gdn_chain(const gdn_chain_dims* dims, const int32_t* start, const int32_t* n
   a.out = out;
   a.status = status;
   // A token costs the steps about the same each, the chunked form 64 of them.
-  // us for 16 and 24 tokens (steps, chunks), 16 / 48 heads of 128: one sequence
-  // 18.5, 27.9 and 25.6, 28.0; 8 of them 50, 56 and 70, 57; 32 of them 96, 124 and
-  // 132, 125; 4 / 8 heads of 64, 16 sequences: 13.6, 24.3 and 18.2, 24.2.
+  // us for 16 and 24 tokens (steps, chunks; chunks take the same up to 64), 16 / 48
+  // heads of 128: one sequence 18.5, 24.6 and 25.6, 24.6; 8 of them 49, 51 and 70,
+  // 51; 32 of them 95, 120 and 132, 120; 16 of 4 / 8 heads of 64: 13.2, 21 and 18.2, 21
   return a.T <= GDN_CHAIN_STEP_T ? launch_chain_steps(a, stream) : launch_chain_chunks(a, stream);
 }
 

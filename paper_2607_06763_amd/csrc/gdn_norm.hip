@@ -169,6 +169,9 @@ __global__ __launch_bounds__(kThreads) void gate_norm_kernel(GateNormArgs a, Typ
   }
 }
 
+// Bound by the bytes: 8192 rows of 4096 channels, bf16 branch, fp32 residual read
+// and written, both norms, bf16 out, 403 MB in 86 us, 4.7 TB/s; the second sum waits
+// for the first.  999 rows of 2051 fp32 channels 9.8 us, one row 3 to 4 us.
 template <int K, int G>
 __global__ __launch_bounds__(kThreads) void add_norm_kernel(AddNormArgs a, Types ty) {
   __shared__ float s_sum[4][4];

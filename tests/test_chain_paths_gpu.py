@@ -33,7 +33,8 @@ FORMS = [
     (3, 2, 6, 128, 64, 150, "bf16", "f32"), (5, 2, 8, 32, 128, 90, "f32", "bf16"), (7, 2, 8, 128, 128, 140, "bf16", "bf16"),
     (9, 4, 16, 64, 64, 130, "f32", "f32"), (12, 4, 16, 32, 64, 100, "bf16", "f32"), (6, 8, 16, 128, 128, 129, "f32", "f32"),
     (12, 4, 16, 16, 128, 130, "bf16", "f32"), (12, 8, 16, 128, 128, 70, "f32", "bf16"), (13, 16, 16, 64, 128, 66, "bf16", "bf16"),
-    (40, 2, 16, 16, 16, 65, "f32", "f32"),
+    (40, 2, 16, 16, 16, 65, "f32", "f32"), (33, 2, 8, 32, 32, 70, "bf16", "f32"), (40, 4, 8, 128, 32, 66, "f32", "bf16"),
+    (35, 8, 8, 64, 32, 129, "bf16", "bf16"),
 ]
 
 
