@@ -466,10 +466,10 @@ typedef struct {
  *              length is negative or above T, or whose rows are outside
  *              [0, rows); 0 otherwise
  * A sequence without tokens, or with a non-zero status, keeps S and gets
- * conv_state_out = conv_state.  No tensor may overlap S or conv_state_out.  A
- * decay below the smallest normal float counts as that in the chunked form.
- * Inputs have to be finite: an infinity or NaN may reach every token of its
- * chunk, those before it too.
+ * conv_state_out = conv_state.  No tensor may overlap S, conv_state_out or
+ * status.  A decay below the smallest normal float counts as that in the
+ * chunked form.  Inputs have to be finite: an infinity or NaN may reach every
+ * token of its chunk, those before it too.
  * Short sequences (T <= GDN_CHAIN_STEP_T) go token by token with the state in
  * registers and need no workspace.  Longer ones go in chunks of 64 tokens, all
  * products in 32 bits (fp16 pairs, three products, fp32 sums), through a

@@ -61,12 +61,17 @@ int gdn_chain(const gdn_chain_dims* dims, const int32_t* start, const int32_t* n
   const size_t e = width(dims->in_dtype), ob = rows * dims->Hv * dims->dv * width(dims->out_dtype);
   const size_t kb = rows * dims->Hk * dims->dk * e, vb = rows * dims->Hv * dims->dv * e, gb = rows * dims->Hv * e;
   const size_t sb = size_t(dims->B) * dims->Hv * dims->dv * dims->dk * 4;
-  const std::pair<const void*, size_t> others[] = {{q, kb},   {k, kb},          {v, vb},           {alpha, gb},
-                                                   {beta, gb}, {conv_w, 16 * C}, {conv_state, cs}, {out, ob}};
-  for (const auto& o : others)
-    if (overlap(S, sb, o.first, o.second) || overlap(conv_state_out, cs, o.first, o.second) || overlap(S, sb, conv_state_out, cs) ||
-        (o.first != out && overlap(out, ob, o.first, o.second)))
-      return set_error(GDN_EINVAL, "chain: S, conv_state_out or out overlaps another tensor");
+  const size_t ib = size_t(dims->B) * 4;
+  const std::pair<const void*, size_t> inputs[] = {{q, kb},    {k, kb},          {v, vb},           {alpha, gb},
+                                                   {beta, gb}, {conv_w, 16 * C}, {conv_state, cs}, {start, ib + 4},
+                                                   {n_new, ib}};
+  const std::pair<const void*, size_t> outputs[] = {{S, sb}, {conv_state_out, cs}, {out, ob}, {status, ib}};
+  for (const auto& o : outputs) {
+    bool bad = false;
+    for (const auto& i : inputs) bad = bad || overlap(o.first, o.second, i.first, i.second);
+    for (const auto& i : outputs) bad = bad || (&i != &o && overlap(o.first, o.second, i.first, i.second));
+    if (bad) return set_error(GDN_EINVAL, "chain: S, conv_state_out, out or status overlaps another tensor");
+  }
   ChainArgs a;
   a.B = dims->B;
   a.T = dims->T;

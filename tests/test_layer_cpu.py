@@ -72,6 +72,17 @@ def test_chain_pointers(lib):
             for shift in (sizes[other] - 16, 16 - sizes[written]):  # their last and first bytes
                 assert chain(lib, d, **{other: at, written: at + shift}) == G.GDN_EINVAL, (written, other)
                 assert "overlap" in G.last_error()
+    at = 1 << 50
+    sizes = dict(sizes, status=8, n_new=8, start=12)
+    for written in ("S", "out", "conv_state_out", "status"):
+        for other in sizes:
+            if "status" not in (written, other) and other not in ("n_new", "start") or other == written:
+                continue
+            rows = dict(start=0) if other != "start" else {}
+            dims = d if other != "start" else L.make_chain_dims(2, 4, 1, 2, 16, 16, rows=8)
+            for shift in (sizes[other] - 4, 4 - sizes[written]):
+                assert chain(lib, dims, **dict(rows, **{other: at, written: at + shift})) == G.GDN_EINVAL, (written, other)
+                assert "overlap" in G.last_error()
 
 
 def gate(lib, d, x=1 << 32, g=2 << 32, w=3 << 32, out=4 << 32):
