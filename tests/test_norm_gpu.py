@@ -151,3 +151,49 @@ def test_add_norm(L, case):
         row = np.sqrt((mag * mag).mean(-1, keepdims=True)) / np.sqrt((z * z).mean(-1, keepdims=True) + eps)
         want = z * f
         assert np.all(np.abs(f64(out) - want) <= REL * mag * np.abs(f) + (REL * (1 + row) + half(to)) * np.abs(want))
+
+
+@pytest.mark.parametrize("D", [16, 72, 640, 2051])
+def test_rows_are_their_own(L, D):
+    """NaN, infinities and zeros in some rows (heads) reach no other."""
+    import torch
+    x, r, g = data(16, 41, D), data(17, 41, D), data(18, 41, D, dtype="bf16")
+    run = lambda: (L.add_norm(x, r, ro, o, post=True), L.gate_norm(x.view(41, 1, D), g.view(41, 1, D), h.view(41, 1, D)))
+    ro, o, h = (torch.empty_like(x) for _ in range(3))
+    run()
+    want = [t.clone() for t in (ro, o, h)]
+    x[3], x[17, D // 2], r[20], g[33, 0] = float("nan"), float("inf"), float("nan"), float("nan")
+    x[5] = 0
+    run()
+    keep = [i for i in range(41) if i not in (3, 5, 17, 20, 33)]
+    for a, b in zip((ro, o, h), want):
+        assert torch.equal(a[keep], b[keep])
+    assert torch.equal(ro[5], r[5]) and (h[5] == 0).all()
+    assert all(torch.isnan(t[3]).all() for t in (ro, o, h))
+
+
+def test_graph_and_stream(L):
+    """Norms around a block captured on a stream of their own and replayed on new inputs, eager work between."""
+    import torch
+    x, r, g, s = data(19, 70, 384), data(20, 70, 384), data(21, 70, 384, dtype="bf16"), data(22, 384)
+    ro, o = torch.empty_like(r), torch.empty_like(x, dtype=torch.bfloat16)
+    y = torch.empty(70, 6, 64, device="cuda")
+
+    def work(ro, o, y):
+        L.gate_norm(x.view(70, 6, 64), g.view(70, 6, 64), y)
+        L.add_norm(y.view(70, 384), r, ro, o, scale=s, post=True)
+
+    stream = torch.cuda.Stream()
+    stream.wait_stream(torch.cuda.current_stream())
+    torch.cuda.synchronize()
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph, stream=stream):
+        work(ro, o, y)
+    for k in range(4):
+        x.copy_(data(30 + k, 70, 384))
+        g.copy_(data(40 + k, 70, 384, dtype="bf16"))
+        graph.replay()
+        want = [torch.empty_like(t) for t in (ro, o, y)]
+        work(*want)
+        torch.cuda.synchronize()
+        assert all(torch.equal(a, b) for a, b in zip((ro, o, y), want)), k
