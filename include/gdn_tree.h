@@ -471,9 +471,13 @@ typedef struct {
  * chunked form.  Inputs have to be finite: an infinity or NaN may reach every
  * token of its chunk, those before it too.
  * Short sequences (T <= GDN_CHAIN_STEP_T) go token by token with the state in
- * registers and need no workspace.  Longer ones go in chunks of 64 tokens, all
- * products in 32 bits (fp16 pairs, three products, fp32 sums), through a
- * workspace that the library keeps (see Workspaces above), at most
+ * registers, in fp32, and need no workspace.  Longer ones go in chunks of 64
+ * tokens: operands are pairs of fp16 values (22 bits), products three on them
+ * with fp32 sums, as near as fp32 products on ordinary inputs.  Beside that an
+ * output, and the state, may be off by about 2^-34 of the largest value (or row of
+ * the state) of its head in this chunk or the one before, also where the decays
+ * have forgotten that since, which the token by token form does not have.  They go
+ * through a workspace that the library keeps (see Workspaces above), at most
  * GDN_CHAIN_WORKSPACE bytes or what one chunk of one sequence needs:
  * a chunk takes 768 Hk dk + 25600 Hv bytes (dk of 16 as 32). */
 #define GDN_CHAIN_STEP_T 20

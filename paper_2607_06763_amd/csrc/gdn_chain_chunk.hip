@@ -16,11 +16,15 @@
 // beforehand, as first built, it was 295 KB, and chunk_kernel, which then
 // convolves the values too, took three times as long.
 //
-// Products.  The outputs have 32-bit accuracy, so each operand is a pair of fp16
-// values, hi + lo, 22 bits together, and a product is three on the matrix units
-// (hi hi, hi lo, lo hi) with 32-bit sums: 2^-22 of an operand is lost.  Scales
-// are powers of two, exact: 2^10 for what is at most 1 (unit keys, queries, Y),
-// else by the largest value of the matrix or of the operand's column.
+// Products.  Each operand is a pair of fp16 values, hi + lo, 22 bits together, and
+// a product is three on the matrix units (hi hi, hi lo, lo hi) with 32-bit sums:
+// lo lo, 2^-22 of a product, is left out, and the outputs come out as near as
+// those of fp32 products.  Scales are powers of two, exact: 2^15 for what is at
+// most 1 (unit keys, queries), else they take the largest value of the matrix or of
+// the operand's column to 2^14 .. 2^15.  A pair has its 22 bits down to 2^-16 of
+// that value; what is smaller is off by up to 2^-39 of it (lo's last step is 2^-24).
+// So a value that is forgotten inside its chunk, 10^6 times what follows it, costs
+// that 1e-6 of its accuracy where fp32 loses nothing.
 //
 // Operand order.  A tile's accumulators hold rows 4 q + r (q = lane / 16) of
 // column lane % 16, and an operand 8 values of one row or column.  Two tiles of
@@ -44,7 +48,7 @@ constexpr int kPrepThreads = 512;
 constexpr int kPrepWaves = kPrepThreads / kWave;
 constexpr int kHeads = 3;       // value heads that are inverted at once
 constexpr int kLd = kC + 4;     // floats of a row of a chunk's matrix in LDS
-constexpr float kUnit = 1024.0f;  // scale of what is at most 1
+constexpr float kUnit = 32768.0f;  // scale of what is at most 1
 constexpr int kFrag = 1024;     // bytes of an operand tile: 64 lanes of 8 fp16 values
 
 // ---------------------------------------------------------------------------
@@ -128,21 +132,23 @@ __device__ __forceinline__ f32x4 mma3(const Pair& a, const Pair& b, f32x4 c) {
   return mma(a.hi, b.hi, c);
 }
 
-// Power of two that takes m to 2^13 .. 2^14, and its inverse (both normal
-// floats: m is clamped to 2^-113 .. 2^126).
+// Power of two that takes m to 2^14 .. 2^15, and its inverse (both normal
+// floats: m is clamped to 2^-112 .. 2^126).
 __device__ __forceinline__ void f16_scale(float m, float& scale, float& inv) {
   int ex = int((__float_as_uint(m) >> 23) & 0xffu);
-  ex = ex < 14 ? 14 : ex > 253 ? 253 : ex;
-  scale = __uint_as_float(unsigned(267 - ex) << 23);
-  inv = __uint_as_float(unsigned(ex - 13) << 23);
+  ex = ex < 15 ? 15 : ex > 253 ? 253 : ex;
+  scale = __uint_as_float(unsigned(268 - ex) << 23);
+  inv = __uint_as_float(unsigned(ex - 14) << 23);
 }
 
-// Over the four lanes of a column (lane % 16): rows of 16 lanes trade places.
+// Of values >= 0 (their bits compare as they do, which spares the instructions that
+// quiet a NaN), over the four lanes of a column (lane % 16): rows of 16 lanes trade
+// places.
 __device__ __forceinline__ float column_max(float x) {
   auto r = __builtin_amdgcn_permlane16_swap(__float_as_uint(x), __float_as_uint(x), false, false);
-  x = fmaxf(__uint_as_float(r[0]), __uint_as_float(r[1]));
-  r = __builtin_amdgcn_permlane32_swap(__float_as_uint(x), __float_as_uint(x), false, false);
-  return fmaxf(__uint_as_float(r[0]), __uint_as_float(r[1]));
+  const unsigned y = max(r[0], r[1]);
+  r = __builtin_amdgcn_permlane32_swap(y, y, false, false);
+  return __uint_as_float(max(r[0], r[1]));
 }
 __device__ __forceinline__ Pair load_pair(const char* p, int tile, int lane) {
   const char* q = p + size_t(tile) * 2 * kFrag + lane * 16;
@@ -160,7 +166,7 @@ struct Prep {
   static constexpr int kPlane = kPacks * (kC + 1) * 16;       // bytes of hi or lo of K or Q: [pack][token]
   static constexpr int kMat = kC * kLd * int(sizeof(float));  // a chunk's matrix
   static constexpr int kRows = 4 * kPlane > kHeads * kMat ? 4 * kPlane : kHeads * kMat;
-  static constexpr int kLds = kRows + kHeads * (kC * 12 + 4);
+  static constexpr int kLds = kRows + kHeads * (kC * 12 + 8);
 };
 
 // ---------------------------------------------------------------------------
@@ -184,7 +190,7 @@ __global__ __launch_bounds__(kPrepThreads, 4) void chunk_kernel(ChainArgs a, Par
   float* s_t = reinterpret_cast<float*>(s_raw);  // [head][64][kLd]
   double* s_log = reinterpret_cast<double*>(s_raw + P::kRows);  // [head][64]
   float* s_beta = reinterpret_cast<float*>(s_log + kHeads * kC);
-  float* s_scale = s_beta + kHeads * kC;  // of (I + A)^-1
+  float *s_scale = s_beta + kHeads * kC, *s_yscale = s_scale + kHeads;  // of (I + A)^-1, of Y
   const int tid = threadIdx.x, lane = tid % kWave, w = __builtin_amdgcn_readfirstlane(tid / kWave);
   const int n16 = lane & 15, q4 = lane >> 4;
   const int hk = blockIdx.x, m = blockIdx.y, b = part.b0 + blockIdx.z;
@@ -335,12 +341,14 @@ __global__ __launch_bounds__(kPrepThreads, 4) void chunk_kernel(ChainArgs a, Par
       const float f = __expf(float(g));
       sc[lane] = be;
       sc[kC + lane] = f;
-      const float to_end = __expf(float(__shfl(g, kC - 1) - g));
-      sc[2 * kC + lane] = to_end;
-      const float most = column_max(group_max<16>(to_end));
+      sc[2 * kC + lane] = __expf(float(__shfl(g, kC - 1) - g));
+      float grown = 1.0f, ys, yi;  // the most that a "decay" above 1 makes of a value
+      if (__any(al > 1.0f)) grown = __expf(group_sum<kWave>(al > 1.0f ? __logf(al) : 0.0f));
+      f16_scale(grown, ys, yi);
       if (lane == kC - 1) {
         sc[3 * kC] = f;
-        sc[3 * kC + 3] = most;
+        sc[3 * kC + 2] = yi;
+        s_yscale[w] = ys * (1.0f / (kUnit * kUnit));
       }
     }
     __syncthreads();
@@ -364,7 +372,7 @@ __global__ __launch_bounds__(kPrepThreads, 4) void chunk_kernel(ChainArgs a, Par
           }
           *reinterpret_cast<f32x4*>(s_t + (r * kC + i) * kLd + j0 + 16 * e) = x;
         }
-        store_pair(value_at(a, slot, hk * per + r0 + r) + kYAt, unit, lane, split(y, 1.0f / kUnit));
+        store_pair(value_at(a, slot, hk * per + r0 + r) + kYAt, unit, lane, split(y, s_yscale[r]));
       }
     }
     __syncthreads();
@@ -434,7 +442,6 @@ __global__ __launch_bounds__(kPrepThreads, 4) void chunk_kernel(ChainArgs a, Par
         s_scale[w] = scale;
         float* sc = reinterpret_cast<float*>(value_at(a, slot, hk * per + r0 + w) + kScalarsAt) + 3 * kC;
         sc[1] = inv;
-        sc[2] = kC * most;  // at least the largest sum of a row
       }
     }
     __syncthreads();
@@ -518,45 +525,52 @@ __device__ __forceinline__ void times_kt(const Pair (&f)[4], const Pair (&vd)[2]
   }
 }
 
-// What a chunk's scalars give: the decay over it, 1 / scale of (I + A)^-1, a
-// bound of the sums of its rows, the largest decay to the chunk's end.
+// What a chunk's scalars give: the decay over it, 1 / scale of (I + A)^-1 and of Y.
 struct ChunkScalars {
-  float last, inv, rows, most;
+  float last, inv, y;
 };
 __device__ __forceinline__ ChunkScalars scalars_of(const float* s_sc) {
   const float4 x = *reinterpret_cast<const float4*>(s_sc + 3 * kC);
-  return {x.x, x.y, x.z, x.w};
+  return {x.x, x.y, x.z};
 }
 
 // V' as operands, plain and decayed to the chunk's end, and the scale of the
-// state behind the chunk.  Scales come from bounds, so that no value waits for
-// the largest of all: |V'| is at most a row's sum of (I + A)^-1 times mr, the
-// largest value of its operand (in a column), and the state at most `last` times
-// what it was plus 64 times that.  They are up to 2^6 and 2^12 too small, and
-// leave the pairs their 22 bits: hi is normal down to 2^-28 of the bound, lo
-// counts in steps of 2^-38 of it.
+// state behind the chunk.  V' and V' decayed have scales from their own largest
+// values in the column: a bound from the largest value in the chunk would keep
+// one that the decays have forgotten by its end, and what is left would lose its
+// bits to it, without limit.  The state's comes from a bound, so that it does not
+// wait for the state: at most `last` times what it was plus 64 times the largest
+// decayed V'.  A unit key leaves at least 1 / sqrt(dk) of that V', so the bound is
+// up to 2^10 too large: the state's pairs have 22 bits down to 2^-6 of its largest
+// value, and what is smaller is off by up to 2^-29 of that.
 struct Scales {
-  float v, iv, d, id, s, is;  // of V', of V' decayed, of the state; their inverses
+  float iv, id, s, is;  // 1 / scale of V', of V' decayed; scale of the state, 1 / it
 };
-__device__ __forceinline__ Scales scales_of(const ChunkScalars& c, float mr, float mx) {
+// x: accumulators of (I + A)^-1 times its operand, in units of 1 / ix; mx: the
+// state's largest value
+__device__ __forceinline__ Scales value_operands(const f32x4 (&x)[4], const float* s_sc, int q4, float ix, float last, float mx,
+                                                 Pair (&vp)[2], Pair (&vd)[2]) {
+  f32x4 xd[4];
+  float mv = 0.0f, md = 0.0f, sv, sd;
+#pragma unroll
+  for (int t = 0; t < 4; ++t) {
+    xd[t] = x[t] * *reinterpret_cast<const f32x4*>(s_sc + 2 * kC + 16 * t + 4 * q4);
+#pragma unroll
+    for (int r = 0; r < 4; ++r) mv = fmaxf(mv, fabsf(x[t][r])), md = fmaxf(md, fabsf(xd[t][r]));
+  }
   Scales k;
-  const float v = c.rows * mr, d = v * c.most;
-  f16_scale(v, k.v, k.iv);
-  f16_scale(d, k.d, k.id);
-  f16_scale(fabsf(c.last) * mx + kC * d, k.s, k.is);
-  return k;
-}
-// x: accumulators of (I + A)^-1 times its operand, which has the scale 1 / ir
-__device__ __forceinline__ void value_operands(const f32x4 (&x)[4], const float* s_sc, int q4, const ChunkScalars& c, float ir,
-                                               const Scales& k, Pair (&vp)[2], Pair (&vd)[2]) {
-  const float fv = ir * k.v * c.inv, fd = ir * k.d * c.inv;
+  md = column_max(md);
+  f16_scale(column_max(mv), sv, k.iv);
+  f16_scale(md, sd, k.id);
+  f16_scale(fabsf(last) * mx + kC * (md * ix), k.s, k.is);
+  k.iv *= ix;
+  k.id *= ix;
 #pragma unroll
   for (int s = 0; s < 2; ++s) {
-    const f32x4 d0 = *reinterpret_cast<const f32x4*>(s_sc + 2 * kC + 32 * s + 4 * q4);
-    const f32x4 d1 = *reinterpret_cast<const f32x4*>(s_sc + 2 * kC + 32 * s + 16 + 4 * q4);
-    vp[s] = operand(x[2 * s], x[2 * s + 1], fv);
-    vd[s] = operand(x[2 * s] * d0, x[2 * s + 1] * d1, fd);
+    vd[s] = operand(xd[2 * s], xd[2 * s + 1], sd);
+    vp[s] = operand(x[2 * s], x[2 * s + 1], sv);
   }
+  return k;
 }
 
 // This wave's loads and stores are done and its LDS reads; then the workgroup's.
@@ -839,14 +853,14 @@ __global__ __launch_bounds__(NW * kWave) void scan_kernel(ChainArgs a, Part part
     times_lower(g[1], r1, x, 1);
     __builtin_amdgcn_sched_barrier(0);
     const ChunkScalars cs = scalars_of(s_sc);
-    const Scales sc = scales_of(cs, mr, column_max(mx));
+    Scales sc;
     Pair vp[2], vd[2];
 #pragma unroll
     for (int n = kGroups / 2; n < kGroups; ++n) {
       if (n + 1 < kGroups) R::read(f[(kGroups + n + 1) & 1], s_q, n + 1, lane);
       __builtin_amdgcn_sched_barrier(0);
       R::times(f[(kGroups + n) & 1], sp, o, n);
-      if (n == kGroups / 2) value_operands(x, s_sc, q4, cs, ir, sc, vp, vd);  // V', beside the others
+      if (n == kGroups / 2) sc = value_operands(x, s_sc, q4, ir * cs.inv, cs.last, column_max(mx), vp, vd);  // beside the others
       __builtin_amdgcn_sched_barrier(0);
     }
     arrive<NW>();  // Y, K^T, raw values; K, Q and (I + A)^-1 are read
@@ -862,7 +876,7 @@ __global__ __launch_bounds__(NW * kWave) void scan_kernel(ChainArgs a, Part part
     read_kt(g[0], s_kt, 0, lane);
     __builtin_amdgcn_sched_barrier(0);
     times_lower(g[1], vp[1], y, 1);
-    const float iv = sc.iv * (a.scale * (1.0f / kUnit)), io = ik * a.scale, id = sc.id * (1.0f / kUnit);
+    const float iv = sc.iv * cs.y * a.scale, io = ik * a.scale, id = sc.id * (1.0f / kUnit);
     mx = 0.0f;
     f32x4 c[2][2];
     auto state_of = [&](int n) {
@@ -1068,9 +1082,8 @@ __global__ __launch_bounds__((2 * NG + kLoaders) * kWave) void scan_pair_kernel(
       times_lower(g[0], r0, x, 0);
       times_lower(g[1], r1, x, 1);
       const ChunkScalars cs = scalars_of(s_sc);
-      const Scales sc = scales_of(cs, mr, column_max(mx));
       Pair vp[2], vd[2];
-      value_operands(x, s_sc, q4, cs, ir, sc, vp, vd);
+      const Scales sc = value_operands(x, s_sc, q4, ir * cs.inv, cs.last, column_max(mx), vp, vd);
       store_pair(s_x, 0, lane, vp[0]);  // in place of the values, which this wave has read
       store_pair(s_x, 1, lane, vp[1]);
       s_scale[16] = sc.iv;
@@ -1149,7 +1162,7 @@ __global__ __launch_bounds__((2 * NG + kLoaders) * kWave) void scan_pair_kernel(
     values_of(m + 1);  // behind the last chunk: not used
     arrive<kWaves>();  // Q, Y; V'
     const Pair v0 = load_pair(s_x, 0, lane), v1 = load_pair(s_x, 1, lane);
-    const float iv = s_scale[16] * (a.scale * (1.0f / kUnit));
+    const float iv = s_scale[16] * scalars_of(s_sc).y * a.scale;
     typename R::Group f[2];
     Pair g[2][4];
 #pragma unroll
