@@ -100,7 +100,7 @@ enum {
   GDN_KV_BAD_LEN = 6,  /* paged cache: ctx_len or n_new out of range, or no room in the page table */
   GDN_KV_BAD_PAGE = 7, /* paged cache: a needed page-table entry outside [0, n_pages) */
   GDN_KV_BAD_POS = 8,  /* paged cache: a position without a row in the rotation table */
-  GDN_CHAIN_BAD_LEN = 9 /* chain: a length outside [0, T], or rows outside the tensors */
+  GDN_CHAIN_BAD_LEN = 9 /* chain: a length outside [0, T], rows outside the tensors or of another sequence */
 };
 
 /* Problem sizes.  B sequences, T node slots per tree (padded tree size),
@@ -463,8 +463,9 @@ typedef struct {
  *   out        out_dtype [rows][Hv][dv]  written: o_t = scale S_t q_t; must not
  *              overlap an input
  *   status     int32 [B] (may be NULL): GDN_CHAIN_BAD_LEN for a sequence whose
- *              length is negative or above T, or whose rows are outside
- *              [0, rows); 0 otherwise
+ *              length is negative or above T, whose rows are outside [0, rows),
+ *              or (where start goes backwards) among those of a sequence before
+ *              it that has neither of these; 0 otherwise
  * A sequence without tokens, or with a non-zero status, keeps S and gets
  * conv_state_out = conv_state.  No tensor may overlap S, conv_state_out or
  * status.  A decay below the smallest normal float counts as that in the

@@ -194,7 +194,7 @@ __global__ __launch_bounds__(kPrepThreads, 4) void chunk_kernel(ChainArgs a, Par
   const int tid = threadIdx.x, lane = tid % kWave, w = __builtin_amdgcn_readfirstlane(tid / kWave);
   const int n16 = lane & 15, q4 = lane >> 4;
   const int hk = blockIdx.x, m = blockIdx.y, b = part.b0 + blockIdx.z;
-  const Tokens tk = tokens_of(a, b);
+  const Tokens tk = tokens_of<false>(a, b);  // only its own slot is written
   const int n0 = (part.c0 + m) * kC, nt = min(kC, tk.n - n0);
   if (nt <= 0) return;
   const int dk = a.dk, dv = a.dv, per = a.Hv / a.Hk, C = 2 * a.Hk * dk + a.Hv * dv;
