@@ -396,11 +396,11 @@ __global__ __launch_bounds__(kPrepThreads, 4) void chunk_kernel(ChainArgs a, Par
           }
           t[i] = y;
         }
-        __builtin_amdgcn_wave_barrier();  // rows are read before they are replaced
+        wave_lds_order();  // rows are read before they are replaced
 #pragma unroll
         for (int i = 0; i < 16; ++i) d[i * kLd + n16] = t[i];
       }
-      __builtin_amdgcn_wave_barrier();
+      wave_lds_order();
       // blocks below: X_j = T_jj, X_i = -T_ii sum_k A_ik X_k down a column of blocks
       auto block = [&](int i, int k) { return *reinterpret_cast<const f32x4*>(x + (16 * i + n16) * kLd + 16 * k + 4 * q4); };
       auto diagonal = [&](int j) {
@@ -422,7 +422,7 @@ __global__ __launch_bounds__(kPrepThreads, 4) void chunk_kernel(ChainArgs a, Par
       const f32x4 x20 = -times(t2, times(a21, x10, times(a20, x0, zero)), zero),
                   x31 = -times(t3, times(a32, x21, times(a31, x1, zero)), zero);
       const f32x4 x30 = -times(t3, times(a32, x20, times(a31, x10, times(a30, x0, zero))), zero);
-      __builtin_amdgcn_wave_barrier();
+      wave_lds_order();
       auto put_block = [&](int i, int j, f32x4 c) {
 #pragma unroll
         for (int r = 0; r < 4; ++r) x[(16 * i + 4 * q4 + r) * kLd + 16 * j + n16] = c[r];

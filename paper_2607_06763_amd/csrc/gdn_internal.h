@@ -120,6 +120,14 @@ __device__ __forceinline__ int opaque(int x) {
   return x;
 }
 
+// Orders LDS accesses of one wave (no instruction besides the waits the
+// compiler places for the data itself).
+__device__ __forceinline__ void wave_lds_order() {
+  __builtin_amdgcn_fence(__ATOMIC_RELEASE, "wavefront", "local");
+  __builtin_amdgcn_wave_barrier();
+  __builtin_amdgcn_fence(__ATOMIC_ACQUIRE, "wavefront", "local");
+}
+
 // ---------------------------------------------------------------------------
 // Cross-lane sums with DPP (VALU-rate, no LDS round trip).
 // ---------------------------------------------------------------------------

@@ -70,14 +70,6 @@ __device__ __forceinline__ f16x4 ld_tr(const unsigned char* p) {
   return __builtin_bit_cast(f16x4, __builtin_amdgcn_ds_read_tr16_b64_v4f16((lds_p)(p)));
 }
 
-// Orders LDS accesses of one wave (no instruction besides the waits the
-// compiler places for the data itself).
-__device__ __forceinline__ void wave_lds_order() {
-  __builtin_amdgcn_fence(__ATOMIC_RELEASE, "wavefront", "local");
-  __builtin_amdgcn_wave_barrier();
-  __builtin_amdgcn_fence(__ATOMIC_ACQUIRE, "wavefront", "local");
-}
-
 // x, or 0 when it is not finite
 __device__ __forceinline__ float finite(float x) { return fabsf(x) < __builtin_inff() ? x : 0.0f; }
 
