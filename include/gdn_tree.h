@@ -29,8 +29,8 @@
  *    it; nothing synchronises the host except a workspace allocation (see
  *    Workspaces below).  Pointers must be 16-byte aligned.
  *  * Workspaces.  gdn_tree_verify and gdn_tree_step above 128 slots,
- *    gdn_tree_verify_chunked and gdn_tree_attend pass intermediate results
- *    through a device buffer that the library allocates on the first call that
+ *    gdn_tree_verify_chunked, gdn_tree_attend and gdn_chain above
+ *    GDN_CHAIN_STEP_T tokens pass intermediate results through a device buffer that the library allocates on the first call that
  *    needs it and keeps per (device, stream).  A call that needs more gets a
  *    larger buffer (hipMalloc) in its place; one that was handed out is not
  *    released before the process ends, so that a captured graph may go on
@@ -478,9 +478,10 @@ typedef struct {
  * output, and the state, may be off by about 2^-34 of the largest value (or row of
  * the state) of its head in this chunk or the one before, also where the decays
  * have forgotten that since, which the token by token form does not have.  They go
- * through a workspace that the library keeps (see Workspaces above), at most
- * GDN_CHAIN_WORKSPACE bytes or what one chunk of one sequence needs:
- * a chunk takes 768 Hk dk + 25600 Hv bytes (dk of 16 as 32). */
+ * through a workspace that the library keeps (see Workspaces above, also for how
+ * much more than a call's need it may hold).  A call needs at most
+ * GDN_CHAIN_WORKSPACE bytes, or what one chunk of one sequence does: a chunk takes
+ * 768 Hk dk + 25600 Hv bytes (dk of 16 as 32). */
 #define GDN_CHAIN_STEP_T 20
 #define GDN_CHAIN_WORKSPACE (1u << 28)
 int gdn_chain(const gdn_chain_dims* dims, const int32_t* start, const int32_t* n_new, const void* q,

@@ -697,8 +697,8 @@ __device__ __forceinline__ bool tail(const ChainArgs& a, const Part& part, const
 //
 // Bound by the vector and matrix instructions of a wave, which do not overlap
 // enough: 4 sequences of 4096 tokens of 48 value heads of 128, 192 workgroups of
-// eight waves, 590 us, 15000 to 17000 clocks a chunk; the matrix units are busy for
-// 34 % of them, the vector units for 48 % (operands made of values and of V', scales).
+// eight waves, 597 us, 15000 to 17000 clocks a chunk; the matrix units are busy for
+// 33 % of them, the vector units for 48 % (operands made of values and of V', scales).
 // ---------------------------------------------------------------------------
 template <typename TIn, int DKP, int NW>
 struct Scan {
@@ -925,9 +925,10 @@ __global__ __launch_bounds__(NW * kWave) void scan_kernel(ChainArgs a, Part part
 // do all loads (a wave has at most 64 on their way).
 //
 // Bound by the state's wave, whose steps wait for one another (8192 tokens of one
-// sequence of 48 heads of 128: 409 us, 6500 to 7000 clocks a chunk, matrix units 22 %
-// busy), and behind it by the loads, 170 KB a chunk and CU at about 30 bytes a clock.
-// With one wave for both 1024 tokens of 32 such heads take 109 us, with two 70.
+// sequence of 48 heads of 128: 412 us, 6500 to 7000 clocks a chunk, matrix units 22 %
+// busy).  The loads, 126 KB a chunk and workgroup (K, Q, K^T 96, the inverse and Y 24,
+// raw values 5), come to 19 bytes a clock and CU.  With one wave for both 1024 tokens of
+// 32 such heads take 109 us, with two 73.
 // ---------------------------------------------------------------------------
 constexpr int kLoaders = 2;
 
@@ -1227,13 +1228,13 @@ int launch_pairs(const ChainArgs& a, const Part& p, hipStream_t stream) {
 // The fewest of a head's channels a workgroup that leave at most one for each of the
 // 256 CUs, else all of them.  us for 1024 tokens and heads of 128, one key head a value
 // head (pairs of waves: 1 and 2 of them; waves: 2, 4 and 8):
-//   32 heads    70  71   109 109 130
-//   48         116  82   117 116 139
-//   64         124  90   122 121 143
-//   80         173 142   213 134 156
-//   128        282 207   260 187 207
-//   144          - 298   389 303 244
-//   256        583 429   545 382 324
+//   32 heads    73  77   111 109 134
+//   48         120  84   118 117 143
+//   64         127  93   125 123 148
+//   80         176 144   214 135 160
+//   128        284 207   262 187 210
+//   144        362 291   390 305 248
+//   256        589 431   549 381 330
 template <typename TIn, typename TOut, int DKP>
 int launch_scan(const ChainArgs& a, const Part& p, hipStream_t stream) {
   const int groups = a.dv / 16;  // of 16 value channels

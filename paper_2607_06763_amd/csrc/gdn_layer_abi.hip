@@ -98,8 +98,10 @@ int gdn_chain(const gdn_chain_dims* dims, const int32_t* start, const int32_t* n
   a.status = status;
   // A token costs the steps about the same each, the chunked form 64 of them.
   // us for 16 and 24 tokens (steps, chunks; chunks take the same up to 64), 16 / 48
-  // heads of 128: one sequence 18.5, 24.6 and 25.6, 24.6; 8 of them 49, 51 and 70,
-  // 51; 32 of them 95, 120 and 132, 120; 16 of 4 / 8 heads of 64: 13.2, 21 and 18.2, 21
+  // heads of 128: one sequence 18, 24 and 25, 24; 8 of them 49, 50 and 72, 51; 32 of
+  // them 95, 119 and 131, 121; 16 of 4 / 8 heads of 64: 13, 21 and 18, 21.  They cross at
+  // 23, 17, 22 and 29 tokens; the one limit costs the second 61 for 50 at 20 tokens, the
+  // last 21 for 18 at 24.
   return a.T <= GDN_CHAIN_STEP_T ? launch_chain_steps(a, stream) : launch_chain_chunks(a, stream);
 }
 

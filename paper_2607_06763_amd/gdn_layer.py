@@ -75,7 +75,8 @@ def chain(d: ChainDims, q, k, v, alpha, beta, conv_w, conv_state, conv_state_out
           stream=None) -> None:
     """gdn_chain: the gated delta rule over sequences; S in place, conv_state to
     conv_state_out.  Tensors [B][T][...] (n_new int32 [B]: tokens of each), or
-    packed [rows][...] with start int32 [B + 1]."""
+    packed [rows][...] with start int32 [B + 1], which does not go backwards
+    (status 9 for a sequence that would take rows of one before it)."""
     import torch
     i32, f32 = torch.int32, torch.float32
     it, ot, ks, vs, gs, ws, cs, ss, ls = d.shapes(start is not None)

@@ -95,7 +95,10 @@ class HybridModel:
 class Decoder:
     """B sequences, draft trees of up to T slots.  Every sequence has
     max_pages pages of the caches to itself; u float32 [B][n] holds the random
-    number of each position, for sequences of up to n tokens."""
+    number of each position, for sequences of up to n tokens.  prompt_form:
+    "chain" needs no tree and reads the prompt out in 32 bits instead of fp16;
+    "tree" stays the default because the two round differently, and a program
+    that does not choose keeps the tokens that it had."""
 
     def __init__(self, model: HybridModel, B: int, T: int, u: np.ndarray, max_pages: int = 32, page: int = 16,
                  dtype: str = "f32", temperature=None, top_k=None, top_p=None, min_p=None, device="cuda",
